@@ -1,8 +1,9 @@
 """Build the HIP library ``libsvfsim.so`` for gfx950 with hipcc.
 
 The library holds every kernel of the simulator and the host runtime behind
-the C ABI of ``include/svfsim.h``, plus the host-side exact optimum of tiny
-burst instances (``include/svfopt.h``).  It is built in-tree so that the same file
+the C ABI of ``include/svfsim.h``, the paged cache's operators
+(``include/svfkv.h``) and the host-side exact optimum of tiny burst instances
+(``include/svfopt.h``).  It is built in-tree so that the same file
 is loaded by the tests, the smoke check and the benchmark.
 """
 
@@ -23,6 +24,9 @@ ARCH = os.environ.get("SVFSIM_ARCH", "gfx950")
 # (the simulation kernels are bound by scalar instruction issue).
 GPU_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-mllvm", "-structurizecfg-skip-uniform-regions"]
+# The cache's kernels are ordinary vector code: the same without the branch flag.
+KV_GPU_FLAGS = GPU_FLAGS[:4]
+KV_KERNELS = ("svf_kv_append", "svf_kv_attend", "svf_kv_evict")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-I", INCLUDE, "-I", CSRC]
 
 
@@ -39,12 +43,19 @@ def build(verbose: bool = False) -> str:
     na_o = os.path.join(BUILD, "svf_noalloc.o")
     _run(["hipcc", f"--offload-arch={ARCH}", *COMMON, *GPU_FLAGS, "-c",
           os.path.join(CSRC, "svf_noalloc.hip"), "-o", na_o])
+    kv_o = []
+    for name in KV_KERNELS:
+        kv_o.append(os.path.join(BUILD, name + ".o"))
+        _run(["hipcc", f"--offload-arch={ARCH}", *COMMON, *KV_GPU_FLAGS, "-c",
+              os.path.join(CSRC, name + ".hip"), "-o", kv_o[-1]])
+    kv_o.append(os.path.join(BUILD, "svf_kv.o"))
+    _run(["hipcc", *COMMON, "-c", os.path.join(CSRC, "svf_kv.cpp"), "-o", kv_o[-1]])
     opt_o = os.path.join(BUILD, "svf_opt.o")
     _run(["hipcc", *COMMON, "-c", os.path.join(CSRC, "svf_runtime.cpp"), "-o", rt_o])
     _run(["hipcc", *COMMON, "-c", os.path.join(CSRC, "svf_opt.cpp"), "-o", opt_o])
     tmp = LIB + ".tmp"
-    _run(["hipcc", f"--offload-arch={ARCH}", "-shared", "-fPIC", kern_o, na_o, rt_o, opt_o, "-pthread",
-          "-o", tmp])
+    _run(["hipcc", f"--offload-arch={ARCH}", "-shared", "-fPIC", kern_o, na_o, rt_o, opt_o, *kv_o,
+          "-pthread", "-o", tmp])
     os.replace(tmp, LIB)
     if verbose:
         print(LIB)

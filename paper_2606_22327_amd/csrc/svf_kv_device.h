@@ -1,0 +1,74 @@
+// svf_kv_device.h -- what the kernels of the paged key-value cache share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "svf_kv.h"
+
+namespace svfk {
+
+// A sequence of the batch: its new tokens are q rows [q0, q0 + n), its slots [0, len).
+struct Seq {
+    int q0, n, len;
+};
+
+__device__ inline int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+__device__ inline int seq_len(const KvView& kv, int i) {
+    return clampi(kv.kv_len[i], 0, kv.width << kv.shift);
+}
+
+__device__ inline Seq seq_of(const KvView& kv, int i) {
+    Seq s;
+    s.q0 = clampi(kv.q_offsets[i], 0, kv.tokens);
+    s.n = clampi(kv.q_offsets[i + 1], s.q0, kv.tokens) - s.q0;
+    s.len = seq_len(kv, i);
+    return s;
+}
+
+// The last sequence whose new tokens begin at or before ``token``: 64 offsets
+// are compared at a time, so the search takes one load for 64 sequences, two for 4096.
+// Called by whole waves with the same token in every lane.
+__device__ inline int find_seq(const KvView& kv, int token) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = kv.seqs;  // the answer lies in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 63) >> 6;
+        const int at = lane * step;
+        const bool le = at < n && kv.q_offsets[lo + at] <= token;
+        const int hits = __popcll(__ballot(le));
+        const int k = hits > 0 ? hits - 1 : 0;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
+// The pool row (page << shift | row) of slot j, or -1 where there is none.
+__device__ inline int pool_row(const KvView& kv, int seq, int j) {
+    const int page = kv.table[(int64_t)seq * kv.table_stride + (j >> kv.shift)];
+    const bool there = (unsigned)page < (unsigned)kv.num_pages;
+    return there ? (page << kv.shift) | (j & ((1 << kv.shift) - 1)) : -1;
+}
+
+__device__ inline int64_t row_offset(int row, int shift, int64_t page_stride, int64_t row_stride) {
+    return (int64_t)(row >> shift) * page_stride + (int64_t)(row & ((1 << shift) - 1)) * row_stride;
+}
+
+// Index of a pool row's entry in weight and position.
+__device__ inline int64_t stat_index(const KvView& kv, int row, int head) {
+    const int64_t page = row >> kv.shift;
+    return ((page * kv.kv_heads + head) << kv.shift) + (row & ((1 << kv.shift) - 1));
+}
+
+struct BF16 {
+    using T = __bf16;
+    typedef __bf16 V8 __attribute__((ext_vector_type(8)));
+};
+struct F16 {
+    using T = _Float16;
+    typedef _Float16 V8 __attribute__((ext_vector_type(8)));
+};
+
+}  // namespace svfk

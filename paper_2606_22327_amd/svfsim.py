@@ -38,7 +38,8 @@ STATUS = {0: "done", 1: "exhausted", 2: "running"}
 EXPORTS = ("svf_create", "svf_reset", "svf_step", "svf_run", "svf_read", "svf_stats",
            "svf_set_profiling", "svf_timings", "svf_shape", "svf_destroy",
            "svf_last_error", "svf_abi_version", "svf_opt_burst", "svf_opt_burst_batch",
-           "svf_run_noalloc")
+           "svf_run_noalloc", "svf_kv_append", "svf_kv_attend", "svf_kv_attend_workspace",
+           "svf_kv_evict", "svf_kv_evict_workspace")
 
 
 class SvfError(RuntimeError):
@@ -120,9 +121,14 @@ def load(path: str = LIB_PATH):
     lib.svf_opt_burst.argtypes = [I32, V, V, I64, I64, ctypes.POINTER(I64), ctypes.POINTER(I64)]
     lib.svf_opt_burst_batch.argtypes = [I32, V, V, V, V, I64, I32, V, V, V]
     lib.svf_run_noalloc.argtypes = [ctypes.POINTER(BatchDesc), V, V, V, V, V, V]
+    for name in ("svf_kv_append", "svf_kv_attend", "svf_kv_evict"):
+        getattr(lib, name).argtypes = [V, V, V, V]
     for name in EXPORTS:
         if name not in ("svf_last_error",):
             getattr(lib, name).restype = ctypes.c_int
+    for name in ("svf_kv_attend_workspace", "svf_kv_evict_workspace"):
+        getattr(lib, name).argtypes = [V, V, V]
+        getattr(lib, name).restype = I64
     _lib = lib
     return lib
 
