@@ -104,6 +104,11 @@ int check_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_atte
     return SVF_OK;
 }
 
+AttendSizes sizes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
+    return {c->num_pages,  c->page_size, c->kv_heads,    a->heads, c->head_dim, c->dtype,
+            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0};
+}
+
 int check_evict(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_evict_args* a) {
     if (int rc = check_sizes(c, b)) return rc;
     if (!a) return fail(SVF_EINVAL, "args must not be NULL");
@@ -170,8 +175,7 @@ int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_app
 
 int64_t svf_kv_attend_workspace(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
     if (int rc = check_attend(c, b, a)) return rc;
-    return (int64_t)attend_workspace(c->num_pages, c->page_size, c->kv_heads, a->heads, c->head_dim, b->num_tokens,
-                                     b->num_seqs, a->add_weight != 0);
+    return attend_workspace(sizes(c, b, a));
 }
 
 int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, void* hip_stream) {
@@ -203,7 +207,8 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     k.causal = a->causal != 0;
     k.window = a->window;
     k.add_weight = a->add_weight != 0;
-    return launched(launch_attend(k, c->dtype, c->head_dim, static_cast<hipStream_t>(hip_stream)));
+    k.q_wide = aligned(a->q, 16) && a->q_token_stride % 8 == 0 && a->q_head_stride % 8 == 0;
+    return launched(launch_attend(k, sizes(c, b, a), static_cast<hipStream_t>(hip_stream)));
 }
 
 int64_t svf_kv_evict_workspace(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_evict_args* a) {

@@ -46,6 +46,13 @@ struct AttendArgs {
     int64_t q_tok, q_head, o_tok, o_head;  // bytes
     float scale;  // times log2(e)
     int32_t heads, causal, window, add_weight;
+    int32_t q_wide;  // q can be read 16 bytes at a time
+    int32_t few;     // rows of a key head up to which the kernels of few rows take a sequence
+};
+
+// The sizes that an attention call's workspace and launches go by.
+struct AttendSizes {
+    int32_t num_pages, page_size, kv_heads, heads, dim, dtype, tokens, seqs, width, max_q, add_weight;
 };
 
 struct EvictArgs {
@@ -57,11 +64,15 @@ struct EvictArgs {
 };
 
 hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStream_t s);
-hipError_t launch_attend(const AttendArgs& a, int32_t dtype, int32_t dim, hipStream_t s);
+hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+int64_t attend_workspace(const AttendSizes& z);
 
-size_t attend_workspace(int32_t num_pages, int32_t page_size, int32_t kv_heads, int32_t heads,
-                        int32_t dim, int32_t tokens, int32_t seqs, bool add_weight);
+// The kernels of few rows (svf_kv_rows.hip).
+int32_t few_rows(const AttendSizes& z);
+int64_t rows_workspace(const AttendSizes& z);
+hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s);
+
 // Pairs (hole, mover) that one sequence's key head can have.
 inline int64_t evict_pairs(int64_t capacity, int64_t budget) {
     return capacity <= budget ? 0 : (capacity - budget < budget ? capacity - budget : budget);

@@ -1,0 +1,109 @@
+// svf_kv_attend.h -- what the attention kernels of the paged cache share.
+#pragma once
+
+#include "svf_kv_device.h"
+
+namespace svfk {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Sixteen 16-bit elements' worth of a matrix product, and the type's constants.
+// kShift: probabilities are scaled by 2^kShift, which cancels against their sum,
+// so that the small ones of a 16-bit float stay above its subnormal numbers.
+struct BF16M : BF16 {
+    static constexpr float kShift = 0.f;
+    static constexpr uint16_t kInf = 0x7f80;
+    static __device__ inline f32x4 mfma16(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+struct F16M : F16 {
+    static constexpr float kShift = 14.f;
+    static constexpr uint16_t kInf = 0x7c00;
+    static __device__ inline f32x4 mfma16(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Two elements in a word: whether one of them is no finite number; the word with zeros in the place of such; and
+// two bits for each, the first for +infinity, the second for -infinity, both for no number.
+template <class E>
+__device__ inline bool odd_pair(uint32_t w) {
+    return (w & E::kInf) == E::kInf || (w >> 16 & E::kInf) == E::kInf;
+}
+template <class E>
+__device__ inline uint32_t finite_pair(uint32_t w) {
+    if ((w & E::kInf) == E::kInf) w &= 0xffff0000u;
+    if ((w >> 16 & E::kInf) == E::kInf) w &= 0x0000ffffu;
+    return w;
+}
+template <class E>
+__device__ inline uint32_t odd_marks_of(uint32_t w) {
+    uint32_t marks = 0;
+    for (int i = 0; i < 2; i++) {
+        const uint32_t b = w >> 16 * i & 0xffff;
+        if ((b & E::kInf) == E::kInf) marks |= ((b & 0x7fff) != E::kInf ? 3u : b & 0x8000 ? 2u : 1u) << 2 * i;
+    }
+    return marks;
+}
+// Adds what the marks of n values stand for.
+__device__ inline void add_marks(uint32_t marks, float* acc, int n) {
+    if (marks == 0) return;
+    for (int i = 0; i < n; i++) {
+        if (marks >> 2 * i & 1) acc[i] += INFINITY;
+        if (marks >> 2 * i & 2) acc[i] -= INFINITY;
+    }
+}
+
+// The first slot that any row of the sequence sees.
+__device__ inline int first_slot(const AttendArgs& p, const Seq& s) {
+    return p.window > 0 ? max(0, s.len - s.n - p.window + 1) : 0;
+}
+
+// Where a lane reads a slot that is not there: a row of zeros, so that loads need no branch.
+static __device__ __align__(16) const char kZeroRow[512] = {};
+__device__ inline const char* zero_row() { return kZeroRow; }
+
+// KS operands of a row's query: dimensions k * 32 + g * 8 and the seven behind.
+template <class E, int KS>
+__device__ inline void load_query(typename E::V8* q, const char* at, int g, bool valid, bool wide) {
+    using T = typename E::T;
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+        if (!valid) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) q[k][i] = (T)0.f;
+        } else if (wide) {
+            q[k] = *(const typename E::V8*)(at + (k * 32 + g * 8) * 2);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) q[k][i] = *(const T*)(at + (k * 32 + g * 8 + i) * 2);
+        }
+    }
+}
+
+// N of a row's dimensions from d0: the sums over the softmax's denominator, rounded once, and with the
+// first of them the row's statistic.
+template <class E, int N>
+__device__ inline void write_row(const AttendArgs& p, int token, int h, int d0, const float* acc, float den, float top) {
+    using T = typename E::T;
+    typedef T V __attribute__((ext_vector_type(N)));
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    V v;
+#pragma unroll
+    for (int j = 0; j < N; j++) v[j] = (T)(acc[j] * inv);
+    *(V*)(p.out + token * p.o_tok + h * p.o_head + d0 * 2) = v;
+    if (d0 == 0) p.lse[(int64_t)token * p.heads + h] = (top - E::kShift + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
+}
+
+// Rows of one key head of a sequence that has more new tokens than it may.
+template <class T, int D>
+__device__ inline void fill_nan(const AttendArgs& p, const Seq& s, int head, int G, int tid, int threads) {
+    const T nan = (T)__builtin_nanf("");
+    for (int64_t i = tid; i < (int64_t)s.n * G * D; i += threads) {
+        const int row = (int)(i / D), d = (int)(i - (int64_t)row * D), t = row / G, h = head * G + row - t * G;
+        *(T*)(p.out + (s.q0 + t) * p.o_tok + h * p.o_head + d * 2) = nan;
+        if (d == 0) p.lse[(int64_t)(s.q0 + t) * p.heads + h] = __builtin_nanf("");
+    }
+}
+
+}  // namespace svfk

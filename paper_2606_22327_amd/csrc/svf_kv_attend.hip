@@ -1,8 +1,14 @@
 // svf_kv_attend.hip -- attention of new tokens over the paged cache.
-#include "svf_kv_device.h"
+#include "svf_kv_attend.h"
 
 namespace svfk {
 namespace {
+
+// Whether these kernels take the sequence, and not those of few rows.
+__device__ inline bool ours(const AttendArgs& p, const Seq& s) {
+    if (s.n > p.kv.max_q) return p.few == 0;
+    return (int64_t)s.n * (p.heads / p.kv.kv_heads) > p.few;
+}
 
 // Row (t, h): one wave; a lane scores one slot at a time, then the wave adds
 // up the values of 64 slots, a lane for D / 64 dimensions.
@@ -12,7 +18,7 @@ __global__ __launch_bounds__(64) void k_attend(AttendArgs p) {
     const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
     const int seq = find_seq(p.kv, t);
     const Seq s = seq_of(p.kv, seq);
-    if (t < s.q0 || t >= s.q0 + s.n) return;
+    if (t < s.q0 || t >= s.q0 + s.n || !ours(p, s)) return;
     const int head = h / (p.heads / p.kv.kv_heads);
     const int r = s.len - s.n + (t - s.q0);
     const int hi = p.causal ? r + 1 : s.len, lo = p.window > 0 ? max(0, r - p.window + 1) : 0;
@@ -65,7 +71,7 @@ __global__ __launch_bounds__(256) void k_weight(AttendArgs p) {
     using T = typename E::T;
     const int j = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y, seq = blockIdx.z;
     const Seq s = seq_of(p.kv, seq);
-    if (j >= s.len || s.n > p.kv.max_q) return;
+    if (j >= s.len || s.n > p.kv.max_q || !ours(p, s)) return;
     const int row = pool_row(p.kv, seq, j);
     if (row < 0) return;
     const T* k = (const T*)(p.kv.k + head * p.kv.k_head + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row));
@@ -102,12 +108,17 @@ hipError_t launch(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_attend(const AttendArgs& a, int32_t dtype, int32_t dim, hipStream_t s) {
-    if (dtype == SVF_KV_BF16)
-        return dim == 64 ? launch<BF16, 64>(a, s) : dim == 128 ? launch<BF16, 128>(a, s) : launch<BF16, 256>(a, s);
-    return dim == 64 ? launch<F16, 64>(a, s) : dim == 128 ? launch<F16, 128>(a, s) : launch<F16, 256>(a, s);
-}
+int64_t attend_workspace(const AttendSizes& z) { return rows_workspace(z); }
 
-size_t attend_workspace(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, bool) { return 0; }
+hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s) {
+    a.few = few_rows(z);
+    if (a.few) {
+        hipError_t e = launch_rows(a, z, a.ws, s);
+        if (e != hipSuccess || (int64_t)z.max_q * (z.heads / z.kv_heads) <= a.few) return e;
+    }
+    if (z.dtype == SVF_KV_BF16)
+        return z.dim == 64 ? launch<BF16, 64>(a, s) : z.dim == 128 ? launch<BF16, 128>(a, s) : launch<BF16, 256>(a, s);
+    return z.dim == 64 ? launch<F16, 64>(a, s) : z.dim == 128 ? launch<F16, 128>(a, s) : launch<F16, 256>(a, s);
+}
 
 }  // namespace svfk

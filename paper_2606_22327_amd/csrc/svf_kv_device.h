@@ -8,6 +8,13 @@
 
 namespace svfk {
 
+// A load that the compiler knows to be of global memory, whatever the address was chosen from.
+template <class V>
+__device__ inline V load_global(uint64_t at) {
+    typedef const __attribute__((address_space(1))) V* G;
+    return *(G)at;
+}
+
 // A sequence of the batch: its new tokens are q rows [q0, q0 + n), its slots [0, len).
 struct Seq {
     int q0, n, len;

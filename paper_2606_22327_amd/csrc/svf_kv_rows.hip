@@ -1,0 +1,537 @@
+// svf_kv_rows.hip -- attention over the paged cache of sequences with few rows
+// (new tokens times query heads of a key head): single tokens and short chunks.
+#include "svf_kv_attend.h"
+
+namespace svfk {
+namespace {
+
+// Slots that a workgroup takes at a time: 32 for each of its four waves.
+constexpr int kUnit = 128;
+
+// What the launches of one call share, in the workspace.
+struct RowsPlan {
+    int64_t* first_unit;  // [seqs + 1]: units of a key head before each sequence
+    float* part;          // [2 * groups][rows * (D + 4)]: partial results
+    float* scores;        // [units][rows][kUnit] (add_weight): scores in log2 terms
+    int64_t score_units;  // units that scores has room for
+    int32_t groups;       // workgroups over which the units are dealt out
+    int32_t rows;         // rows of a sequence's key head at most
+};
+
+// Units of one key head of a sequence, 0 where this kernel leaves it to another.
+// One without a slot still has its rows to write.
+__device__ inline int units_of(const AttendArgs& p, const Seq& s, int rows) {
+    if (s.n <= 0) return 0;
+    const int G = p.heads / p.kv.kv_heads;
+    if (s.n <= p.kv.max_q && (int64_t)s.n * G > rows) return 0;
+    if (s.n > p.kv.max_q) return 1;
+    const int lo = first_slot(p, s);
+    const int u = (s.len - lo + kUnit - 1) / kUnit;
+    return u > 0 ? u : 1;
+}
+
+// S^T = K Q^T and O^T = V^T P^T on 16x16x32 products, 32 slots at a time: a lane has the
+// scores of one row (l % 16) in both, so maxima and sums need two shuffles, and
+// the probabilities are the second product's operand where the first left them.
+// The slots that a lane's four-by-two scores belong to are the slots
+// whose values it loads: eight rows of a head, D / 16 dimensions each, put
+// together by byte permutes. Keys and values go from memory to registers
+// once and through no LDS.
+template <class E, int D>
+struct Tile {
+    typename E::V8 k[2][D / 32];
+    uint32_t v[8][D / 32];  // two dimensions a word
+};
+
+// Where slots lie: a lane has the addresses of slot lane % 32 of the wave's tile and hands them
+// to the lanes that load it. A slot that is not there is a row of zeros.
+struct Where {
+    uint64_t k, v;
+    bool there;
+};
+
+__device__ inline uint64_t from_lane(uint64_t x, int lane) {
+    const uint32_t lo = __shfl((int)(uint32_t)x, lane), hi = __shfl((int)(x >> 32), lane);
+    return (uint64_t)hi << 32 | lo;
+}
+
+template <class E, int D>
+__device__ inline void load_k(Tile<E, D>& x, const Where& w) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+        const uint64_t at = from_lane(w.k, t * 16 + c) + g * 16;
+#pragma unroll
+        for (int s = 0; s < D / 32; s++) x.k[t][s] = load_global<typename E::V8>(at + s * 64);
+    }
+}
+
+template <class E, int D>
+__device__ inline void load_v(Tile<E, D>& x, const Where& w) {
+    typedef uint32_t Row __attribute__((ext_vector_type(D / 32)));
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const Row r = load_global<Row>(from_lane(w.v, (j >> 2) * 16 + g * 4 + (j & 3)) + c * (D / 8));
+#pragma unroll
+        for (int i = 0; i < D / 32; i++) x.v[j][i] = r[i];
+    }
+}
+
+// Waves of a SIMD that the registers of a tile leave room for.
+template <int D, int RT>
+constexpr int waves_per_simd() {
+    return D * RT <= 64 ? 4 : D * RT <= 128 ? 3 : D * RT <= 256 && D < 256 ? 2 : 1;
+}
+
+template <class E, int D, int RT>
+__global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(AttendArgs p, RowsPlan plan) {
+    using T = typename E::T;
+    using V8 = typename E::V8;
+    constexpr int KS = D / 32, VD = D / 16;
+    __shared__ float red[4][16][D + 4];
+    __shared__ float red_m[4][16], red_l[4][16];
+    __shared__ int64_t scan[4];
+    __shared__ uint32_t odd_marks[16 * RT][16];  // a word for D / 16 dimensions of a row
+    __shared__ int sh_seq;
+    __shared__ int64_t sh_first;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
+    const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads;
+
+    // Deal the units out: sequences in order, key head by key head, an equal run of units for
+    // every workgroup.
+    const int per = (p.kv.seqs + 255) / 256;
+    const int i0 = min(tid * per, p.kv.seqs), i1 = min(i0 + per, p.kv.seqs);
+    int64_t mine = 0;
+    for (int i = i0; i < i1; i++) mine += units_of(p, seq_of(p.kv, i), plan.rows);
+    int64_t incl = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t x = __shfl_up(incl, d);
+        if (lane >= d) incl += x;
+    }
+    if (lane == 63) scan[wave] = incl;
+    __syncthreads();
+    int64_t total = 0, before = incl - mine;
+    for (int w = 0; w < 4; w++) {
+        if (w < wave) before += scan[w];
+        total += scan[w];
+    }
+    const int64_t all = total * hk;
+    const int64_t a = all * blockIdx.x / plan.groups, b = all * (blockIdx.x + 1) / plan.groups;
+    if (blockIdx.x == 0) {
+        int64_t at = before;
+        for (int i = i0; i < i1; i++) {
+            plan.first_unit[i] = at;
+            at += units_of(p, seq_of(p.kv, i), plan.rows);
+        }
+        if (tid == 0) plan.first_unit[p.kv.seqs] = total;
+    }
+    if (a == b) return;
+    if (before * hk <= a && a < (before + mine) * hk) {
+        int64_t at = before;
+        int i = i0;
+        for (; i < i1; i++) {
+            const int u = units_of(p, seq_of(p.kv, i), plan.rows);
+            if (a < (at + u) * hk) break;
+            at += u;
+        }
+        sh_seq = i;
+        sh_first = at;
+    }
+    __syncthreads();
+    int seq = sh_seq;
+    int64_t first = sh_first;  // units of a key head before seq
+
+    for (int64_t pos = a; pos < b;) {
+        const Seq s = seq_of(p.kv, seq);
+        const int units = units_of(p, s, plan.rows);
+        if (pos >= (first + units) * hk) {  // a sequence done, or one without units
+            first += units;
+            seq++;
+            continue;
+        }
+        const int64_t rel = pos - first * hk;
+        const int head = (int)(rel / units), u0 = (int)(rel - (int64_t)head * units);
+        const int u1 = (int)min((int64_t)units, u0 + (b - pos));
+        const int64_t unit0 = pos;
+        pos += u1 - u0;
+        const int rows = s.n * G;
+        if (s.n > p.kv.max_q) {
+            fill_nan<T, D>(p, s, head, G, tid, 256);
+            continue;
+        }
+        const int lo = first_slot(p, s);
+        const int r0 = s.len - s.n;  // the first new token's slot
+        const char* kbase = p.kv.k + head * p.kv.k_head;
+        const char* vbase = p.kv.v + head * p.kv.v_head;
+
+        V8 q[RT][KS];
+        int last[RT], from[RT];  // a lane's rows see slots from .. last
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            const int row = rt * 16 + c;
+            const int t = row < rows ? row / G : 0;
+            const char* at = p.q + (s.q0 + t) * p.q_tok + (head * G + (row < rows ? row - t * G : 0)) * p.q_head;
+            load_query<E, KS>(q[rt], at, g, row < rows, p.q_wide);
+            last[rt] = p.causal ? r0 + t : s.len - 1;
+            from[rt] = p.window > 0 ? r0 + t - p.window + 1 : 0;
+        }
+        float m[RT], l[RT];
+        f32x4 o[RT][VD];
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            m[rt] = -INFINITY, l[rt] = 0.f;
+#pragma unroll
+            for (int j = 0; j < VD; j++) o[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        auto lookup = [&](int u) {
+            const int j = lo + u * kUnit + wave * 32 + (lane & 31);
+            const int row = u < u1 && j < s.len ? pool_row(p.kv, seq, j) : -1;
+            Where w;
+            w.there = row >= 0;
+            w.k = w.v = (uint64_t)zero_row();
+            if (w.there) {
+                w.k = (uint64_t)kbase + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row);
+                w.v = (uint64_t)vbase + row_offset(row, p.kv.shift, p.kv.v_page, p.kv.v_row);
+            }
+            return w;
+        };
+        for (int i = tid; i < 16 * RT * 16; i += 256) (&odd_marks[0][0])[i] = 0;
+        __syncthreads();
+        Tile<E, D> x;
+        Where now = lookup(u0), next = lookup(u0 + 1);
+        load_k(x, now);
+        load_v(x, now);
+        for (int u = u0; u < u1; u++) {
+            const Where later = lookup(u + 2);
+            const int base = lo + u * kUnit + wave * 32;
+            f32x4 sc[RT][2];
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    sc[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < KS; k++) sc[rt][t] = E::mfma16(x.k[t][k], q[rt][k], sc[rt][t]);
+                }
+            // which of the tile's slots are there: the same for every row
+            const uint32_t there = (uint32_t)__ballot(now.there);
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(x, next);
+            __builtin_amdgcn_sched_barrier(0);
+            V8 hi[RT], low[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int off = (i >> 2) * 16 + g * 4 + (i & 3), j = base + off;
+                    const bool vis = (there >> off & 1) && j <= last[rt] && j >= from[rt];
+                    float v = sc[rt][i >> 2][i & 3] * p.scale;
+                    v = vis ? v : -INFINITY;
+                    sc[rt][i >> 2][i & 3] = v;
+                    top = fmaxf(top, v);
+                }
+                if (plan.scores && unit0 + (u - u0) < plan.score_units && rt * 16 + c < rows) {
+                    float* to = plan.scores + ((unit0 + (u - u0)) * plan.rows + rt * 16 + c) * kUnit + wave * 32 + g * 4;
+                    *(f32x4*)to = sc[rt][0];
+                    *(f32x4*)(to + 16) = sc[rt][1];
+                }
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float peak = fmaxf(m[rt], top);
+                const float ref = (peak == -INFINITY ? 0.f : peak) - E::kShift;
+                const float keep = exp2_fast(m[rt] - (peak == -INFINITY ? 0.f : peak));
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float e = exp2_fast(sc[rt][i >> 2][i & 3] - ref);
+                    sum += e;
+                    // the probability as the sum of two numbers of the type: twice its bits, for
+                    // products that memory hides
+                    hi[rt][i] = (T)e;
+                    low[rt][i] = (T)(e - (float)hi[rt][i]);
+                }
+                l[rt] = l[rt] * keep + sum;  // of this lane's slots; the four lanes of a row are added at the end
+                m[rt] = peak;
+#pragma unroll
+                for (int j = 0; j < VD; j++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) o[rt][j][r] *= keep;
+            }
+            // A value that is no finite number would reach rows that do not see it (0 times infinity), and
+            // meet both halves of a probability.  It counts as 0 here, and the rows that see it
+            // get it from its marks.
+            {
+                u16x2 size = {0, 0};
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+#pragma unroll
+                    for (int w = 0; w < D / 32; w++)
+                        size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, x.v[i][w] & 0x7fff7fffu));
+                const bool odd = max(size.x, size.y) >= E::kInf;
+                if (__any(odd)) {
+                    // through this wave's part of ``red``, a word at a time: rare, and registers are scarce
+                    uint32_t* own = (uint32_t*)&red[wave][0][0] + lane;
+#pragma unroll
+                    for (int i = 0; i < 8 * (D / 32); i++) own[i * 64] = x.v[i / (D / 32)][i % (D / 32)];
+#pragma unroll 1
+                    for (int i = 0; i < 8 * (D / 32); i++) {
+                        const uint32_t pair = own[i * 64];
+                        if (!odd_pair<E>(pair)) continue;
+                        const int at = i / (D / 32), j = base + (at >> 2) * 16 + g * 4 + (at & 3);
+                        const uint32_t marks = odd_marks_of<E>(pair) << 4 * (i % (D / 32));
+                        for (int row = 0; row < rows; row++) {
+                            const int r = r0 + row / G;
+                            if ((!p.causal || j <= r) && (p.window == 0 || j > r - p.window)) atomicOr(&odd_marks[row][c], marks);
+                        }
+                        own[i * 64] = finite_pair<E>(pair);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8 * (D / 32); i++) x.v[i / (D / 32)][i % (D / 32)] = own[i * 64];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < VD; j++) {
+                uint4 t;
+                const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+                t.x = __builtin_amdgcn_perm(x.v[1][j / 2], x.v[0][j / 2], sel);
+                t.y = __builtin_amdgcn_perm(x.v[3][j / 2], x.v[2][j / 2], sel);
+                t.z = __builtin_amdgcn_perm(x.v[5][j / 2], x.v[4][j / 2], sel);
+                t.w = __builtin_amdgcn_perm(x.v[7][j / 2], x.v[6][j / 2], sel);
+                const V8 vt = __builtin_bit_cast(V8, t);
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++) {
+                    o[rt][j] = E::mfma16(vt, hi[rt], o[rt][j]);
+                    o[rt][j] = E::mfma16(vt, low[rt], o[rt][j]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(x, next);
+            __builtin_amdgcn_sched_barrier(0);
+            now = next;
+            next = later;
+        }
+
+        // The four waves' parts of a row, then the row: whole, or this workgroup's part of it.
+        const bool whole = u0 == 0 && u1 == units;
+        float* part = plan.part + (int64_t)(2 * blockIdx.x + (u0 == 0 ? 1 : 0)) * plan.rows * (D + 4);
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            if (rt * 16 >= rows) break;
+            float sum = l[rt];
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (g == 0) red_m[wave][c] = m[rt], red_l[wave][c] = sum;
+#pragma unroll
+            for (int r = 0; r < 4; r++)
+#pragma unroll
+                for (int j = 0; j < VD; j += 4)
+                    *(f32x4*)&red[wave][c][(g * 4 + r) * VD + j] =
+                        f32x4{o[rt][j][r], o[rt][j + 1][r], o[rt][j + 2][r], o[rt][j + 3][r]};
+            __syncthreads();
+            const int rr = tid >> 4, d0 = (tid & 15) * VD, row = rt * 16 + rr;
+            if (row < rows) {
+                float top = -INFINITY;
+                for (int w = 0; w < 4; w++) top = fmaxf(top, red_m[w][rr]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                float den = 0.f, acc[VD];
+#pragma unroll
+                for (int j = 0; j < VD; j++) acc[j] = 0.f;
+                for (int w = 0; w < 4; w++) {
+                    const float f = exp2_fast(red_m[w][rr] - ref);
+                    den += red_l[w][rr] * f;
+#pragma unroll
+                    for (int j = 0; j < VD; j++) acc[j] += red[w][rr][d0 + j] * f;
+                }
+                add_marks(odd_marks[row][tid & 15], acc, VD);
+                if (whole) {
+                    const int t = row / G, h = head * G + row - t * G;
+                    write_row<E, VD>(p, s.q0 + t, h, d0, acc, den, top);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VD; j += 4) *(f32x4*)&part[row * D + d0 + j] = f32x4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
+                    if (d0 == 0) {
+                        part[plan.rows * D + 2 * row] = top;
+                        part[plan.rows * D + 2 * row + 1] = den;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// The parts of a row that was split over workgroups, in the order of its units: one workgroup for a
+// row, eight parts at a time.
+template <class E, int D>
+__global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan) {
+    constexpr int VD = D / 32;
+    const int hk = p.kv.kv_heads, G = p.heads / hk;
+    const int seq = blockIdx.x / hk, head = blockIdx.x - seq * hk, row = blockIdx.y;
+    const int64_t first = plan.first_unit[seq], units = plan.first_unit[seq + 1] - first;
+    if (units < 2) return;
+    const int64_t all = plan.first_unit[p.kv.seqs] * hk;
+    const int64_t s0 = first * hk + head * units, s1 = s0 + units;
+    // workgroup w has units [all * w / groups, all * (w + 1) / groups): the one that holds unit x
+    auto holder = [&](int64_t x) {
+        int64_t w = x * plan.groups / all;
+        while (all * (w + 1) / plan.groups <= x) w++;
+        while (w > 0 && all * w / plan.groups > x) w--;
+        return (int)w;
+    };
+    const int w0 = holder(s0), w1 = holder(s1 - 1);
+    if (w0 == w1) return;
+    const Seq s = seq_of(p.kv, seq);
+    if (row >= s.n * G) return;
+    const int tid = threadIdx.x, sub = tid >> 5, d0 = (tid & 31) * VD;
+    const int64_t stride = (int64_t)plan.rows * (D + 4);
+    auto part_of = [&](int w) { return plan.part + (2 * (int64_t)w + (w == w0 ? 1 : 0)) * stride; };
+    float top = -INFINITY, den = 0.f, acc[VD];
+#pragma unroll
+    for (int j = 0; j < VD; j++) acc[j] = 0.f;
+    for (int w = w0 + sub; w <= w1; w += 8) {
+        // a workgroup whose run of units is empty has no part
+        if (all * w / plan.groups == all * (w + 1) / plan.groups) continue;
+        const float* q = part_of(w);
+        const float pm = q[plan.rows * D + 2 * row], pl = q[plan.rows * D + 2 * row + 1];
+        const float now = fmaxf(top, pm), ref = now == -INFINITY ? 0.f : now;
+        const float keep = exp2_fast(top - ref), f = exp2_fast(pm - ref);
+        den = den * keep + pl * f;
+#pragma unroll
+        for (int j = 0; j < VD; j++) acc[j] = acc[j] * keep + q[row * D + d0 + j] * f;
+        top = now;
+    }
+    __shared__ float red[8][D], red_m[8], red_l[8];
+#pragma unroll
+    for (int j = 0; j < VD; j++) red[sub][d0 + j] = acc[j];
+    if ((tid & 31) == 0) red_m[sub] = top, red_l[sub] = den;
+    __syncthreads();
+    if (tid >= 32) return;
+    top = -INFINITY;
+    for (int w = 0; w < 8; w++) top = fmaxf(top, red_m[w]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    den = 0.f;
+#pragma unroll
+    for (int j = 0; j < VD; j++) acc[j] = 0.f;
+    for (int w = 0; w < 8; w++) {
+        const float f = exp2_fast(red_m[w] - ref);
+        den += red_l[w] * f;
+#pragma unroll
+        for (int j = 0; j < VD; j++) acc[j] += red[w][d0 + j] * f;
+    }
+    const int t = row / G;
+    write_row<E, VD>(p, s.q0 + t, head * G + row - t * G, d0, acc, den, top);
+}
+
+// The weights of these sequences' slots from the scores and the rows' final statistics: a wave
+// for half a unit, its rows in order.
+template <class E>
+__global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan) {
+    const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
+    const int64_t all = plan.first_unit[p.kv.seqs] * hk;
+    for (int64_t half = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); half < 2 * all; half += (int64_t)gridDim.x * 4) {
+        const int64_t unit = half >> 1;
+        if (unit >= plan.score_units) return;
+        // the last sequence that begins at or before the unit
+        int lo = 0, n = p.kv.seqs;
+        while (n > 1) {
+            const int step = (n + 63) >> 6, at = lane * step;
+            const bool le = at < n && plan.first_unit[lo + at] * hk <= unit;
+            const int hits = __popcll(__ballot(le)), k = hits > 0 ? hits - 1 : 0;
+            lo += k * step;
+            n = min(step, n - k * step);
+        }
+        const Seq s = seq_of(p.kv, lo);
+        const int64_t units = plan.first_unit[lo + 1] - plan.first_unit[lo], rel = unit - plan.first_unit[lo] * hk;
+        if (units <= 0 || s.n > p.kv.max_q) continue;
+        const int head = (int)(rel / units);
+        const int j = first_slot(p, s) + (int)(rel - head * units) * kUnit + (int)(half & 1) * 64 + lane;
+        const int row = j < s.len ? pool_row(p.kv, lo, j) : -1;
+        const float* sc = plan.scores + unit * plan.rows * kUnit + (half & 1) * 64 + lane;
+        float sum = 0.f;
+        for (int r = 0; r < s.n * G; r++) {
+            const int t = r / G;
+            const float lse = p.lse[(int64_t)(s.q0 + t) * p.heads + head * G + r - t * G] * 1.4426950408889634f;
+            if (lse != -INFINITY) sum += exp2_fast(sc[r * kUnit] - lse);
+        }
+        if (row >= 0) p.kv.weight[stat_index(p.kv, row, head)] += sum;
+    }
+}
+
+template <class E, int D>
+hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
+    if (plan.rows <= 16)
+        k_attend_rows<E, D, 1><<<plan.groups, 256, 0, s>>>(a, plan);
+    else if (plan.rows <= 32)
+        k_attend_rows<E, D, 2><<<plan.groups, 256, 0, s>>>(a, plan);
+    else if constexpr (D <= 128)
+        k_attend_rows<E, D, 4><<<plan.groups, 256, 0, s>>>(a, plan);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t cap = (int64_t)a.kv.width << a.kv.shift;
+    if (cap > kUnit) {  // else no row has a second unit
+        k_join_rows<E, D><<<dim3(a.kv.seqs * a.kv.kv_heads, plan.rows), 256, 0, s>>>(a, plan);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.add_weight) k_weight_rows<E><<<2048, 256, 0, s>>>(a, plan);
+    return hipGetLastError();
+}
+
+constexpr int kGroups = 768;
+
+int64_t round256(int64_t x) { return (x + 255) & ~int64_t(255); }
+
+struct Layout {
+    int64_t part, scores, units, bytes;
+    int32_t groups, rows;
+};
+
+Layout layout(const AttendSizes& z) {
+    Layout y;
+    const int64_t cap = (int64_t)z.width * z.page_size;
+    const int64_t most = (int64_t)z.seqs * z.kv_heads * ((cap + kUnit - 1) / kUnit > 0 ? (cap + kUnit - 1) / kUnit : 1);
+    y.groups = (int32_t)(most < kGroups ? most : kGroups);
+    y.rows = few_rows(z);
+    y.part = round256((int64_t)(z.seqs + 1) * 8);
+    y.scores = y.part + round256((int64_t)2 * y.groups * y.rows * (z.dim + 4) * 4);
+    // every page once at most: the pool's slots, and a unit that is not full for each sequence
+    y.units = 0;
+    if (z.add_weight) {
+        y.units = ((int64_t)z.num_pages * z.page_size / kUnit + z.seqs) * z.kv_heads;
+        if (y.units > most) y.units = most;
+    }
+    y.bytes = y.scores + round256(y.units * y.rows * kUnit * 4);
+    return y;
+}
+
+}  // namespace
+
+// Rows that these kernels take: a whole batch's where no sequence has more than 64 (32 of 256 dimensions), else
+// single tokens' (or 16, whichever is more).
+int32_t few_rows(const AttendSizes& z) {
+    const int32_t G = z.heads / z.kv_heads, most = z.dim <= 128 ? 64 : 32;
+    const int64_t want = (int64_t)z.max_q * G;
+    if (want <= most) return (int32_t)(want < 1 ? 1 : want);
+    const int32_t single = G > 16 ? G : 16;
+    return single <= most ? single : 0;
+}
+
+int64_t rows_workspace(const AttendSizes& z) { return few_rows(z) ? layout(z).bytes : 0; }
+
+hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {
+    const Layout y = layout(z);
+    RowsPlan plan;
+    plan.first_unit = (int64_t*)ws;
+    plan.part = (float*)(ws + y.part);
+    plan.scores = a.add_weight ? (float*)(ws + y.scores) : nullptr;
+    plan.score_units = y.units;
+    plan.groups = y.groups;
+    plan.rows = y.rows;
+    if (z.dtype == SVF_KV_BF16)
+        return z.dim == 64 ? launch<BF16M, 64>(a, plan, s) : z.dim == 128 ? launch<BF16M, 128>(a, plan, s) : launch<BF16M, 256>(a, plan, s);
+    return z.dim == 64 ? launch<F16M, 64>(a, plan, s) : z.dim == 128 ? launch<F16M, 128>(a, plan, s) : launch<F16M, 256>(a, plan, s);
+}
+
+}  // namespace svfk
