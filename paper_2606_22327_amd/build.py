@@ -26,7 +26,7 @@ GPU_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-mllvm", "-structurizecfg-skip-uniform-regions"]
 # The cache's kernels are ordinary vector code: the same without the branch flag.
 KV_GPU_FLAGS = GPU_FLAGS[:4]
-KV_KERNELS = ("svf_kv_append", "svf_kv_attend", "svf_kv_rows", "svf_kv_evict")
+KV_KERNELS = ("svf_kv_append", "svf_kv_rows", "svf_kv_chunk", "svf_kv_evict")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-I", INCLUDE, "-I", CSRC]
 
 

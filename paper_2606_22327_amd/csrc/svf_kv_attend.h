@@ -6,20 +6,27 @@
 namespace svfk {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // Sixteen 16-bit elements' worth of a matrix product, and the type's constants.
 // kShift: probabilities are scaled by 2^kShift, which cancels against their sum,
 // so that the small ones of a 16-bit float stay above its subnormal numbers.
+// kSlack: powers of two by which a row's scores may pass the maximum that its
+// probabilities are taken against before the row's sums are scaled down to a new one.
 struct BF16M : BF16 {
     static constexpr float kShift = 0.f;
     static constexpr uint16_t kInf = 0x7f80;
+    static constexpr float kSlack = 8.f;
     static __device__ inline f32x4 mfma16(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ inline f32x16 mfma32(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16M : F16 {
     static constexpr float kShift = 14.f;
     static constexpr uint16_t kInf = 0x7c00;
+    static constexpr float kSlack = 1.f;
     static __device__ inline f32x4 mfma16(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ inline f32x16 mfma32(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
