@@ -292,31 +292,151 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     }
 }
 
-// A thread has one slot: its softmax summed over the rows in order.
+// The weights of these sequences' slots: scores once more, now against the rows' final statistics.
+// A workgroup has 256 slots, 64 for each wave, whose keys stay in registers while the rows'
+// queries pass through LDS, 64 at a time; a lane sums its own rows for 32 slots and the lanes
+// are added at the end, so nothing is added atomically.  The exponentials bound it.
+constexpr int kWSlots = 256, kWRows = 64;
+
+__device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
+    if (s.n <= 0 || s.n > p.kv.max_q || !ours(p, s)) return 0;
+    return (s.len - first_slot(p, s) + kWSlots - 1) / kWSlots;
+}
+
 template <class E, int D>
-__global__ __launch_bounds__(256) void k_weight(AttendArgs p) {
+__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(AttendArgs p) {
     using T = typename E::T;
-    const int j = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y, seq = blockIdx.z;
+    using V8 = typename E::V8;
+    constexpr int KS = D / 16, CH = D / 8, PER = kWRows * CH / 256;
+    __shared__ __align__(16) char lds[2][kWRows * D * 2];
+    __shared__ float stat[2][kWRows];
+    __shared__ int64_t scan[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads, head = blockIdx.x % hk;
+    int seq, tile;
+    if (!find_item(p.kv, blockIdx.x / hk, [&](const Seq& s) { return slot_tiles(p, s); }, scan, seq, tile)) return;
     const Seq s = seq_of(p.kv, seq);
-    if (j >= s.len || s.n > p.kv.max_q || !ours(p, s)) return;
-    const int row = pool_row(p.kv, seq, j);
-    if (row < 0) return;
-    const T* k = (const T*)(p.kv.k + head * p.kv.k_head + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row));
-    const int G = p.heads / p.kv.kv_heads;
-    float sum = 0.f;
-    for (int t = s.q0; t < s.q0 + s.n; t++) {
-        const int r = s.len - s.n + (t - s.q0);
-        if ((p.causal && j > r) || (p.window > 0 && j <= r - p.window)) continue;
-        for (int g = 0; g < G; g++) {
-            const int h = head * G + g;
-            const float lse = p.lse[(int64_t)t * p.heads + h] * 1.4426950408889634f;
-            const T* qp = (const T*)(p.q + t * p.q_tok + h * p.q_head);
-            float sc = 0.f;
-            for (int d = 0; d < D; d++) sc += (float)qp[d] * p.scale * (float)k[d];
-            if (lse != -INFINITY) sum += exp2f(sc - lse);
-        }
+    const int r0 = s.len - s.n;
+    const int j0 = first_slot(p, s) + tile * kWSlots, j1 = min(j0 + kWSlots, s.len);
+    // rows that see one of the slots: tokens t0 .. t1 - 1
+    const int t0 = p.causal ? max(0, j0 - r0) : 0;
+    const int t1 = p.window > 0 ? (int)max((int64_t)0, min((int64_t)s.n, (int64_t)j1 - 1 + p.window - r0)) : s.n;
+    const int row0 = t0 * G, row1 = t1 * G;
+
+    // this wave's slots and their keys
+    const int base = j0 + wave * 64;
+    int pool[2];
+    V8 k[2][KS];
+#pragma unroll
+    for (int st = 0; st < 2; st++) {
+        const int j = base + st * 32 + c;
+        pool[st] = j < j1 ? pool_row(p.kv, seq, j) : -1;
+        const uint64_t at = pool[st] < 0 ? (uint64_t)zero_row()
+                                         : (uint64_t)(p.kv.k + head * p.kv.k_head) + row_offset(pool[st], p.kv.shift, p.kv.k_page, p.kv.k_row);
+#pragma unroll
+        for (int x = 0; x < KS; x++) k[st][x] = load_global<V8>(at + x * 32 + h * 16);
     }
-    p.kv.weight[stat_index(p.kv, row, head)] += sum;
+    V8 staged[PER];
+    float staged_stat = 0.f;
+    auto take = [&](int at) {  // rows at .. at + 63 into registers
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int piece = i * 256 + tid, row = at + piece / CH, x = piece % CH;
+            if (row < row1) {
+                const int t = row / G;
+                const char* from = p.q + (s.q0 + t) * p.q_tok + (head * G + row - t * G) * p.q_head + x * 16;
+                if (p.q_wide) {
+                    staged[i] = *(const V8*)from;
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 8; y++) staged[i][y] = *(const T*)(from + y * 2);
+                }
+            } else {
+#pragma unroll
+                for (int y = 0; y < 8; y++) staged[i][y] = (T)0.f;
+            }
+        }
+        if (tid < kWRows) {
+            const int row = at + tid, t = row / G;
+            // a row that saw nothing, or is none, adds exp2(-inf)
+            float x = -INFINITY;
+            if (row < row1) x = p.lse[(int64_t)(s.q0 + t) * p.heads + head * G + row - t * G];
+            staged_stat = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int piece = i * 256 + tid, r = piece / CH, x = piece % CH;
+            *(V8*)(lds[buf] + r * (D * 2) + (x ^ swizzle<D>(r)) * 16) = staged[i];
+        }
+        if (tid < kWRows) stat[buf][tid] = staged_stat;
+    };
+    f32x16 sum[2];
+#pragma unroll
+    for (int st = 0; st < 2; st++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) sum[st][i] = 0.f;
+    if (row0 < row1) {
+        take(row0);
+        put(0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int at = row0; at < row1; at += kWRows, buf ^= 1) {
+        if (at + kWRows < row1) take(at + kWRows);
+        // tokens of the first and the last row
+        const int ta = at / G, tb = min(at + kWRows - 1, row1 - 1) / G;
+        const bool whole = (!p.causal || base + 63 <= r0 + ta) && (p.window == 0 || base > r0 + tb - p.window) && base + 63 < j1;
+        const bool none = (p.causal && base > r0 + tb) || (p.window > 0 && base + 63 <= r0 + ta - p.window) || base >= j1;
+        if (!none) {
+#pragma unroll
+            for (int rt = 0; rt < kWRows / 32; rt++) {
+                f32x16 sc[2];
+#pragma unroll
+                for (int st = 0; st < 2; st++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) sc[st][i] = 0.f;
+#pragma unroll
+                for (int x = 0; x < KS; x++) {
+                    const int r = rt * 32 + c;
+                    const V8 b = *(const V8*)(lds[buf] + r * (D * 2) + ((2 * x + h) ^ swizzle<D>(c)) * 16);
+                    sc[0] = E::mfma32(k[0][x], b, sc[0]);
+                    sc[1] = E::mfma32(k[1][x], b, sc[1]);
+                }
+                const float lse = stat[buf][rt * 32 + c];
+                if (whole) {
+#pragma unroll
+                    for (int st = 0; st < 2; st++)
+#pragma unroll
+                        for (int i = 0; i < 16; i++) sum[st][i] += exp2_fast(fmaf(sc[st][i], p.scale, -lse));
+                } else {
+                    const int r = r0 + (at + rt * 32 + c) / G;
+#pragma unroll
+                    for (int st = 0; st < 2; st++)
+#pragma unroll
+                        for (int i = 0; i < 16; i++) {
+                            const int j = base + st * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
+                            const bool seen = (!p.causal || j <= r) && (p.window == 0 || j > r - p.window);
+                            const float e = exp2_fast(fmaf(sc[st][i], p.scale, -lse));
+                            sum[st][i] += seen ? e : 0.f;
+                        }
+                }
+            }
+        }
+        if (at + kWRows < row1) put(buf ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int st = 0; st < 2; st++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            float x = sum[st][i];
+            for (int d = 16; d; d >>= 1) x += __shfl_xor(x, d);
+            // the lane that looked this slot up has its row
+            const int off = (i >> 2) * 8 + h * 4 + (i & 3);
+            if (c == off && pool[st] >= 0) p.kv.weight[stat_index(p.kv, pool[st], head)] += x;
+        }
 }
 
 template <class E, int D>
@@ -327,9 +447,12 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, hipStream_t s) {
     if (blocks > 0) k_attend_chunk<E, D><<<(unsigned)blocks, 256, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.add_weight && a.kv.width > 0) {
-        const unsigned n = (unsigned)((((int64_t)a.kv.width << a.kv.shift) + 255) / 256);
-        k_weight<E, D><<<dim3(n, a.kv.kv_heads, a.kv.seqs), 256, 0, s>>>(a);
+    if (a.add_weight) {
+        // slot tiles at most: each page is in the batch once
+        const int64_t cap = (int64_t)z.width * z.page_size, most = seqs < z.seqs ? seqs : z.seqs;
+        int64_t tiles = (int64_t)z.num_pages * z.page_size / kWSlots + most;
+        if (tiles > most * ((cap + kWSlots - 1) / kWSlots)) tiles = most * ((cap + kWSlots - 1) / kWSlots);
+        if (tiles > 0) k_weight_chunk<E, D><<<(unsigned)(tiles * z.kv_heads), 256, 0, s>>>(a);
     }
     return hipGetLastError();
 }
