@@ -10,7 +10,7 @@ constexpr int kUnit = 128;
 
 // What the launches of one call share, in the workspace.
 struct RowsPlan {
-    int64_t* first_unit;  // [seqs + 1]: units of a key head before each sequence
+    int64_t* first_unit;  // [seqs + 1]: units of a key head before each sequence; null where no launch follows
     float* part;          // [2 * groups][rows * (D + 4)]: partial results
     float* scores;        // [units][rows][kUnit] (add_weight): scores in log2 terms
     int64_t score_units;  // units that scores has room for
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
     }
     const int64_t all = total * hk;
     const int64_t a = all * blockIdx.x / plan.groups, b = all * (blockIdx.x + 1) / plan.groups;
-    if (blockIdx.x == 0) {
+    if (blockIdx.x == 0 && plan.first_unit) {
         int64_t at = before;
         for (int i = i0; i < i1; i++) {
             plan.first_unit[i] = at;
@@ -518,12 +518,15 @@ int32_t few_rows(const AttendSizes& z) {
     return single <= most ? single : 0;
 }
 
-int64_t rows_workspace(const AttendSizes& z) { return few_rows(z) ? layout(z).bytes : 0; }
+// One launch does where every row has its slots in one unit and no weights are kept.
+bool one_launch(const AttendSizes& z) { return (int64_t)z.width * z.page_size <= kUnit && !z.add_weight; }
+
+int64_t rows_workspace(const AttendSizes& z) { return few_rows(z) && !one_launch(z) ? layout(z).bytes : 0; }
 
 hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {
     const Layout y = layout(z);
     RowsPlan plan;
-    plan.first_unit = (int64_t*)ws;
+    plan.first_unit = one_launch(z) ? nullptr : (int64_t*)ws;
     plan.part = (float*)(ws + y.part);
     plan.scores = a.add_weight ? (float*)(ws + y.scores) : nullptr;
     plan.score_units = y.units;

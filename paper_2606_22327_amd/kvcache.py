@@ -72,61 +72,98 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+# A step is some microseconds on the GPU, so the checks are one expression each
+# where all is well; which of them failed is found out afterwards.
+
 def _pack(cache: Cache, batch: Batch, tokens: int) -> Tuple[bytes, bytes]:
     k, v, weight, position = cache
     offsets, kv_len, table, max_q = batch
-    dtype = DTYPE.get(k.dtype)
-    _need(dtype is not None and v.dtype == k.dtype, "k and v must both be bfloat16 or float16")
+    dtype, kshape, ks, vs, dev = k.dtype, k.shape, k.stride(), v.stride(), k.get_device()
+    tshape, seqs = table.shape, kv_len.shape[0] if kv_len.dim() else -1
+    if not (dtype in DTYPE and v.dtype == dtype and len(kshape) == 4 and v.shape == kshape and ks[3] == 1
+            and vs[3] == 1 and dev >= 0 and v.get_device() == dev and kv_len.get_device() == dev
+            and table.get_device() == dev and kv_len.dtype == torch.int32 and kv_len.dim() == 1
+            and kv_len.is_contiguous() and table.dtype == torch.int32 and len(tshape) == 2 and tshape[0] == seqs
+            and (tshape[1] < 2 or table.stride(1) == 1)):
+        _refuse(cache, batch)
+    pages, heads, size, dim = kshape
+    if weight is not None and not (weight.dtype == torch.float32 and weight.shape == kshape[:3]
+                                   and weight.is_contiguous() and weight.get_device() == dev):
+        _refuse(cache, batch)
+    if position is not None and not (position.dtype == torch.int32 and position.shape == kshape[:3]
+                                     and position.is_contiguous() and position.get_device() == dev):
+        _refuse(cache, batch)
+    if offsets is not None and not (offsets.dtype == torch.int32 and offsets.dim() == 1
+                                    and offsets.shape[0] == seqs + 1 and offsets.is_contiguous()
+                                    and offsets.get_device() == dev):
+        _refuse(cache, batch)
+    width = tshape[1]
+    # a table of one row may have any stride
+    stride = table.stride(0)
+    if seqs < 2 and stride < width:
+        stride = width
+    return (_CACHE.pack(k.data_ptr(), v.data_ptr(), 0 if weight is None else weight.data_ptr(),
+                        0 if position is None else position.data_ptr(), ks[0], ks[1], ks[2],
+                        vs[0], vs[1], vs[2], pages, size, heads, dim, DTYPE[dtype]),
+            _BATCH.pack(0 if offsets is None else offsets.data_ptr(), kv_len.data_ptr(), table.data_ptr(), stride,
+                        seqs, tokens, width, max_q))
+
+
+def _refuse(cache: Cache, batch: Batch):
+    """Says what ``_pack`` did not accept."""
+    k, v, weight, position = cache
+    offsets, kv_len, table, _ = batch
+    _need(k.dtype in DTYPE and v.dtype == k.dtype, "k and v must both be bfloat16 or float16")
     _need(k.dim() == 4 and k.shape == v.shape, "k and v must have the shape [num_pages, kv_heads, page_size, head_dim]")
-    ks, vs = k.stride(), v.stride()
-    _need(ks[3] == 1 and vs[3] == 1, "k and v must be contiguous in head_dim")
-    pages, heads, size, dim = k.shape
-    device = k.device
-    _need(device.type == "cuda", "tensors must be on a GPU")
+    _need(k.stride(3) == 1 and v.stride(3) == 1, "k and v must be contiguous in head_dim")
+    _need(k.is_cuda, "tensors must be on a GPU")
+    dev = k.get_device()
     for t, dt in ((weight, torch.float32), (position, torch.int32)):
-        _need(t is None or (t.dtype == dt and t.shape == (pages, heads, size) and t.is_contiguous()
-                            and t.device == device),
+        _need(t is None or (t.dtype == dt and t.shape == k.shape[:3] and t.is_contiguous() and t.get_device() == dev),
               "weight (float32) and position (int32) must be contiguous [num_pages, kv_heads, page_size]")
-    _need(v.device == device and kv_len.device == device and table.device == device,
+    _need(v.get_device() == dev and kv_len.get_device() == dev and table.get_device() == dev,
           "tensors must be on one GPU")
     _need(kv_len.dtype == torch.int32 and kv_len.dim() == 1 and kv_len.is_contiguous(),
           "kv_len must be contiguous int32 [seqs]")
     seqs = kv_len.shape[0]
     _need(table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == seqs
           and (table.shape[1] < 2 or table.stride(1) == 1), "page_table must be int32 [seqs, pages], rows contiguous")
-    width = table.shape[1]
-    if offsets is not None:
-        _need(offsets.dtype == torch.int32 and offsets.shape == (seqs + 1,) and offsets.is_contiguous()
-              and offsets.device == device, "q_offsets must be contiguous int32 [seqs + 1]")
-    # a table of one row may have any stride
-    stride = max(table.stride(0), width) if seqs < 2 else table.stride(0)
-    return (_CACHE.pack(k.data_ptr(), v.data_ptr(), _ptr(weight), _ptr(position), ks[0], ks[1], ks[2],
-                        vs[0], vs[1], vs[2], pages, size, heads, dim, dtype),
-            _BATCH.pack(_ptr(offsets), kv_len.data_ptr(), table.data_ptr(), stride, seqs, tokens, width, max_q))
+    _need(False, "q_offsets must be contiguous int32 [seqs + 1] on the GPU of the cache")
 
 
-def _rows(x: torch.Tensor, name: str, like: torch.Tensor, tokens: int, dim: int):
-    _need(x.dim() == 3 and x.shape[0] == tokens and x.shape[2] == dim and (dim < 2 or x.stride(2) == 1),
-          f"{name} must be [tokens, heads, head_dim], contiguous in head_dim")
-    _need(x.dtype == like.dtype and x.device == like.device, f"{name} must have the cache's dtype and device")
+def _rows(x: torch.Tensor, name: str, like: torch.Tensor, heads: int = 0):
+    """Strides of token and head of a [tokens, heads, head_dim] tensor of the cache's kind."""
+    shape, st, pool = x.shape, x.stride(), like.shape
+    if not (len(shape) == 3 and len(pool) == 4 and shape[2] == pool[3] and st[2] == 1 and x.dtype == like.dtype
+            and x.get_device() == like.get_device() and (not heads or shape[1] == heads)):
+        _need(len(shape) == 3 and len(pool) == 4 and shape[2] == pool[3] and st[2] == 1,
+              f"{name} must be [tokens, heads, head_dim] of the cache's head_dim, contiguous in it")
+        _need(False, f"{name} must have the cache's dtype, device and kv_heads")
+    return st[0], st[1]
 
 
-def _call(fn: str, device: torch.device, *packed: bytes):
-    lib = svfsim.load()
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index is None or device.index == torch.cuda.current_device():
-        rc = getattr(lib, fn)(*packed, stream)
+def _call(fn, dev: int, *packed: bytes):
+    if dev == torch.cuda.current_device():
+        rc = fn(*packed, _raw_stream(dev))
     else:
-        with torch.cuda.device(device):
-            rc = getattr(lib, fn)(*packed, stream)
-    svfsim._check(rc)
+        with torch.cuda.device(dev):
+            rc = fn(*packed, _raw_stream(dev))
+    if rc != 0:
+        svfsim._check(rc)
 
 
-def _workspace(fn: str, device: torch.device, *packed: bytes) -> Optional[torch.Tensor]:
-    n = getattr(svfsim.load(), fn)(*packed)
+def _raw_stream(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):      # the same handle without a Stream object
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _workspace(n: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     if n < 0:
         svfsim._check(int(n))
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    return like.new_empty(n, dtype=torch.uint8) if n else None
 
 
 def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, rope: Optional[torch.Tensor],
@@ -137,28 +174,31 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     ``q``).  ``rope`` is a table of ``rope_table`` (None: nothing is rotated);
     its width is the rotated part of a head.  Views with any strides of
     tokens and heads are taken, such as the parts of one projection's output."""
-    tokens, dim = q.shape[0] if q.dim() == 3 else -1, cache.k.shape[-1]
-    for x, name in ((q, "q"), (k, "k"), (v, "v")):
-        _rows(x, name, cache.k, tokens, dim)
-    _need(k.shape == v.shape and k.shape[1] == cache.k.shape[1], "k and v must have the cache's kv_heads")
-    _need(positions.dtype == torch.int32 and positions.shape == (tokens,) and positions.is_contiguous()
-          and positions.device == q.device, "positions must be contiguous int32 [tokens]")
-    _need(batch.q_offsets is not None, "q_offsets must not be None")
-    _need(layout in LAYOUT, f"layout must be one of {tuple(LAYOUT)}")
-    rows = rot = 0
+    like, kv_heads = cache.k, cache.k.shape[1]
+    (qt, qh), (kt, kh), (vt, vh) = _rows(q, "q", like), _rows(k, "k", like, kv_heads), _rows(v, "v", like, kv_heads)
+    tokens, heads = q.shape[:2]
+    if not (k.shape[0] == tokens and v.shape[0] == tokens):
+        _need(False, "q, k and v must have as many tokens")
+    if not (positions.dtype == torch.int32 and positions.dim() == 1 and positions.shape[0] == tokens
+            and positions.is_contiguous() and positions.get_device() == q.get_device()):
+        _need(False, "positions must be contiguous int32 [tokens]")
+    if batch.q_offsets is None or layout not in LAYOUT:
+        _need(batch.q_offsets is not None, "q_offsets must not be None")
+        _need(False, f"layout must be one of {tuple(LAYOUT)}")
+    rows = rot = table = 0
     if rope is not None:
-        _need(rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous() and rope.device == q.device,
-              "rope must be contiguous float32 [positions, rot]")
-        rows, rot = rope.shape
+        if not (rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous()
+                and rope.get_device() == q.get_device()):
+            _need(False, "rope must be contiguous float32 [positions, rot]")
+        (rows, rot), table = rope.shape, rope.data_ptr()
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    else:
-        _rows(q_out, "q_out", cache.k, tokens, dim)
-        _need(q_out.shape == q.shape, "q_out must have the shape of q")
-    a = _APPEND.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), positions.data_ptr(), _ptr(rope),
-                     q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-                     q_out.stride(0), q_out.stride(1), q.shape[1], rot, LAYOUT[layout], rows)
-    _call("svf_kv_append", q.device, *_pack(cache, batch, tokens), a)
+        q_out = torch.empty_like(q)
+    elif q_out.shape != q.shape:
+        _need(False, "q_out must have the shape of q")
+    ot, oh = _rows(q_out, "q_out", like)
+    a = _APPEND.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), positions.data_ptr(), table,
+                     qt, qh, kt, kh, vt, vh, ot, oh, heads, rot, LAYOUT[layout], rows)
+    _call(svfsim.load().svf_kv_append, q.get_device(), *_pack(cache, batch, tokens), a)
     return q_out
 
 
@@ -171,27 +211,28 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     slots up to its own.  ``add_weight`` adds every slot's softmax, summed
     over the tokens and the query heads that share its key head, to
     ``cache.weight``.  A token that sees no slot has out = 0, lse = -inf."""
-    tokens, dim = q.shape[0] if q.dim() == 3 else -1, cache.k.shape[-1]
-    _rows(q, "q", cache.k, tokens, dim)
-    _need(batch.q_offsets is not None, "q_offsets must not be None")
-    heads = q.shape[1]
+    qt, qh = _rows(q, "q", cache.k)
+    if batch.q_offsets is None:
+        _need(False, "q_offsets must not be None")
+    tokens, heads, dim = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    else:
-        _rows(out, "out", cache.k, tokens, dim)
-        _need(out.shape == q.shape, "out must have the shape of q")
-    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
-    packed = _pack(cache, batch, tokens)
-    scale = 1.0 / math.sqrt(dim) if scale is None else float(scale)
-
-    def args(ws):
-        return _ATTEND.pack(q.data_ptr(), out.data_ptr(), lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
-                            q.stride(0), q.stride(1), out.stride(0), out.stride(1), scale, heads, bool(causal),
-                            int(window), bool(add_weight))
-
-    a = args(None)
-    ws = _workspace("svf_kv_attend_workspace", q.device, *packed, a)
-    _call("svf_kv_attend", q.device, *packed, a if ws is None else args(ws))
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != q.shape:
+        _need(False, "out must have the shape of q")
+    ot, oh = _rows(out, "out", cache.k)
+    kv, seqs = _pack(cache, batch, tokens)
+    lse = q.new_empty((tokens, heads), dtype=torch.float32)
+    scale = dim ** -0.5 if scale is None else float(scale)
+    fixed = (qt, qh, ot, oh, scale, heads, bool(causal), int(window), bool(add_weight))
+    at = (q.data_ptr(), out.data_ptr(), lse.data_ptr())
+    lib = svfsim.load()
+    a = _ATTEND.pack(*at, 0, 0, *fixed)
+    need = lib.svf_kv_attend_workspace(kv, seqs, a)
+    ws = None
+    if need:
+        ws = _workspace(need, q)
+        a = _ATTEND.pack(*at, ws.data_ptr(), need, *fixed)
+    _call(lib.svf_kv_attend, q.get_device(), kv, seqs, a)
     return out, lse
 
 
@@ -202,19 +243,19 @@ def evict(batch: Batch, cache: Cache, budget: int, recent: int, next_position: t
     before ``next_position`` (int32 [seqs]) and the rest by largest ``cache.weight``
     (ties to the lower slot).  Rows move inside the cache; returns the new lengths."""
     k, kv_len = cache.k, batch.kv_len
-    packed = _pack(cache, batch, 0)
-    _need(cache.weight is not None and cache.position is not None, "evict needs the cache's weight and position")
-    _need(next_position.dtype == torch.int32 and next_position.shape == kv_len.shape
-          and next_position.is_contiguous() and next_position.device == k.device,
-          "next_position must be contiguous int32 [seqs]")
+    kv, seqs = _pack(cache, batch, 0)
+    if cache.weight is None or cache.position is None:
+        _need(False, "evict needs the cache's weight and position")
+    if not (next_position.dtype == torch.int32 and next_position.shape == kv_len.shape
+            and next_position.is_contiguous() and next_position.get_device() == k.get_device()):
+        _need(False, "next_position must be contiguous int32 [seqs]")
     new_len = torch.empty_like(kv_len)
-
-    def args(ws):
-        return _EVICT.pack(next_position.data_ptr(), new_len.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
-                           int(budget), int(recent), int(first))
-
-    ws = _workspace("svf_kv_evict_workspace", k.device, *packed, args(None))
-    _call("svf_kv_evict", k.device, *packed, args(ws))
+    fixed = (int(budget), int(recent), int(first))
+    lib = svfsim.load()
+    need = lib.svf_kv_evict_workspace(kv, seqs, _EVICT.pack(0, 0, 0, 0, *fixed))
+    ws = _workspace(need, k)
+    a = _EVICT.pack(next_position.data_ptr(), new_len.data_ptr(), ws.data_ptr(), need, *fixed)
+    _call(lib.svf_kv_evict, k.get_device(), kv, seqs, a)
     return new_len
 
 
