@@ -84,7 +84,7 @@ typedef struct svf_kv_cache {
  *               used, those behind kv_len never read
  *   max_q       no sequence has more new tokens than this (svf_kv_attend:
  *               the rows of a sequence that has more are NaN)
- * table_width * page_size < 2^31.
+ * table_width * page_size < 2^31 - 2^16.
  */
 typedef struct svf_kv_batch {
     const int32_t *q_offsets;

@@ -44,8 +44,8 @@ int check_sizes(const svf_kv_cache* c, const svf_kv_batch* b) {
     if (b->num_seqs < 0 || b->num_tokens < 0 || b->table_width < 0 || b->max_q < 0)
         return fail(SVF_EINVAL, "num_seqs, num_tokens, table_width and max_q must be >= 0");
     if ((int64_t)b->num_seqs * c->kv_heads > kGridLimit) return fail(SVF_EINVAL, "num_seqs * kv_heads is too large");
-    if ((int64_t)b->table_width * c->page_size >= kLimit31)
-        return fail(SVF_EINVAL, "table_width * page_size must be below 2^31");
+    if ((int64_t)b->table_width * c->page_size >= kLimit31 - 65536)  // a tile past the last slot is still an int
+        return fail(SVF_EINVAL, "table_width * page_size must be below 2^31 - 2^16");
     if (b->table_stride < b->table_width || b->table_stride >= kStrideLimit)
         return fail(SVF_EINVAL, "table_stride must be at least table_width");
     return SVF_OK;

@@ -133,16 +133,15 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         uint64_t k, v;
         bool there;
     };
-    auto lookup = [&](int it) {
-        const int j = lo + it * kTile + lane;
-        const int at = it < tiles && j < hi ? pool_row(p.kv, seq, j) : -1;
+    auto entry = [&](int it) { return table_entry(p.kv, seq, lo + it * kTile + lane); };
+    auto where = [&](int it, int page) {
+        const int j = lo + it * kTile + lane, at = entry_row(p.kv, page, j, j < hi);
         Where w;
         w.there = at >= 0;
-        w.k = w.v = (uint64_t)zero_row();
-        if (w.there) {
-            w.k = (uint64_t)kbase + row_offset(at, p.kv.shift, p.kv.k_page, p.kv.k_row);
-            w.v = (uint64_t)vbase + row_offset(at, p.kv.shift, p.kv.v_page, p.kv.v_row);
-        }
+        const uint64_t k = (uint64_t)kbase + row_offset(at, p.kv.shift, p.kv.k_page, p.kv.k_row);
+        const uint64_t v = (uint64_t)vbase + row_offset(at, p.kv.shift, p.kv.v_page, p.kv.v_row);
+        w.k = w.there ? k : (uint64_t)zero_row();
+        w.v = w.there ? v : (uint64_t)zero_row();
         return w;
     };
     auto from_lane = [](uint64_t x, int l) {
@@ -168,16 +167,17 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.f;
 
-    Where now = lookup(0), next = lookup(1);
+    Where now = where(0, entry(0));
+    int page_next = entry(1);
     if (tiles > 0) fetch(now, 0);
     auto step = [&](int it, int buf) {
         // this tile is there once every wave's loads have arrived, and the other buffer free
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
         __syncthreads();
         const uint64_t there = __ballot(now.there);
-        if (it + 1 < tiles) fetch(next, buf ^ 1);
-        now = next;
-        next = lookup(it + 2);
+        now = where(it + 1, page_next);
+        page_next = entry(it + 2);
+        if (it + 1 < tiles) fetch(now, buf ^ 1);
         const int base = lo + it * kTile;
         if (base > any_last || base + kTile - 1 < any_from) return;
         const char* kb = lds + 2 * buf * BUF;

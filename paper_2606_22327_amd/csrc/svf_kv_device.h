@@ -59,6 +59,18 @@ __device__ inline int pool_row(const KvView& kv, int seq, int j) {
     return there ? (page << kv.shift) | (j & ((1 << kv.shift) - 1)) : -1;
 }
 
+// The same in two steps, so that the load can be on its way while the row before it is used: the
+// table's entry (of the nearest slot that the table has, and any number without a table) ...
+__device__ inline int table_entry(const KvView& kv, int seq, int j) {
+    const int last = kv.width - 1, at = j >> kv.shift;
+    return last < 0 ? -1 : load_global<int32_t>((uint64_t)(kv.table + (int64_t)seq * kv.table_stride + clampi(at, 0, last)));
+}
+// ... and its row, -1 unless the slot is ``in`` range and the page there.
+__device__ inline int entry_row(const KvView& kv, int page, int j, bool in) {
+    const int row = page << kv.shift | (j & ((1 << kv.shift) - 1));
+    return in && (unsigned)page < (unsigned)kv.num_pages ? row : -1;
+}
+
 __device__ inline int64_t row_offset(int row, int shift, int64_t page_stride, int64_t row_stride) {
     return (int64_t)(row >> shift) * page_stride + (int64_t)(row & ((1 << shift) - 1)) * row_stride;
 }

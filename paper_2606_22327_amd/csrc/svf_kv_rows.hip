@@ -78,10 +78,11 @@ __device__ inline void load_v(Tile<E, D>& x, const Where& w) {
     }
 }
 
-// Waves of a SIMD that the registers of a tile leave room for.
+// Waves of a SIMD that the registers of a tile leave room for. (Spilled registers are reloaded in the loop, and a wait
+// for one is a wait for every load on its way.)
 template <int D, int RT>
 constexpr int waves_per_simd() {
-    return D * RT <= 64 ? 4 : D * RT <= 128 ? 3 : D * RT <= 256 && D < 256 ? 2 : 1;
+    return D * RT <= 64 ? 3 : D * RT <= 128 ? 2 : 1;
 }
 
 template <class E, int D, int RT>
@@ -117,7 +118,9 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
         total += scan[w];
     }
     const int64_t all = total * hk;
-    const int64_t a = all * blockIdx.x / plan.groups, b = all * (blockIdx.x + 1) / plan.groups;
+    const int64_t groups = min((int64_t)plan.groups, all);  // of which each has a unit
+    const bool idle = blockIdx.x >= groups;
+    const int64_t a = idle ? 0 : all * blockIdx.x / groups, b = idle ? 0 : all * (blockIdx.x + 1) / groups;
     if (blockIdx.x == 0 && plan.first_unit) {
         int64_t at = before;
         for (int i = i0; i < i1; i++) {
@@ -126,7 +129,7 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
         }
         if (tid == 0) plan.first_unit[p.kv.seqs] = total;
     }
-    if (a == b) return;
+    if (idle) return;
     if (before * hk <= a && a < (before + mine) * hk) {
         int64_t at = before;
         int i = i0;
@@ -184,26 +187,28 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
 #pragma unroll
             for (int j = 0; j < VD; j++) o[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        auto lookup = [&](int u) {
-            const int j = lo + u * kUnit + wave * 32 + (lane & 31);
-            const int row = u < u1 && j < s.len ? pool_row(p.kv, seq, j) : -1;
+        const int slot0 = lo + wave * 32 + (lane & 31);
+        auto entry = [&](int u) { return table_entry(p.kv, seq, slot0 + u * kUnit); };
+        auto where = [&](int u, int page) {
+            const int j = slot0 + u * kUnit, row = entry_row(p.kv, page, j, u < u1 && j < s.len);
             Where w;
             w.there = row >= 0;
-            w.k = w.v = (uint64_t)zero_row();
-            if (w.there) {
-                w.k = (uint64_t)kbase + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row);
-                w.v = (uint64_t)vbase + row_offset(row, p.kv.shift, p.kv.v_page, p.kv.v_row);
-            }
+            const uint64_t k = (uint64_t)kbase + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row);
+            const uint64_t v = (uint64_t)vbase + row_offset(row, p.kv.shift, p.kv.v_page, p.kv.v_row);
+            w.k = w.there ? k : (uint64_t)zero_row();
+            w.v = w.there ? v : (uint64_t)zero_row();
             return w;
         };
+        int page0 = entry(u0), page_next = entry(u0 + 1);
         for (int i = tid; i < 16 * RT * 16; i += 256) (&odd_marks[0][0])[i] = 0;
         __syncthreads();
         Tile<E, D> x;
-        Where now = lookup(u0), next = lookup(u0 + 1);
+        Where now = where(u0, page0);
         load_k(x, now);
         load_v(x, now);
         for (int u = u0; u < u1; u++) {
-            const Where later = lookup(u + 2);
+            const Where next = where(u + 1, page_next);
+            page_next = entry(u + 2);
             const int base = lo + u * kUnit + wave * 32;
             f32x4 sc[RT][2];
 #pragma unroll
@@ -216,6 +221,7 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
                 }
             // which of the tile's slots are there: the same for every row
             const uint32_t there = (uint32_t)__ballot(now.there);
+            const bool all_seen = there == 0xffffffffu && (!p.causal || base + 31 <= r0) && (p.window == 0 || base > s.len - 1 - p.window);
             __builtin_amdgcn_sched_barrier(0);
             load_k(x, next);
             __builtin_amdgcn_sched_barrier(0);
@@ -224,14 +230,16 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
             for (int rt = 0; rt < RT; rt++) {
                 float top = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const int off = (i >> 2) * 16 + g * 4 + (i & 3), j = base + off;
-                    const bool vis = (there >> off & 1) && j <= last[rt] && j >= from[rt];
-                    float v = sc[rt][i >> 2][i & 3] * p.scale;
-                    v = vis ? v : -INFINITY;
-                    sc[rt][i >> 2][i & 3] = v;
-                    top = fmaxf(top, v);
+                for (int i = 0; i < 8; i++) sc[rt][i >> 2][i & 3] *= p.scale;
+                if (!all_seen) {
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const int off = (i >> 2) * 16 + g * 4 + (i & 3), j = base + off;
+                        if (!(there >> off & 1) || j > last[rt] || j < from[rt]) sc[rt][i >> 2][i & 3] = -INFINITY;
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < 8; i++) top = fmaxf(top, sc[rt][i >> 2][i & 3]);
                 if (plan.scores && unit0 + (u - u0) < plan.score_units && rt * 16 + c < rows) {
                     float* to = plan.scores + ((unit0 + (u - u0)) * plan.rows + rt * 16 + c) * kUnit + wave * 32 + g * 4;
                     *(f32x4*)to = sc[rt][0];
@@ -310,7 +318,6 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
             load_v(x, next);
             __builtin_amdgcn_sched_barrier(0);
             now = next;
-            next = later;
         }
 
         // The four waves' parts of a row, then the row: whole, or this workgroup's part of it.
@@ -362,66 +369,90 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
     }
 }
 
-// The parts of a row that was split over workgroups, in the order of its units: one workgroup for a
-// row, eight parts at a time.
+// The sequence that a unit belongs to: the last that begins at or before it. For whole waves.
+__device__ inline int seq_of_unit(const AttendArgs& p, const RowsPlan& plan, int64_t unit) {
+    const int lane = threadIdx.x & 63, hk = p.kv.kv_heads;
+    int lo = 0, n = p.kv.seqs;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, at = lane * step;
+        const bool le = at < n && plan.first_unit[lo + at] * hk <= unit;
+        const int hits = __popcll(__ballot(le)), k = hits > 0 ? hits - 1 : 0;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
+// The parts of the rows that were split over workgroups, in the order of their units.  One workgroup for
+// each boundary between two workgroups' runs: it does its work if the boundary is the first inside a key head's
+// units.  ``parts`` groups of 32 lanes share a row's parts.
 template <class E, int D>
-__global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan) {
+__global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, int parts) {
     constexpr int VD = D / 32;
     const int hk = p.kv.kv_heads, G = p.heads / hk;
-    const int seq = blockIdx.x / hk, head = blockIdx.x - seq * hk, row = blockIdx.y;
+    const int64_t all = plan.first_unit[p.kv.seqs] * hk, groups = min((int64_t)plan.groups, all);
+    const int64_t w = (int64_t)blockIdx.x + 1;
+    if (w >= groups) return;
+    const int64_t cut = all * w / groups;
+    const int seq = seq_of_unit(p, plan, cut);
     const int64_t first = plan.first_unit[seq], units = plan.first_unit[seq + 1] - first;
-    if (units < 2) return;
-    const int64_t all = plan.first_unit[p.kv.seqs] * hk;
+    const int64_t rel = cut - first * hk;
+    const int head = (int)(rel / units);
     const int64_t s0 = first * hk + head * units, s1 = s0 + units;
-    // workgroup w has units [all * w / groups, all * (w + 1) / groups): the one that holds unit x
-    auto holder = [&](int64_t x) {
-        int64_t w = x * plan.groups / all;
-        while (all * (w + 1) / plan.groups <= x) w++;
-        while (w > 0 && all * w / plan.groups > x) w--;
-        return (int)w;
-    };
-    const int w0 = holder(s0), w1 = holder(s1 - 1);
-    if (w0 == w1) return;
+    const int64_t w0 = w - 1;  // the workgroup that has the first unit
+    if (cut == s0 || all * w0 / groups > s0) return;
+    int64_t w1 = (s1 - 1) * groups / all;  // and the one that has the last
+    while (all * (w1 + 1) / groups <= s1 - 1) w1++;
+    while (all * w1 / groups > s1 - 1) w1--;
     const Seq s = seq_of(p.kv, seq);
-    if (row >= s.n * G) return;
-    const int tid = threadIdx.x, sub = tid >> 5, d0 = (tid & 31) * VD;
+    const int tid = threadIdx.x, sub = (tid >> 5) % parts, d0 = (tid & 31) * VD;
     const int64_t stride = (int64_t)plan.rows * (D + 4);
-    auto part_of = [&](int w) { return plan.part + (2 * (int64_t)w + (w == w0 ? 1 : 0)) * stride; };
-    float top = -INFINITY, den = 0.f, acc[VD];
-#pragma unroll
-    for (int j = 0; j < VD; j++) acc[j] = 0.f;
-    for (int w = w0 + sub; w <= w1; w += 8) {
-        // a workgroup whose run of units is empty has no part
-        if (all * w / plan.groups == all * (w + 1) / plan.groups) continue;
-        const float* q = part_of(w);
-        const float pm = q[plan.rows * D + 2 * row], pl = q[plan.rows * D + 2 * row + 1];
-        const float now = fmaxf(top, pm), ref = now == -INFINITY ? 0.f : now;
-        const float keep = exp2_fast(top - ref), f = exp2_fast(pm - ref);
-        den = den * keep + pl * f;
-#pragma unroll
-        for (int j = 0; j < VD; j++) acc[j] = acc[j] * keep + q[row * D + d0 + j] * f;
-        top = now;
-    }
     __shared__ float red[8][D], red_m[8], red_l[8];
+    const int rows = s.n * G, here = 8 / parts;
+    for (int row0 = blockIdx.y * here; row0 < rows; row0 += gridDim.y * here) {
+        const int row = row0 + (tid >> 5) / parts;
+        float top = -INFINITY, den = 0.f, acc[VD];
 #pragma unroll
-    for (int j = 0; j < VD; j++) red[sub][d0 + j] = acc[j];
-    if ((tid & 31) == 0) red_m[sub] = top, red_l[sub] = den;
-    __syncthreads();
-    if (tid >= 32) return;
-    top = -INFINITY;
-    for (int w = 0; w < 8; w++) top = fmaxf(top, red_m[w]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    den = 0.f;
+        for (int j = 0; j < VD; j++) acc[j] = 0.f;
+        if (row < rows) {
+#pragma unroll 4
+            for (int64_t x = w0 + sub; x <= w1; x += parts) {
+                const float* q = plan.part + (2 * x + (x == w0 ? 1 : 0)) * stride;
+                const float pm = q[plan.rows * D + 2 * row], pl = q[plan.rows * D + 2 * row + 1];
+                const float now = fmaxf(top, pm), ref = now == -INFINITY ? 0.f : now;
+                const float keep = exp2_fast(top - ref), f = exp2_fast(pm - ref);
+                den = den * keep + pl * f;
 #pragma unroll
-    for (int j = 0; j < VD; j++) acc[j] = 0.f;
-    for (int w = 0; w < 8; w++) {
-        const float f = exp2_fast(red_m[w] - ref);
-        den += red_l[w] * f;
+                for (int j = 0; j < VD; j++) acc[j] = acc[j] * keep + q[row * D + d0 + j] * f;
+                top = now;
+            }
+        }
+        if (parts > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int j = 0; j < VD; j++) acc[j] += red[w][d0 + j] * f;
+            for (int j = 0; j < VD; j++) red[tid >> 5][d0 + j] = acc[j];
+            if ((tid & 31) == 0) red_m[tid >> 5] = top, red_l[tid >> 5] = den;
+            __syncthreads();
+            if (sub == 0) {
+                const int g0 = tid >> 5;
+                for (int x = 1; x < parts; x++) top = fmaxf(top, red_m[g0 + x]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                den = 0.f;
+#pragma unroll
+                for (int j = 0; j < VD; j++) acc[j] = 0.f;
+                for (int x = 0; x < parts; x++) {
+                    const float f = exp2_fast(red_m[g0 + x] - ref);
+                    den += red_l[g0 + x] * f;
+#pragma unroll
+                    for (int j = 0; j < VD; j++) acc[j] += red[g0 + x][d0 + j] * f;
+                }
+            }
+        }
+        if (sub == 0 && row < rows) {
+            const int t = row / G;
+            write_row<E, VD>(p, s.q0 + t, head * G + row - t * G, d0, acc, den, top);
+        }
     }
-    const int t = row / G;
-    write_row<E, VD>(p, s.q0 + t, head * G + row - t * G, d0, acc, den, top);
 }
 
 // The weights of these sequences' slots from the scores and the rows' final statistics: a wave
@@ -433,15 +464,7 @@ __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan
     for (int64_t half = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); half < 2 * all; half += (int64_t)gridDim.x * 4) {
         const int64_t unit = half >> 1;
         if (unit >= plan.score_units) return;
-        // the last sequence that begins at or before the unit
-        int lo = 0, n = p.kv.seqs;
-        while (n > 1) {
-            const int step = (n + 63) >> 6, at = lane * step;
-            const bool le = at < n && plan.first_unit[lo + at] * hk <= unit;
-            const int hits = __popcll(__ballot(le)), k = hits > 0 ? hits - 1 : 0;
-            lo += k * step;
-            n = min(step, n - k * step);
-        }
+        const int lo = seq_of_unit(p, plan, unit);
         const Seq s = seq_of(p.kv, lo);
         const int64_t units = plan.first_unit[lo + 1] - plan.first_unit[lo], rel = unit - plan.first_unit[lo] * hk;
         if (units <= 0 || s.n > p.kv.max_q) continue;
@@ -470,8 +493,13 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t cap = (int64_t)a.kv.width << a.kv.shift;
-    if (cap > kUnit) {  // else no row has a second unit
-        k_join_rows<E, D><<<dim3(a.kv.seqs * a.kv.kv_heads, plan.rows), 256, 0, s>>>(a, plan);
+    if (cap > kUnit && plan.groups > 1) {  // else no row has a second unit
+        // Few key heads are split over many workgroups: a row's parts over 8 groups of lanes, a workgroup for each
+        // row.  Many are split over two or three: a workgroup for all rows, its groups on as many rows as there are.
+        const bool many = plan.groups >= 8 * (int64_t)a.kv.seqs * a.kv.kv_heads;
+        int parts = 8;
+        while (!many && parts > 1 && 8 / parts < plan.rows) parts >>= 1;
+        k_join_rows<E, D><<<dim3(plan.groups - 1, many ? plan.rows : 1), 256, 0, s>>>(a, plan, parts);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -479,7 +507,11 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
     return hipGetLastError();
 }
 
-constexpr int kGroups = 768;
+// As many workgroups as the GPU holds at a time.
+int32_t most_groups(int32_t dim, int32_t rows) {
+    const int rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    return 256 * (dim * rt <= 64 ? 3 : dim * rt <= 128 ? 2 : 1);
+}
 
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
@@ -492,8 +524,9 @@ Layout layout(const AttendSizes& z) {
     Layout y;
     const int64_t cap = (int64_t)z.width * z.page_size;
     const int64_t most = (int64_t)z.seqs * z.kv_heads * ((cap + kUnit - 1) / kUnit > 0 ? (cap + kUnit - 1) / kUnit : 1);
-    y.groups = (int32_t)(most < kGroups ? most : kGroups);
     y.rows = few_rows(z);
+    y.groups = most_groups(z.dim, y.rows);
+    if (most < y.groups) y.groups = (int32_t)most;
     y.part = round256((int64_t)(z.seqs + 1) * 8);
     y.scores = y.part + round256((int64_t)2 * y.groups * y.rows * (z.dim + 4) * 4);
     // every page once at most: the pool's slots, and a unit that is not full for each sequence

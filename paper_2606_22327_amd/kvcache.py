@@ -87,10 +87,11 @@ def _pack(cache: Cache, batch: Batch, tokens: int) -> Tuple[bytes, bytes]:
             and (tshape[1] < 2 or table.stride(1) == 1)):
         _refuse(cache, batch)
     pages, heads, size, dim = kshape
-    if weight is not None and not (weight.dtype == torch.float32 and weight.shape == kshape[:3]
+    stat = kshape[:3] if weight is not None or position is not None else None
+    if weight is not None and not (weight.dtype == torch.float32 and weight.shape == stat
                                    and weight.is_contiguous() and weight.get_device() == dev):
         _refuse(cache, batch)
-    if position is not None and not (position.dtype == torch.int32 and position.shape == kshape[:3]
+    if position is not None and not (position.dtype == torch.int32 and position.shape == stat
                                      and position.is_contiguous() and position.get_device() == dev):
         _refuse(cache, batch)
     if offsets is not None and not (offsets.dtype == torch.int32 and offsets.dim() == 1
@@ -131,15 +132,24 @@ def _refuse(cache: Cache, batch: Batch):
     _need(False, "q_offsets must be contiguous int32 [seqs + 1] on the GPU of the cache")
 
 
-def _rows(x: torch.Tensor, name: str, like: torch.Tensor, heads: int = 0):
+def _rows(x: torch.Tensor, name: str, dtype: torch.dtype, dev: int, dim: int, heads: int = 0):
     """Strides of token and head of a [tokens, heads, head_dim] tensor of the cache's kind."""
-    shape, st, pool = x.shape, x.stride(), like.shape
-    if not (len(shape) == 3 and len(pool) == 4 and shape[2] == pool[3] and st[2] == 1 and x.dtype == like.dtype
-            and x.get_device() == like.get_device() and (not heads or shape[1] == heads)):
-        _need(len(shape) == 3 and len(pool) == 4 and shape[2] == pool[3] and st[2] == 1,
+    shape, st = x.shape, x.stride()
+    if not (len(shape) == 3 and shape[2] == dim and st[2] == 1 and x.dtype == dtype and x.get_device() == dev
+            and (not heads or shape[1] == heads)):
+        _need(len(shape) == 3 and shape[2] == dim and st[2] == 1,
               f"{name} must be [tokens, heads, head_dim] of the cache's head_dim, contiguous in it")
         _need(False, f"{name} must have the cache's dtype, device and kv_heads")
     return st[0], st[1]
+
+
+def _kind(cache: Cache):
+    """What queries and outputs have to match: type, device and head size, and the key heads."""
+    k = cache.k
+    shape = k.shape
+    if len(shape) != 4:
+        _need(False, "k and v must have the shape [num_pages, kv_heads, page_size, head_dim]")
+    return (k.dtype, k.get_device(), shape[3]), shape[1]
 
 
 def _call(fn, dev: int, *packed: bytes):
@@ -174,13 +184,16 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     ``q``).  ``rope`` is a table of ``rope_table`` (None: nothing is rotated);
     its width is the rotated part of a head.  Views with any strides of
     tokens and heads are taken, such as the parts of one projection's output."""
-    like, kv_heads = cache.k, cache.k.shape[1]
-    (qt, qh), (kt, kh), (vt, vh) = _rows(q, "q", like), _rows(k, "k", like, kv_heads), _rows(v, "v", like, kv_heads)
+    kind, kv_heads = _kind(cache)
+    dev = kind[1]
+    qt, qh = _rows(q, "q", *kind)
+    kt, kh = _rows(k, "k", *kind, kv_heads)
+    vt, vh = _rows(v, "v", *kind, kv_heads)
     tokens, heads = q.shape[:2]
     if not (k.shape[0] == tokens and v.shape[0] == tokens):
         _need(False, "q, k and v must have as many tokens")
     if not (positions.dtype == torch.int32 and positions.dim() == 1 and positions.shape[0] == tokens
-            and positions.is_contiguous() and positions.get_device() == q.get_device()):
+            and positions.is_contiguous() and positions.get_device() == dev):
         _need(False, "positions must be contiguous int32 [tokens]")
     if batch.q_offsets is None or layout not in LAYOUT:
         _need(batch.q_offsets is not None, "q_offsets must not be None")
@@ -188,17 +201,17 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     rows = rot = table = 0
     if rope is not None:
         if not (rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous()
-                and rope.get_device() == q.get_device()):
+                and rope.get_device() == dev):
             _need(False, "rope must be contiguous float32 [positions, rot]")
         (rows, rot), table = rope.shape, rope.data_ptr()
     if q_out is None:
         q_out = torch.empty_like(q)
     elif q_out.shape != q.shape:
         _need(False, "q_out must have the shape of q")
-    ot, oh = _rows(q_out, "q_out", like)
+    ot, oh = _rows(q_out, "q_out", *kind)
     a = _APPEND.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), positions.data_ptr(), table,
                      qt, qh, kt, kh, vt, vh, ot, oh, heads, rot, LAYOUT[layout], rows)
-    _call(svfsim.load().svf_kv_append, q.get_device(), *_pack(cache, batch, tokens), a)
+    _call(svfsim.load().svf_kv_append, dev, *_pack(cache, batch, tokens), a)
     return q_out
 
 
@@ -211,7 +224,8 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     slots up to its own.  ``add_weight`` adds every slot's softmax, summed
     over the tokens and the query heads that share its key head, to
     ``cache.weight``.  A token that sees no slot has out = 0, lse = -inf."""
-    qt, qh = _rows(q, "q", cache.k)
+    kind, _ = _kind(cache)
+    qt, qh = _rows(q, "q", *kind)
     if batch.q_offsets is None:
         _need(False, "q_offsets must not be None")
     tokens, heads, dim = q.shape
@@ -219,7 +233,7 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape:
         _need(False, "out must have the shape of q")
-    ot, oh = _rows(out, "out", cache.k)
+    ot, oh = _rows(out, "out", *kind)
     kv, seqs = _pack(cache, batch, tokens)
     lse = q.new_empty((tokens, heads), dtype=torch.float32)
     scale = dim ** -0.5 if scale is None else float(scale)
@@ -232,7 +246,7 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     if need:
         ws = _workspace(need, q)
         a = _ATTEND.pack(*at, ws.data_ptr(), need, *fixed)
-    _call(lib.svf_kv_attend, q.get_device(), kv, seqs, a)
+    _call(lib.svf_kv_attend, kind[1], kv, seqs, a)
     return out, lse
 
 
