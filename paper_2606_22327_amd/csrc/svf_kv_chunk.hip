@@ -133,7 +133,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         uint64_t k, v;
         bool there;
     };
-    auto entry = [&](int it) { return table_entry(p.kv, seq, lo + it * kTile + lane); };
+    const Table table = table_of(p.kv, seq, zero_row());
+    auto entry = [&](int it) { return table_entry(p.kv, table, lo + it * kTile + lane); };
     auto where = [&](int it, int page) {
         const int j = lo + it * kTile + lane, at = entry_row(p.kv, page, j, j < hi);
         Where w;

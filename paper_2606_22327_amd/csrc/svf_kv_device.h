@@ -60,10 +60,20 @@ __device__ inline int pool_row(const KvView& kv, int seq, int j) {
 }
 
 // The same in two steps, so that the load can be on its way while the row before it is used: the
-// table's entry (of the nearest slot that the table has, and any number without a table) ...
-__device__ inline int table_entry(const KvView& kv, int seq, int j) {
-    const int last = kv.width - 1, at = j >> kv.shift;
-    return last < 0 ? -1 : load_global<int32_t>((uint64_t)(kv.table + (int64_t)seq * kv.table_stride + clampi(at, 0, last)));
+// table's entry, of the nearest slot that the table has (there is no branch in it: at its end the
+// compiler would wait for every load on its way) ...
+struct Table {
+    uint64_t base;
+    int last;
+};
+__device__ inline Table table_of(const KvView& kv, int seq, const void* zero) {
+    Table t;
+    t.last = kv.width > 0 ? kv.width - 1 : 0;
+    t.base = kv.width > 0 ? (uint64_t)(kv.table + (int64_t)seq * kv.table_stride) : (uint64_t)zero;
+    return t;
+}
+__device__ inline int table_entry(const KvView& kv, const Table& t, int j) {
+    return load_global<int32_t>(t.base + (uint64_t)(uint32_t)clampi(j >> kv.shift, 0, t.last) * 4);
 }
 // ... and its row, -1 unless the slot is ``in`` range and the page there.
 __device__ inline int entry_row(const KvView& kv, int page, int j, bool in) {

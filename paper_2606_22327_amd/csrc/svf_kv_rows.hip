@@ -188,7 +188,8 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
             for (int j = 0; j < VD; j++) o[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         const int slot0 = lo + wave * 32 + (lane & 31);
-        auto entry = [&](int u) { return table_entry(p.kv, seq, slot0 + u * kUnit); };
+        const Table table = table_of(p.kv, seq, zero_row());
+        auto entry = [&](int u) { return table_entry(p.kv, table, slot0 + u * kUnit); };
         auto where = [&](int u, int page) {
             const int j = slot0 + u * kUnit, row = entry_row(p.kv, page, j, u < u1 && j < s.len);
             Where w;
@@ -204,8 +205,12 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
         __syncthreads();
         Tile<E, D> x;
         Where now = where(u0, page0);
+        // In the loop's order: where the two meet, the compiler waits for the more careful of them.
+        __builtin_amdgcn_sched_barrier(0);
         load_k(x, now);
+        __builtin_amdgcn_sched_barrier(0);
         load_v(x, now);
+        __builtin_amdgcn_sched_barrier(0);
         for (int u = u0; u < u1; u++) {
             const Where next = where(u + 1, page_next);
             page_next = entry(u + 2);
