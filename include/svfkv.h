@@ -54,8 +54,8 @@ enum {
 /*
  * One layer's cache.  Element (page, head, row, d) of k is at
  * k[page * k_page_stride + head * k_head_stride + row * k_row_stride + d]; v
- * the same.  Strides are in elements, multiples of 8; k and v are aligned to
- * 16 bytes.
+ * the same.  Strides are in elements, multiples of 8, those of pages and rows
+ * below 2^31; k and v are aligned to 16 bytes.
  *   page_size  a power of two, 1 .. 65536;  num_pages * page_size < 2^31
  *   head_dim   64, 128 or 256
  *   weight     float [num_pages][kv_heads][page_size]: each slot's summed

@@ -54,10 +54,11 @@ int check_sizes(const svf_kv_cache* c, const svf_kv_batch* b) {
 int check_buffers(const svf_kv_cache* c, const svf_kv_batch* b) {
     if (c->num_pages > 0 && (!c->k || !c->v)) return fail(SVF_EINVAL, "k and v must not be NULL");
     if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(SVF_EINVAL, "k and v must be aligned to 16 bytes");
-    const int64_t strides[6] = {c->k_page_stride, c->k_head_stride, c->k_row_stride,
-                                c->v_page_stride, c->v_head_stride, c->v_row_stride};
-    for (int64_t s : strides)
-        if (!stride_ok(s) || s % 8) return fail(SVF_EINVAL, "strides of k and v must be multiples of 8, 0 .. 2^40");
+    const int64_t strides[6] = {c->k_head_stride, c->v_head_stride, c->k_page_stride,
+                                c->k_row_stride,  c->v_page_stride, c->v_row_stride};
+    for (int i = 0; i < 6; i++)
+        if (!stride_ok(strides[i]) || strides[i] % 8 || (i >= 2 && strides[i] >= kLimit31))
+            return fail(SVF_EINVAL, "strides of k and v must be multiples of 8, from 0, of pages and rows below 2^31");
     if (b->num_seqs > 0 && (!b->kv_len || (b->table_width > 0 && !b->page_table)))
         return fail(SVF_EINVAL, "kv_len and page_table must not be NULL");
     return SVF_OK;

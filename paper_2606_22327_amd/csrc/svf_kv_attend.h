@@ -29,6 +29,13 @@ struct F16M : F16 {
     static __device__ inline f32x16 mfma32(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
+// The largest of three (the compiler's own first quiets every operand).
+__device__ inline float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Two elements in a word: whether one of them is no finite number; the word with zeros in the place of such; and

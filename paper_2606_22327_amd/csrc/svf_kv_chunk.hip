@@ -75,7 +75,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* Lds4;
     constexpr int KS = D / 16, DT = D / 32, CH = D / 8, BUF = kTile * D * 2;
-    __shared__ __align__(16) char lds[4 * BUF];  // keys and values, twice
+    // keys and values twice, each an object of its own: reads of one do not wait for loads into another
+    __shared__ __align__(16) char k0[BUF], v0[BUF], k1[BUF], v1[BUF];
     __shared__ uint32_t odd_marks[kRows][D / 16];
     __shared__ int64_t scan[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
@@ -103,6 +104,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     const int all_last = p.causal ? r0 + wt0 : s.len - 1, any_last = p.causal ? r0 + wt1 : s.len - 1;
     const int all_from = p.window > 0 ? r0 + wt1 - p.window + 1 : 0;
     const int any_from = p.window > 0 ? r0 + wt0 - p.window + 1 : 0;
+    const int block_last = p.causal ? r0 + first_row / G : s.len - 1;
+    const int block_from = p.window > 0 ? r0 + last_row / G - p.window + 1 : 0;
 
     // Scores are compared before they are scaled: the queries take the scale's sign.
     const float sign = p.scale < 0.f ? -1.f : 1.f, scale = p.scale == 0.f ? 1.f : fabsf(p.scale);
@@ -126,40 +129,76 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     for (int i = tid; i < kRows * (D / 16); i += 256) (&odd_marks[0][0])[i] = 0;
     __syncthreads();
 
-    const char* kbase = p.kv.k + head * p.kv.k_head;
-    const char* vbase = p.kv.v + head * p.kv.v_head;
-    // a lane has the addresses of slot ``lane`` of a tile
-    struct Where {
-        uint64_t k, v;
-        bool there;
-    };
+    const uint64_t kbase = (uint64_t)(p.kv.k + head * p.kv.k_head), vbase = (uint64_t)(p.kv.v + head * p.kv.v_head);
     const Table table = table_of(p.kv, seq, zero_row());
-    auto entry = [&](int it) { return table_entry(p.kv, table, lo + it * kTile + lane); };
-    auto where = [&](int it, int page) {
-        const int j = lo + it * kTile + lane, at = entry_row(p.kv, page, j, j < hi);
-        Where w;
-        w.there = at >= 0;
-        const uint64_t k = (uint64_t)kbase + row_offset(at, p.kv.shift, p.kv.k_page, p.kv.k_row);
-        const uint64_t v = (uint64_t)vbase + row_offset(at, p.kv.shift, p.kv.v_page, p.kv.v_row);
-        w.k = w.there ? k : (uint64_t)zero_row();
-        w.v = w.there ? v : (uint64_t)zero_row();
-        return w;
-    };
-    auto from_lane = [](uint64_t x, int l) {
-        const uint32_t a = __shfl((int)(uint32_t)x, l), b = __shfl((int)(x >> 32), l);
-        return (uint64_t)b << 32 | a;
+    const int mask = (1 << p.kv.shift) - 1;
+    // A wave fetches sixteen of a tile's slots, 64 / CH of them with an instruction; a lane's
+    // slot of instruction i is own + i * 64 / CH.
+    constexpr int NI = CH / 4, PER = 64 / CH;
+    const int own = wave * 16 + lane / CH;
+    int page[NI], page_all;  // of the lane's slots, and of slot ``lane``
+    auto look = [&](int it) {
+        page_all = table_entry(p.kv, table, lo + it * kTile + lane);
+#pragma unroll
+        for (int i = 0; i < NI; i++) page[i] = table_entry(p.kv, table, lo + it * kTile + own + i * PER);
     };
     typedef const __attribute__((address_space(1))) void* Global;
     typedef __attribute__((address_space(3))) void* Lds;
-    auto fetch = [&](const Where& w, int buf) {
+    uint64_t there, there_next;
+    auto fetch = [&](int it, char* kto, char* vto) {
+        const int j0 = lo + it * kTile;
+        there_next = __ballot((unsigned)page_all < (unsigned)p.kv.num_pages && j0 + lane < hi);
 #pragma unroll
-        for (int i = 0; i < CH / 4; i++) {
-            const int piece = (wave * (CH / 4) + i) * 64, at = piece + lane;
-            const int r = at / CH, x = ((at % CH) ^ swizzle<D>(r)) * 16;
-            __builtin_amdgcn_global_load_lds((Global)(from_lane(w.k, r) + x), (Lds)(lds + (2 * buf) * BUF + piece * 16), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((Global)(from_lane(w.v, r) + x), (Lds)(lds + (2 * buf + 1) * BUF + piece * 16), 16, 0, 0);
+        for (int i = 0; i < NI; i++) {
+            const int r = own + i * PER, j = j0 + r, x = ((lane % CH) ^ swizzle<D>(r)) * 16;
+            const bool in = (unsigned)page[i] < (unsigned)p.kv.num_pages && j < hi;
+            const uint64_t k = in ? row_address(kbase, page[i], j & mask, p.kv.k_page, p.kv.k_row) : (uint64_t)zero_row();
+            const uint64_t v = in ? row_address(vbase, page[i], j & mask, p.kv.v_page, p.kv.v_row) : (uint64_t)zero_row();
+            const int to = (wave * NI + i) * 1024;
+            __builtin_amdgcn_global_load_lds((Global)(k + x), (Lds)(kto + to), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((Global)(v + x), (Lds)(vto + to), 16, 0, 0);
         }
     };
+    // Where the tile's rows do not all see the same slots, a value that is no finite number would reach those
+    // that do not see it (0 times infinity): it counts as 0, and the rows that see it get it
+    // from their marks.  Each wave looks through the values of sixteen slots.
+    auto clean = [&](char* vb, int base) {
+        u16x2 size = {0, 0};
+        uint32_t* words = (uint32_t*)(vb + wave * 16 * D * 2) + lane;
+        for (int x = 0; x < 8 * D; x += 64) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, words[x] & 0x7fff7fffu));
+        if (!__any(max(size.x, size.y) >= E::kInf)) return;
+        for (int x = 0; x < 8 * D; x += 64) {
+            const uint32_t pair = words[x];
+            if (!odd_pair<E>(pair)) continue;
+            const int r = wave * 16 + (x + lane) / (D / 2), at = (x + lane) % (D / 2);
+            const int w = ((at >> 2) ^ swizzle<D>(r)) * 4 + (at & 3);  // the dimensions 2 w and 2 w + 1
+            const uint32_t marks = odd_marks_of<E>(pair) << 4 * (w & 7);
+            for (int y = 0; y <= last_row - first_row; y++) {
+                const int t = r0 + (first_row + y) / G;
+                if ((!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window)) atomicOr(&odd_marks[y][w >> 3], marks);
+            }
+            words[x] = finite_pair<E>(pair);
+        }
+    };
+
+    // Where a lane reads in a tile: keys, 16 bytes of row c, and values, eight bytes of the rows that it gives for
+    // the transposed read (16 lanes give four slots' rows, four dimensions each, and get four
+    // slots of one dimension).  Kept in registers; what is constant goes into the reads' offsets.
+    constexpr int KA = KS < 8 ? KS : 8, VA = DT < 4 ? DT : 4;
+    int ka[KA], va[VA][2];
+#pragma unroll
+    for (int k = 0; k < KA; k++) {
+        ka[k] = c * (D * 2) + ((2 * k + h) ^ swizzle<D>(c)) * 16;
+        asm volatile("" : "+v"(ka[k]));
+    }
+#pragma unroll
+    for (int d = 0; d < VA; d++)
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int r = i * 8 + h * 4 + (lane >> 2 & 3), dim = d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+            va[d][i] = r * (D * 2) + ((dim >> 3) ^ swizzle<D>(r)) * 16 + (dim & 7) * 2;
+            asm volatile("" : "+v"(va[d][i]));
+        }
 
     float m = -INFINITY, l = 0.f;
     f32x16 o[DT];
@@ -168,21 +207,26 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.f;
 
-    Where now = where(0, entry(0));
-    int page_next = entry(1);
-    if (tiles > 0) fetch(now, 0);
-    auto step = [&](int it, int buf) {
-        // this tile is there once every wave's loads have arrived, and the other buffer free
+    if (tiles > 0) {
+        look(0);
+        fetch(0, k0, v0);
+        look(1);
+    }
+    auto step = [&](int it, char* kb, char* vb, char* knext, char* vnext) {
+        // this tile is there once every wave's loads have arrived, and the other buffers free
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
         __syncthreads();
-        const uint64_t there = __ballot(now.there);
-        now = where(it + 1, page_next);
-        page_next = entry(it + 2);
-        if (it + 1 < tiles) fetch(now, buf ^ 1);
+        there = there_next;
+        if (it + 1 < tiles) {
+            fetch(it + 1, knext, vnext);
+            look(it + 2);
+        }
         const int base = lo + it * kTile;
+        if (!(base + kTile - 1 <= block_last && base >= block_from && ~there == 0)) {
+            clean(vb, base);
+            __syncthreads();
+        }
         if (base > any_last || base + kTile - 1 < any_from) return;
-        const char* kb = lds + 2 * buf * BUF;
-        const char* vb = kb + BUF;
         f32x16 sc[2];
 #pragma unroll
         for (int st = 0; st < 2; st++) {
@@ -190,13 +234,11 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             for (int i = 0; i < 16; i++) sc[st][i] = 0.f;
 #pragma unroll
             for (int k = 0; k < KS; k++) {
-                const int r = st * 32 + c;
-                const V8 a = *(const V8*)(kb + r * (D * 2) + ((2 * k + h) ^ swizzle<D>(c)) * 16);
+                const V8 a = *(const V8*)(kb + ka[k % KA] + st * 32 * (D * 2) + k / KA * 256);
                 sc[st] = E::mfma32(a, q[k], sc[st]);
             }
         }
-        const bool whole = base + kTile - 1 <= all_last && base >= all_from && ~there == 0;
-        if (!whole) {
+        if (!(base + kTile - 1 <= all_last && base >= all_from && ~there == 0)) {
 #pragma unroll
             for (int st = 0; st < 2; st++)
 #pragma unroll
@@ -205,9 +247,13 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
                     if (!(there >> off & 1) || j > last || j < from) sc[st][i] = -INFINITY;
                 }
         }
-        float top = sc[0][0];
+        float top = max3(sc[0][0], sc[0][1], sc[0][2]);
 #pragma unroll
-        for (int i = 0; i < 16; i++) top = fmaxf(top, fmaxf(sc[0][i], sc[1][i]));
+        for (int i = 3; i < 15; i += 2) top = max3(top, sc[0][i], sc[0][i + 1]);
+        top = max3(top, sc[0][15], sc[1][0]);
+#pragma unroll
+        for (int i = 1; i < 15; i += 2) top = max3(top, sc[1][i], sc[1][i + 1]);
+        top = fmaxf(top, sc[1][15]);
         top = fmaxf(top, __shfl_xor(top, 32)) * scale;
         if (__any(top > m + E::kSlack)) {
             const float peak = fmaxf(m, top);
@@ -229,49 +275,21 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
                 l += e;
                 pr[st * 2 + (i >> 3)][i & 7] = (T)e;
             }
-        // Where rows do not see the same slots, a value that is no finite number would reach those that
-        // do not see it (0 times infinity): it counts as 0, and the rows that see it get it from its marks.
-        bool odd = false;
-        if (!whole) {
-            u16x2 size = {0, 0};
-            for (int r = lane & 1; r < kTile; r += 2)
-                for (int x = lane >> 1; x < D / 2; x += 32)
-                    size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, *(const uint32_t*)(vb + r * (D * 2) + x * 4) & 0x7fff7fffu));
-            odd = __any(max(size.x, size.y) >= E::kInf);
-            if (odd) {
-                for (int r = lane & 1; r < kTile; r += 2)
-                    for (int x = lane >> 1; x < D / 2; x += 32) {
-                        const uint32_t pair = *(const uint32_t*)(vb + r * (D * 2) + x * 4);
-                        if (!odd_pair<E>(pair)) continue;
-                        const int w = ((x >> 2) ^ swizzle<D>(r)) * 4 + (x & 3);  // the dimensions 2 w and 2 w + 1
-                        const uint32_t marks = odd_marks_of<E>(pair) << 4 * (w & 7);
-                        for (int y = 0; y < 32 && wrow0 + y < rows; y++) {
-                            const int at = r0 + (wrow0 + y) / G;
-                            if ((!p.causal || base + r <= at) && (p.window == 0 || base + r > at - p.window))
-                                atomicOr(&odd_marks[wave * 32 + y][w >> 3], marks);
-                        }
-                    }
-            }
-        }
 #pragma unroll
         for (int k = 0; k < 4; k++)
 #pragma unroll
             for (int d = 0; d < DT; d++) {
                 s16x4 part[2];
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    // 16 lanes give four slots' rows, four dimensions each, and get four slots of one dimension
-                    const int r = k * 16 + i * 8 + h * 4 + (lane >> 2 & 3), dim = d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
-                    part[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(vb + r * (D * 2) + ((dim >> 3) ^ swizzle<D>(r)) * 16 + (dim & 7) * 2));
-                }
-                uint2 a = __builtin_bit_cast(uint2, part[0]), b = __builtin_bit_cast(uint2, part[1]);
-                if (odd) a = make_uint2(finite_pair<E>(a.x), finite_pair<E>(a.y)), b = make_uint2(finite_pair<E>(b.x), finite_pair<E>(b.y));
+                for (int i = 0; i < 2; i++)
+                    part[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(vb + va[d % VA][i] + k * 16 * (D * 2) + d / VA * 256));
+                const uint2 a = __builtin_bit_cast(uint2, part[0]), b = __builtin_bit_cast(uint2, part[1]);
                 o[d] = E::mfma32(__builtin_bit_cast(V8, make_uint4(a.x, a.y, b.x, b.y)), pr[k], o[d]);
             }
     };
     for (int it = 0; it < tiles; it += 2) {
-        step(it, 0);
-        if (it + 1 < tiles) step(it + 1, 1);
+        step(it, k0, v0, k1, v1);
+        if (it + 1 < tiles) step(it + 1, k1, v1, k0, v0);
     }
 
     if (row < rows) {

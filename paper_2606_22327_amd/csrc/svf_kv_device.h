@@ -81,6 +81,11 @@ __device__ inline int entry_row(const KvView& kv, int page, int j, bool in) {
     return in && (unsigned)page < (unsigned)kv.num_pages ? row : -1;
 }
 
+// Where a pool's rows lie: the address of a row of a page (strides are below 2^32 bytes).
+__device__ inline uint64_t row_address(uint64_t base, int page, int row, int64_t page_stride, int64_t row_stride) {
+    return base + (uint64_t)(uint32_t)page * (uint32_t)page_stride + (uint64_t)(uint32_t)row * (uint32_t)row_stride;
+}
+
 __device__ inline int64_t row_offset(int row, int shift, int64_t page_stride, int64_t row_stride) {
     return (int64_t)(row >> shift) * page_stride + (int64_t)(row & ((1 << shift) - 1)) * row_stride;
 }
