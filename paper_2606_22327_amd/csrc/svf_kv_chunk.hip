@@ -55,6 +55,13 @@ __device__ inline bool find_item(const KvView& kv, int64_t at, Count count, int6
     return seq >= 0;
 }
 
+// The bits from .. last, both included, of those that a word has.
+__device__ inline uint64_t bits_between(int from, int last) {
+    if (last < 0 || from > 63 || from > last) return 0;
+    const uint64_t below = last >= 63 ? ~0ull : (2ull << last) - 1;
+    return from <= 0 ? below : below & (~0ull << from);
+}
+
 // Rows of the tile in LDS lie one behind the other, their 16-byte pieces permuted so that the lanes of
 // a read meet every bank alike: sixteen rows' same piece (keys), and eight rows' four neighbouring
 // pieces (values, read transposed).
@@ -229,23 +236,32 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         if (base > any_last || base + kTile - 1 < any_from) return;
         f32x16 sc[2];
 #pragma unroll
-        for (int st = 0; st < 2; st++) {
+        for (int st = 0; st < 2; st++)
 #pragma unroll
             for (int i = 0; i < 16; i++) sc[st][i] = 0.f;
 #pragma unroll
-            for (int k = 0; k < KS; k++) {
-                const V8 a = *(const V8*)(kb + ka[k % KA] + st * 32 * (D * 2) + k / KA * 256);
-                sc[st] = E::mfma32(a, q[k], sc[st]);
-            }
-        }
-        if (!(base + kTile - 1 <= all_last && base >= all_from && ~there == 0)) {
+        for (int k = 0; k < KS; k++)
 #pragma unroll
             for (int st = 0; st < 2; st++)
+                sc[st] = E::mfma32(*(const V8*)(kb + ka[k % KA] + st * 32 * (D * 2) + k / KA * 256), q[k], sc[st]);
+        // reads two products ahead of their use
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    const int off = st * 32 + (i >> 2) * 8 + h * 4 + (i & 3), j = base + off;
-                    if (!(there >> off & 1) || j > last || j < from) sc[st][i] = -INFINITY;
-                }
+        for (int i = 0; i < 2 * KS - 4; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        if (!(base + kTile - 1 <= all_last && base >= all_from && ~there == 0)) {
+            // bit (i / 4) * 8 + i % 4 of a word: whether the lane's row sees the slot of score i
+            const uint64_t seen = (there & bits_between(from - base, last - base)) >> (h * 4);
+#pragma unroll
+            for (int st = 0; st < 2; st++) {
+                const uint32_t word = (uint32_t)(seen >> (st * 32));
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (!(word >> ((i >> 2) * 8 + (i & 3)) & 1)) sc[st][i] = -INFINITY;
+            }
         }
         float top = max3(sc[0][0], sc[0][1], sc[0][2]);
 #pragma unroll
@@ -286,6 +302,13 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
                 const uint2 a = __builtin_bit_cast(uint2, part[0]), b = __builtin_bit_cast(uint2, part[1]);
                 o[d] = E::mfma32(__builtin_bit_cast(V8, make_uint4(a.x, a.y, b.x, b.y)), pr[k], o[d]);
             }
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
+#pragma unroll
+        for (int i = 0; i < 4 * DT - 3; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 3, 1);
     };
     for (int it = 0; it < tiles; it += 2) {
         step(it, k0, v0, k1, v1);
