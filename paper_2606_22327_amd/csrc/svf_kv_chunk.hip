@@ -75,7 +75,10 @@ __device__ inline int swizzle(int row) {
 // scores of a lane are, in order, the second product's operand for the slots 16 s + 4 h + {0..3, 8..11}
 // (h the half), and the values of those slots come transposed out of LDS, four slots a read.
 // Keys and values go from memory straight to LDS, the next tile's while this one is worked on.
-template <class E, int D>
+// WIDE: pages of 16 slots or more, so that the sixteen slots that a wave fetches lie in one page: their address is the same for
+// the whole wave but for an offset that stays the same all along (a tile costs a wave 8 loads and some scalar
+// instructions, and 100 vector instructions otherwise).
+template <class E, int D, bool WIDE>
 __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(AttendArgs p) {
     using T = typename E::T;
     using V8 = typename E::V8;
@@ -86,7 +89,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     __shared__ __align__(16) char k0[BUF], v0[BUF], k1[BUF], v1[BUF];
     __shared__ uint32_t odd_marks[kRows][D / 16];
     __shared__ int64_t scan[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads;
     const int head = blockIdx.x % hk;
     int seq, tile;
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     tile = row_tiles(p, s) - 1 - tile;  // the longest first
     const int rows = s.n * G, r0 = s.len - s.n;
     const int first_row = tile * kRows, last_row = min(first_row + kRows, rows) - 1;
-    const int lo = p.window > 0 ? max(0, r0 + first_row / G - p.window + 1) : 0;
+    const int lo = p.window > 0 ? max(0, r0 + first_row / G - p.window + 1) & ~15 : 0;
     const int hi = p.causal ? min(s.len, r0 + last_row / G + 1) : s.len;
     const int tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
 
@@ -143,27 +147,56 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     // slot of instruction i is own + i * 64 / CH.
     constexpr int NI = CH / 4, PER = 64 / CH;
     const int own = wave * 16 + lane / CH;
-    int page[NI], page_all;  // of the lane's slots, and of slot ``lane``
+    int page[NI], page_all;  // of the lane's slots (not WIDE), and of slot ``lane``
+    uint32_t koff[NI], voff[NI];  // WIDE: of the lane's piece from the first of the sixteen slots
+#pragma unroll
+    for (int i = 0; i < NI; i++) {
+        const int r = lane / CH + i * PER, x = ((lane % CH) ^ swizzle<D>(r)) * 16;
+        koff[i] = (uint32_t)r * (uint32_t)p.kv.k_row + x;
+        voff[i] = (uint32_t)r * (uint32_t)p.kv.v_row + x;
+    }
     auto look = [&](int it) {
         page_all = table_entry(p.kv, table, lo + it * kTile + lane);
+        if constexpr (!WIDE) {
 #pragma unroll
-        for (int i = 0; i < NI; i++) page[i] = table_entry(p.kv, table, lo + it * kTile + own + i * PER);
+            for (int i = 0; i < NI; i++) page[i] = table_entry(p.kv, table, lo + it * kTile + own + i * PER);
+        }
     };
-    typedef const __attribute__((address_space(1))) void* Global;
+    typedef const __attribute__((address_space(1))) char* Global;
     typedef __attribute__((address_space(3))) void* Lds;
+    auto load = [](Global from, char* to) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (Lds)to, 16, 0, 0);
+    };
     uint64_t there, there_next;
     auto fetch = [&](int it, char* kto, char* vto) {
         const int j0 = lo + it * kTile;
         there_next = __ballot((unsigned)page_all < (unsigned)p.kv.num_pages && j0 + lane < hi);
+        kto += wave * NI * 1024;
+        vto += wave * NI * 1024;
+        if constexpr (WIDE) {
+            // Slots behind the last one are read with the others: they are there, and their values count as 0.
+            if (there_next >> (wave * 16) & 1) {
+                const int at = __builtin_amdgcn_readlane(page_all, wave * 16), row = (j0 + wave * 16) & mask;
+                const Global k = (Global)row_address(kbase, at, row, p.kv.k_page, p.kv.k_row);
+                const Global v = (Global)row_address(vbase, at, row, p.kv.v_page, p.kv.v_row);
 #pragma unroll
-        for (int i = 0; i < NI; i++) {
-            const int r = own + i * PER, j = j0 + r, x = ((lane % CH) ^ swizzle<D>(r)) * 16;
-            const bool in = (unsigned)page[i] < (unsigned)p.kv.num_pages && j < hi;
-            const uint64_t k = in ? row_address(kbase, page[i], j & mask, p.kv.k_page, p.kv.k_row) : (uint64_t)zero_row();
-            const uint64_t v = in ? row_address(vbase, page[i], j & mask, p.kv.v_page, p.kv.v_row) : (uint64_t)zero_row();
-            const int to = (wave * NI + i) * 1024;
-            __builtin_amdgcn_global_load_lds((Global)(k + x), (Lds)(kto + to), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((Global)(v + x), (Lds)(vto + to), 16, 0, 0);
+                for (int i = 0; i < NI; i++) load(k + koff[i], kto + i * 1024), load(v + voff[i], vto + i * 1024);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NI; i++) {
+                    const Global zero = (Global)(uint64_t)zero_row() + lane % CH * 16;
+                    load(zero, kto + i * 1024), load(zero, vto + i * 1024);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NI; i++) {
+                const int r = own + i * PER, j = j0 + r, x = ((lane % CH) ^ swizzle<D>(r)) * 16;
+                const bool in = (unsigned)page[i] < (unsigned)p.kv.num_pages && j < hi;
+                const uint64_t k = in ? row_address(kbase, page[i], j & mask, p.kv.k_page, p.kv.k_row) : (uint64_t)zero_row();
+                const uint64_t v = in ? row_address(vbase, page[i], j & mask, p.kv.v_page, p.kv.v_row) : (uint64_t)zero_row();
+                load((Global)(k + x), kto + i * 1024), load((Global)(v + x), vto + i * 1024);
+            }
         }
     };
     // Where the tile's rows do not all see the same slots, a value that is no finite number would reach those
@@ -182,7 +215,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             const uint32_t marks = odd_marks_of<E>(pair) << 4 * (w & 7);
             for (int y = 0; y <= last_row - first_row; y++) {
                 const int t = r0 + (first_row + y) / G;
-                if ((!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window)) atomicOr(&odd_marks[y][w >> 3], marks);
+                if ((there >> r & 1) && (!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window))
+                    atomicOr(&odd_marks[y][w >> 3], marks);
             }
             words[x] = finite_pair<E>(pair);
         }
@@ -486,7 +520,14 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, hipStream_t s) {
     // Row tiles at most: the full ones of all tokens, and one more for each sequence that is long enough to come here.
     const int64_t rows = (int64_t)z.tokens * (z.heads / z.kv_heads), seqs = rows / (a.few + 1);
     const int64_t blocks = (rows / kRows + (seqs < z.seqs ? seqs : z.seqs)) * z.kv_heads;
-    if (blocks > 0) k_attend_chunk<E, D><<<(unsigned)blocks, 256, 0, s>>>(a);
+    if (blocks > 0) {
+        // Offsets of sixteen rows are 32 bits.
+        const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
+        if (z.page_size >= 16 && far < (int64_t(1) << 31))
+            k_attend_chunk<E, D, true><<<(unsigned)blocks, 256, 0, s>>>(a);
+        else
+            k_attend_chunk<E, D, false><<<(unsigned)blocks, 256, 0, s>>>(a);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.add_weight) {
