@@ -412,25 +412,34 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
 #pragma unroll
         for (int x = 0; x < KS; x++) k[st][x] = load_global<V8>(at + x * 32 + h * 16);
     }
+    // The rows whose pieces this thread brings to LDS, as token and query head: a tile on is ``step_t`` tokens
+    // and ``step_g`` heads on.
+    int qt[PER], qg[PER];
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+        const int row = row0 + (i * 256 + tid) / CH;
+        qt[i] = row / G;
+        qg[i] = row - qt[i] * G;
+    }
+    const int step_t = kWRows / G, step_g = kWRows - step_t * G;
     V8 staged[PER];
     float staged_stat = 0.f;
     auto take = [&](int at) {  // rows at .. at + 63 into registers
 #pragma unroll
         for (int i = 0; i < PER; i++) {
-            const int piece = i * 256 + tid, row = at + piece / CH, x = piece % CH;
-            if (row < row1) {
-                const int t = row / G;
-                const char* from = p.q + (s.q0 + t) * p.q_tok + (head * G + row - t * G) * p.q_head + x * 16;
-                if (p.q_wide) {
-                    staged[i] = *(const V8*)from;
-                } else {
-#pragma unroll
-                    for (int y = 0; y < 8; y++) staged[i][y] = *(const T*)(from + y * 2);
-                }
+            const int piece = i * 256 + tid, x = piece % CH;
+            // a row behind the last has the last one's query: its statistic takes it out
+            const int t = min(qt[i], t1 - 1);
+            const char* from = p.q + (s.q0 + t) * p.q_tok + (head * G + qg[i]) * p.q_head + x * 16;
+            if (p.q_wide) {
+                staged[i] = load_global<V8>((uint64_t)from);
             } else {
 #pragma unroll
-                for (int y = 0; y < 8; y++) staged[i][y] = (T)0.f;
+                for (int y = 0; y < 8; y++) staged[i][y] = load_global<T>((uint64_t)(from + y * 2));
             }
+            qt[i] += step_t;
+            qg[i] += step_g;
+            if (qg[i] >= G) qg[i] -= G, qt[i]++;
         }
         if (tid < kWRows) {
             const int row = at + tid, t = row / G;
@@ -457,6 +466,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
         take(row0);
         put(0);
     }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // the keys are there: no wait for them in the loop
     __syncthreads();
     int buf = 0;
     for (int at = row0; at < row1; at += kWRows, buf ^= 1) {
@@ -480,6 +490,14 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
                     sc[0] = E::mfma32(k[0][x], b, sc[0]);
                     sc[1] = E::mfma32(k[1][x], b, sc[1]);
                 }
+                // reads two products ahead of their use
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+                for (int x = 0; x < KS - 2; x++) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
                 const float lse = stat[buf][rt * 32 + c];
                 if (whole) {
 #pragma unroll
@@ -488,15 +506,16 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
                         for (int i = 0; i < 16; i++) sum[st][i] += exp2_fast(fmaf(sc[st][i], p.scale, -lse));
                 } else {
                     const int r = r0 + (at + rt * 32 + c) / G;
+                    const uint64_t seen = bits_between(p.window > 0 ? r - p.window + 1 - base : 0, p.causal ? r - base : 63) >> (h * 4);
 #pragma unroll
-                    for (int st = 0; st < 2; st++)
+                    for (int st = 0; st < 2; st++) {
+                        const uint32_t word = (uint32_t)(seen >> (st * 32));
 #pragma unroll
                         for (int i = 0; i < 16; i++) {
-                            const int j = base + st * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
-                            const bool seen = (!p.causal || j <= r) && (p.window == 0 || j > r - p.window);
                             const float e = exp2_fast(fmaf(sc[st][i], p.scale, -lse));
-                            sum[st][i] += seen ? e : 0.f;
+                            sum[st][i] += word >> ((i >> 2) * 8 + (i & 3)) & 1 ? e : 0.f;
                         }
+                    }
                 }
             }
         }
