@@ -72,8 +72,6 @@ int64_t attend_workspace(const AttendSizes& z);
 int32_t few_rows(const AttendSizes& z);
 int64_t rows_workspace(const AttendSizes& z);
 hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s);
-// The kernels of many rows (svf_kv_chunk.hip).
-hipError_t launch_chunk(const AttendArgs& a, const AttendSizes& z, hipStream_t s);
 
 // Pairs (hole, mover) that one sequence's key head can have.
 inline int64_t evict_pairs(int64_t capacity, int64_t budget) {

@@ -8,6 +8,19 @@ namespace {
 constexpr int kRows = 128;  // rows of a workgroup, 32 for each of its four waves
 constexpr int kTile = 64;   // slots that it takes at a time
 
+// A row tile of a key head whose slots are split, and what its parts are joined by.
+struct Item {
+    int32_t q0, first_row, rows, parts;
+};
+constexpr int kMostParts = 64;
+
+struct ChunkPlan {
+    int32_t groups;  // workgroups that the GPU holds; 0: no tile is split
+    int32_t* items;  // row tiles over all key heads, 0 where none is split
+    Item* item;      // [groups / 2]
+    float* part;     // [groups][kRows][D + 4]
+};
+
 // Whether these kernels take the sequence, and not those of few rows.
 __device__ inline bool ours(const AttendArgs& p, const Seq& s) {
     if (s.n > p.kv.max_q) return p.few == 0;
@@ -19,9 +32,10 @@ __device__ inline int row_tiles(const AttendArgs& p, const Seq& s) {
 }
 
 // Finds what ``count`` numbers: the sequence that item ``at`` of all sequences' items
-// belongs to, and the item's number in it. For a whole workgroup of 256; false where there are fewer items.
-template <class Count>
-__device__ inline bool find_item(const KvView& kv, int64_t at, Count count, int64_t* scan, int& seq, int& item) {
+// belongs to, and the item's number in it; ``place`` makes ``at`` from the number of all items.
+// For a whole workgroup of 256; false where there is no such item.
+template <class Count, class Place>
+__device__ inline bool find_item(const KvView& kv, Place place, Count count, int64_t* scan, int& seq, int& item) {
     __shared__ int sh_seq, sh_item;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (kv.seqs + 255) / 256;
@@ -36,8 +50,12 @@ __device__ inline bool find_item(const KvView& kv, int64_t at, Count count, int6
     if (lane == 63) scan[wave] = incl;
     if (tid == 0) sh_seq = -1;
     __syncthreads();
-    int64_t before = incl - mine;
-    for (int w = 0; w < wave; w++) before += scan[w];
+    int64_t before = incl - mine, total = 0;
+    for (int w = 0; w < 4; w++) {
+        if (w < wave) before += scan[w];
+        total += scan[w];
+    }
+    const int64_t at = place(total);
     if (before <= at && at < before + mine) {
         for (int i = i0; i < i1; i++) {
             const int c = count(seq_of(kv, i));
@@ -79,7 +97,7 @@ __device__ inline int swizzle(int row) {
 // the whole wave but for an offset that stays the same all along (a tile costs a wave 8 loads and some scalar
 // instructions, and 100 vector instructions otherwise).
 template <class E, int D, bool WIDE>
-__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(AttendArgs p) {
+__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(AttendArgs p, ChunkPlan plan) {
     using T = typename E::T;
     using V8 = typename E::V8;
     typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -92,20 +110,44 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads;
-    const int head = blockIdx.x % hk;
-    int seq, tile;
-    if (!find_item(p.kv, blockIdx.x / hk, [&](const Seq& s) { return row_tiles(p, s); }, scan, seq, tile)) return;
+    int seq, tile, item = 0, part = 0, parts = 1;
+    const bool found = find_item(
+        p.kv,
+        [&](int64_t total) {
+            // Few row tiles: as many parts of each one's slots as there is room for, all first parts first.
+            const int64_t all = total * hk;
+            if (plan.groups > 0 && all > 0) parts = (int)min((int64_t)kMostParts, max((int64_t)1, plan.groups / all));
+            if (plan.groups > 0 && blockIdx.x == 0 && threadIdx.x == 0) *plan.items = parts > 1 ? (int)all : 0;
+            if (blockIdx.x >= all * parts) return total;
+            part = (int)(blockIdx.x / all);
+            item = (int)(blockIdx.x - part * all);
+            return (int64_t)(item / hk);
+        },
+        [&](const Seq& s) { return row_tiles(p, s); }, scan, seq, tile);
+    if (!found) return;
+    const int head = item % hk;
     const Seq s = seq_of(p.kv, seq);
     if (s.n > p.kv.max_q) {
-        if (tile == 0) fill_nan<T, D>(p, s, head, G, tid, 256);
+        if (tile == 0 && part == 0) fill_nan<T, D>(p, s, head, G, tid, 256);
+        if (parts > 1 && part == 0 && tid == 0) plan.item[item] = Item{0, 0, 0, 0};
         return;
     }
     tile = row_tiles(p, s) - 1 - tile;  // the longest first
     const int rows = s.n * G, r0 = s.len - s.n;
     const int first_row = tile * kRows, last_row = min(first_row + kRows, rows) - 1;
-    const int lo = p.window > 0 ? max(0, r0 + first_row / G - p.window + 1) & ~15 : 0;
-    const int hi = p.causal ? min(s.len, r0 + last_row / G + 1) : s.len;
-    const int tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+    int lo = p.window > 0 ? max(0, r0 + first_row / G - p.window + 1) & ~15 : 0;
+    int hi = p.causal ? min(s.len, r0 + last_row / G + 1) : s.len;
+    int tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+    if (parts > 1) {
+        // no part of fewer than four tiles: it would cost more to join than it saves
+        parts = max(1, min(parts, tiles / 4));
+        if (part >= parts) return;
+        if (part == 0 && tid == 0) plan.item[item] = Item{s.q0, first_row, rows, parts};
+        const int from = (int)((int64_t)tiles * part / parts), to = (int)((int64_t)tiles * (part + 1) / parts);
+        hi = min(hi, lo + to * kTile);
+        lo += from * kTile;
+        tiles = to - from;
+    }
 
     // this lane's row, and the slots that all and any of the wave's rows see
     const int row = first_row + wave * 32 + c;
@@ -349,23 +391,59 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         if (it + 1 < tiles) step(it + 1, k1, v1, k0, v0);
     }
 
-    if (row < rows) {
-        l += __shfl_xor(l, 32);
-        const int hq = head * G + row - t * G;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        char* out = p.out + (s.q0 + t) * p.o_tok + hq * p.o_head;
-        typedef T V4 __attribute__((ext_vector_type(4)));
+    l += __shfl_xor(l, 32);
+    if (row >= rows) return;
+    const int hq = head * G + row - t * G;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    char* out = p.out + (s.q0 + t) * p.o_tok + hq * p.o_head;
+    float* to = nullptr;
+    if (parts > 1) to = plan.part + ((int64_t)blockIdx.x * kRows + wave * 32 + c) * (D + 4);
+    typedef T V4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int d = 0; d < DT; d++)
+    for (int d = 0; d < DT; d++)
 #pragma unroll
-            for (int b = 0; b < 4; b++) {
-                const int dim = d * 32 + b * 8 + h * 4;
-                float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
-                add_marks(odd_marks[wave * 32 + c][dim >> 4] >> 2 * (dim & 15), x, 4);
+        for (int b = 0; b < 4; b++) {
+            const int dim = d * 32 + b * 8 + h * 4;
+            float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+            add_marks(odd_marks[wave * 32 + c][dim >> 4] >> 2 * (dim & 15), x, 4);
+            if (to)
+                *(f32x4*)(to + dim) = f32x4{x[0], x[1], x[2], x[3]};
+            else
                 *(V4*)(out + dim * 2) = V4{(T)(x[0] * inv), (T)(x[1] * inv), (T)(x[2] * inv), (T)(x[3] * inv)};
-            }
-        if (h == 0) p.lse[(int64_t)(s.q0 + t) * p.heads + hq] = (m - E::kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+        }
+    if (h == 0) {
+        if (to)
+            to[D] = m, to[D + 1] = l;
+        else
+            p.lse[(int64_t)(s.q0 + t) * p.heads + hq] = (m - E::kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
     }
+}
+
+// The parts of row tiles that were split: eight rows of a tile at a time, 32 lanes a row.
+template <class E, int D>
+__global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan) {
+    constexpr int VD = D / 32;
+    const int items = *plan.items, G = p.heads / p.kv.kv_heads;
+    const int item = blockIdx.x / (kRows / 8), row = blockIdx.x % (kRows / 8) * 8 + (threadIdx.x >> 5);
+    if (item >= items) return;
+    const Item x = plan.item[item];
+    const int head = item % p.kv.kv_heads, at = x.first_row + row, d0 = (threadIdx.x & 31) * VD;
+    if (x.parts < 2 || at >= x.rows) return;
+    float top = -INFINITY, den = 0.f, acc[VD];
+#pragma unroll
+    for (int j = 0; j < VD; j++) acc[j] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < x.parts; i++) {
+        const float* from = plan.part + (((int64_t)i * items + item) * kRows + row) * (D + 4);
+        const float now = fmaxf(top, from[D]), ref = now == -INFINITY ? 0.f : now;
+        const float keep = exp2_fast(top - ref), f = exp2_fast(from[D] - ref);
+        den = den * keep + from[D + 1] * f;
+#pragma unroll
+        for (int j = 0; j < VD; j++) acc[j] = acc[j] * keep + from[d0 + j] * f;
+        top = now;
+    }
+    const int t = at / G;
+    write_row<E, VD>(p, x.q0 + t, head * G + at - t * G, d0, acc, den, top);
 }
 
 // The weights of these sequences' slots: scores once more, now against the rows' final statistics.
@@ -390,7 +468,9 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads, head = blockIdx.x % hk;
     int seq, tile;
-    if (!find_item(p.kv, blockIdx.x / hk, [&](const Seq& s) { return slot_tiles(p, s); }, scan, seq, tile)) return;
+    if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles(p, s); }, scan,
+                   seq, tile))
+        return;
     const Seq s = seq_of(p.kv, seq);
     const int r0 = s.len - s.n;
     const int j0 = first_slot(p, s) + tile * kWSlots, j1 = min(j0 + kWSlots, s.len);
@@ -534,21 +614,46 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
         }
 }
 
+// Row tiles at least: those of the rows that sequences of few rows cannot have. With more than half as many as the
+// GPU holds workgroups none is split.
+int32_t split_groups(const AttendSizes& z, int32_t few) {
+    const int32_t groups = z.dim <= 128 ? 512 : 256;
+    const int64_t least = ((int64_t)z.tokens * (z.heads / z.kv_heads) - (int64_t)z.seqs * few) / kRows;
+    return least * z.kv_heads > groups / 2 ? 0 : groups;
+}
+
+int64_t chunk_workspace(const AttendSizes& z, int32_t few) {
+    const int32_t groups = split_groups(z, few);
+    return groups ? 256 + groups / 2 * (int64_t)sizeof(Item) + (int64_t)groups * kRows * (z.dim + 4) * 4 : 0;
+}
+
 template <class E, int D>
-hipError_t launch(const AttendArgs& a, const AttendSizes& z, hipStream_t s) {
+hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {
+    ChunkPlan plan{split_groups(z, a.few), nullptr, nullptr, nullptr};
+    if (plan.groups) {
+        plan.items = (int32_t*)ws;
+        plan.item = (Item*)(ws + 256);
+        plan.part = (float*)(ws + 256 + plan.groups / 2 * sizeof(Item));
+    }
     // Row tiles at most: the full ones of all tokens, and one more for each sequence that is long enough to come here.
     const int64_t rows = (int64_t)z.tokens * (z.heads / z.kv_heads), seqs = rows / (a.few + 1);
-    const int64_t blocks = (rows / kRows + (seqs < z.seqs ? seqs : z.seqs)) * z.kv_heads;
+    int64_t blocks = (rows / kRows + (seqs < z.seqs ? seqs : z.seqs)) * z.kv_heads;
+    if (blocks < plan.groups) blocks = plan.groups;
     if (blocks > 0) {
         // Offsets of sixteen rows are 32 bits.
         const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
         if (z.page_size >= 16 && far < (int64_t(1) << 31))
-            k_attend_chunk<E, D, true><<<(unsigned)blocks, 256, 0, s>>>(a);
+            k_attend_chunk<E, D, true><<<(unsigned)blocks, 256, 0, s>>>(a, plan);
         else
-            k_attend_chunk<E, D, false><<<(unsigned)blocks, 256, 0, s>>>(a);
+            k_attend_chunk<E, D, false><<<(unsigned)blocks, 256, 0, s>>>(a, plan);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    if (plan.groups) {
+        k_join_chunk<E, D><<<plan.groups / 2 * (kRows / 8), 256, 0, s>>>(a, plan);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if (a.add_weight) {
         // slot tiles at most: each page is in the batch once
         const int64_t cap = (int64_t)z.width * z.page_size, most = seqs < z.seqs ? seqs : z.seqs;
@@ -561,22 +666,24 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_chunk(const AttendArgs& a, const AttendSizes& z, hipStream_t s) {
-    if (z.dtype == SVF_KV_BF16)
-        return z.dim == 64 ? launch<BF16M, 64>(a, z, s) : z.dim == 128 ? launch<BF16M, 128>(a, z, s) : launch<BF16M, 256>(a, z, s);
-    return z.dim == 64 ? launch<F16M, 64>(a, z, s) : z.dim == 128 ? launch<F16M, 128>(a, z, s) : launch<F16M, 256>(a, z, s);
-}
-
 // A call's launches: single tokens and short chunks, and, where a sequence may have more rows, chunks.
-int64_t attend_workspace(const AttendSizes& z) { return rows_workspace(z); }
+bool has_chunks(const AttendSizes& z) { return (int64_t)z.max_q * (z.heads / z.kv_heads) > few_rows(z); }
+
+int64_t attend_workspace(const AttendSizes& z) {
+    return ((rows_workspace(z) + 255) & ~int64_t(255)) + (has_chunks(z) ? chunk_workspace(z, few_rows(z)) : 0);
+}
 
 hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s) {
     a.few = few_rows(z);
     if (a.few) {
         const hipError_t e = launch_rows(a, z, a.ws, s);
-        if (e != hipSuccess || (int64_t)z.max_q * (z.heads / z.kv_heads) <= a.few) return e;
+        if (e != hipSuccess) return e;
     }
-    return launch_chunk(a, z, s);
+    if (!has_chunks(z)) return hipSuccess;
+    char* ws = a.ws + ((rows_workspace(z) + 255) & ~int64_t(255));
+    if (z.dtype == SVF_KV_BF16)
+        return z.dim == 64 ? launch<BF16M, 64>(a, z, ws, s) : z.dim == 128 ? launch<BF16M, 128>(a, z, ws, s) : launch<BF16M, 256>(a, z, ws, s);
+    return z.dim == 64 ? launch<F16M, 64>(a, z, ws, s) : z.dim == 128 ? launch<F16M, 128>(a, z, ws, s) : launch<F16M, 256>(a, z, ws, s);
 }
 
 }  // namespace svfk

@@ -222,6 +222,28 @@ def test_attend_long_rows_are_split():
         assert torch.equal(out, a[0]) and torch.equal(lse, a[1]) and torch.equal(w, a[2])
 
 
+@pytest.mark.parametrize("dtype,heads,kv_heads,dim", [(BF, 8, 1, 128), (HF, 4, 2, 64), (BF, 4, 1, 256)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 700)])
+def test_attend_few_row_tiles_are_split(dtype, heads, kv_heads, dim, causal, window):
+    from paper_2606_22327_amd import kvcache as C
+    s = make(18, [3000, 30, 1029, 0, 300], [40, 1, 70, 0, 33], heads, kv_heads, dim, 16, dtype, stats=True)
+    s["table"][0, 50:55] = -1
+    a = check_attend(s, causal=causal, window=window, add_weight=True)
+    w = s["weight"].cuda()
+    out, lse = C.attend(s["q"].cuda(), batch_of(s), C.Cache(s["k"].cuda(), s["v"].cuda(), w), causal=causal, window=window,
+                        add_weight=True)
+    assert torch.equal(out, a[0]) and torch.equal(lse, a[1]) and torch.equal(w, a[2])
+
+
+def test_attend_split_tiles_and_values_that_are_not_numbers():
+    s = make(19, [2000], [60], 4, 1, 128, 16, BF)
+    pg, row = P.slots_of(s["table"], 0, 2000, 16, s["k"].shape[0])
+    s["v"][pg[100], 0, row[100], 7] = float("inf")
+    s["v"][pg[1990], 0, row[1990], 9] = float("nan")
+    out, _, _ = check_attend(s)
+    assert (out[:, 0, 7] == math.inf).all() and torch.isfinite(out[:49, 0, 9]).all() and out[50:, 0, 9].isnan().all()
+
+
 @pytest.mark.parametrize("new", [1, 64])
 def test_attend_past_32_bit_offsets(new):
     """Pages whose elements lie past 2^32 bytes and 2^31 elements."""
