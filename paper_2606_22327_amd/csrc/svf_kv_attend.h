@@ -68,9 +68,10 @@ __device__ inline void add_marks(uint32_t marks, float* acc, int n) {
     }
 }
 
-// The first slot that any row of the sequence sees.
+// The first slot that any row of the sequence sees, or one of the fifteen before it: pages of 16 slots and more
+// are read from a multiple of 16.
 __device__ inline int first_slot(const AttendArgs& p, const Seq& s) {
-    return p.window > 0 ? max(0, s.len - s.n - p.window + 1) : 0;
+    return p.window > 0 ? max(0, s.len - s.n - p.window + 1) & ~15 : 0;
 }
 
 // Where a lane reads a slot that is not there: a row of zeros, so that loads need no branch.

@@ -13,6 +13,7 @@ struct RowsPlan {
     int64_t* first_unit;  // [seqs + 1]: units of a key head before each sequence; null where no launch follows
     float* part;          // [2 * groups][rows * (D + 4)]: partial results
     float* scores;        // [units][rows][kUnit] (add_weight): scores in log2 terms
+    int4* units;          // [units] (add_weight): sequence, index of the first row's statistic, first slot, head | rows << 16
     int64_t score_units;  // units that scores has room for
     int32_t groups;       // workgroups over which the units are dealt out
     int32_t rows;         // rows of a sequence's key head at most
@@ -43,10 +44,14 @@ struct Tile {
     uint32_t v[8][D / 32];  // two dimensions a word
 };
 
-// Where slots lie: a lane has the addresses of slot lane % 32 of the wave's tile and hands them
-// to the lanes that load it. A slot that is not there is a row of zeros.
+// Where the slots of a wave's tile lie.
+// WIDE: pages of 16 slots or more, so that each half of the tile lies in one page: two addresses for the whole wave, and what
+// a lane adds to them stays the same all along.
+// Else a lane has the addresses of slot lane % 32 and hands them to the lanes that load it.
+// A slot that is not there is a row of zeros; behind the last slot of a page that is there, WIDE reads what
+// the page holds, and nothing comes of it.
 struct Where {
-    uint64_t k, v;
+    uint64_t k[2], v[2];
     bool there;
 };
 
@@ -55,38 +60,52 @@ __device__ inline uint64_t from_lane(uint64_t x, int lane) {
     return (uint64_t)hi << 32 | lo;
 }
 
-template <class E, int D>
-__device__ inline void load_k(Tile<E, D>& x, const Where& w) {
+// ``rows``: bytes from one row to the next, 0 in the zeros.
+template <class E, int D, bool WIDE>
+__device__ inline void load_k(Tile<E, D>& x, const Where& w, uint32_t row_bytes) {
+    typedef const __attribute__((address_space(1))) char* Global;
+    typedef const __attribute__((address_space(1))) typename E::V8* Global8;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int t = 0; t < 2; t++) {
-        const uint64_t at = from_lane(w.k, t * 16 + c) + g * 16;
+        if constexpr (WIDE) {
+            const uint32_t off = (w.k[t] == (uint64_t)zero_row() ? 0 : c * row_bytes) + g * 16;
 #pragma unroll
-        for (int s = 0; s < D / 32; s++) x.k[t][s] = load_global<typename E::V8>(at + s * 64);
+            for (int s = 0; s < D / 32; s++) x.k[t][s] = *(Global8)((Global)w.k[t] + off + s * 64);
+        } else {
+            const uint64_t at = from_lane(w.k[0], t * 16 + c) + g * 16;
+#pragma unroll
+            for (int s = 0; s < D / 32; s++) x.k[t][s] = load_global<typename E::V8>(at + s * 64);
+        }
     }
 }
 
-template <class E, int D>
-__device__ inline void load_v(Tile<E, D>& x, const Where& w) {
+template <class E, int D, bool WIDE>
+__device__ inline void load_v(Tile<E, D>& x, const Where& w, uint32_t row_bytes) {
     typedef uint32_t Row __attribute__((ext_vector_type(D / 32)));
+    typedef const __attribute__((address_space(1))) char* Global;
+    typedef const __attribute__((address_space(1))) Row* GlobalRow;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-        const Row r = load_global<Row>(from_lane(w.v, (j >> 2) * 16 + g * 4 + (j & 3)) + c * (D / 8));
+        Row r;
+        if constexpr (WIDE) {
+            const uint32_t off = (w.v[j >> 2] == (uint64_t)zero_row() ? 0 : (g * 4 + (j & 3)) * row_bytes) + c * (D / 8);
+            r = *(GlobalRow)((Global)w.v[j >> 2] + off);
+        } else {
+            r = load_global<Row>(from_lane(w.v[0], (j >> 2) * 16 + g * 4 + (j & 3)) + c * (D / 8));
+        }
 #pragma unroll
         for (int i = 0; i < D / 32; i++) x.v[j][i] = r[i];
     }
 }
 
-// Waves of a SIMD that the registers of a tile leave room for. (Spilled registers are reloaded in the loop, and a wait
-// for one is a wait for every load on its way.)
-template <int D, int RT>
-constexpr int waves_per_simd() {
-    return D * RT <= 64 ? 3 : D * RT <= 128 ? 2 : 1;
-}
+// Waves of a SIMD that the registers of a tile leave room for.  (Squeezed into a third wave's, 128 dimensions spill
+// 14 registers, though none that the loop needs, and take 78 us where they took 68.)
+constexpr int waves_per_simd(int dim, int rt) { return dim * rt <= 64 ? 3 : dim * rt <= 128 ? 2 : 1; }
 
-template <class E, int D, int RT>
-__global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(AttendArgs p, RowsPlan plan) {
+template <class E, int D, int RT, bool WIDE>
+__global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(AttendArgs p, RowsPlan plan) {
     using T = typename E::T;
     using V8 = typename E::V8;
     constexpr int KS = D / 32, VD = D / 16;
@@ -96,7 +115,8 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
     __shared__ uint32_t odd_marks[16 * RT][16];  // a word for D / 16 dimensions of a row
     __shared__ int sh_seq;
     __shared__ int64_t sh_first;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads;
 
     // Deal the units out: sequences in order, key head by key head, an equal run of units for
@@ -161,12 +181,12 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
         const int rows = s.n * G;
         if (s.n > p.kv.max_q) {
             fill_nan<T, D>(p, s, head, G, tid, 256);
+            if (plan.scores && unit0 < plan.score_units && tid == 0) plan.units[unit0] = make_int4(seq, 0, 0, head);
             continue;
         }
         const int lo = first_slot(p, s);
         const int r0 = s.len - s.n;  // the first new token's slot
-        const char* kbase = p.kv.k + head * p.kv.k_head;
-        const char* vbase = p.kv.v + head * p.kv.v_head;
+        const uint64_t kbase = (uint64_t)(p.kv.k + head * p.kv.k_head), vbase = (uint64_t)(p.kv.v + head * p.kv.v_head);
 
         V8 q[RT][KS];
         int last[RT], from[RT];  // a lane's rows see slots from .. last
@@ -194,12 +214,24 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
             const int j = slot0 + u * kUnit, row = entry_row(p.kv, page, j, u < u1 && j < s.len);
             Where w;
             w.there = row >= 0;
-            const uint64_t k = (uint64_t)kbase + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row);
-            const uint64_t v = (uint64_t)vbase + row_offset(row, p.kv.shift, p.kv.v_page, p.kv.v_row);
-            w.k = w.there ? k : (uint64_t)zero_row();
-            w.v = w.there ? v : (uint64_t)zero_row();
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    const int at = __builtin_amdgcn_readlane(row, t * 16);
+                    const int pg = at >> p.kv.shift, r = at & ((1 << p.kv.shift) - 1);
+                    w.k[t] = at < 0 ? (uint64_t)zero_row() : row_address(kbase, pg, r, p.kv.k_page, p.kv.k_row);
+                    w.v[t] = at < 0 ? (uint64_t)zero_row() : row_address(vbase, pg, r, p.kv.v_page, p.kv.v_row);
+                }
+            } else {
+                const int pg = row >> p.kv.shift, r = row & ((1 << p.kv.shift) - 1);
+                const uint64_t k = row_address(kbase, pg, r, p.kv.k_page, p.kv.k_row);
+                const uint64_t v = row_address(vbase, pg, r, p.kv.v_page, p.kv.v_row);
+                w.k[0] = w.there ? k : (uint64_t)zero_row();
+                w.v[0] = w.there ? v : (uint64_t)zero_row();
+            }
             return w;
         };
+        const uint32_t k_row = (uint32_t)p.kv.k_row, v_row = (uint32_t)p.kv.v_row;
         int page0 = entry(u0), page_next = entry(u0 + 1);
         for (int i = tid; i < 16 * RT * 16; i += 256) (&odd_marks[0][0])[i] = 0;
         __syncthreads();
@@ -207,9 +239,9 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
         Where now = where(u0, page0);
         // In the loop's order: where the two meet, the compiler waits for the more careful of them.
         __builtin_amdgcn_sched_barrier(0);
-        load_k(x, now);
+        load_k<E, D, WIDE>(x, now, k_row);
         __builtin_amdgcn_sched_barrier(0);
-        load_v(x, now);
+        load_v<E, D, WIDE>(x, now, v_row);
         __builtin_amdgcn_sched_barrier(0);
         for (int u = u0; u < u1; u++) {
             const Where next = where(u + 1, page_next);
@@ -228,7 +260,7 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
             const uint32_t there = (uint32_t)__ballot(now.there);
             const bool all_seen = there == 0xffffffffu && (!p.causal || base + 31 <= r0) && (p.window == 0 || base > s.len - 1 - p.window);
             __builtin_amdgcn_sched_barrier(0);
-            load_k(x, next);
+            load_k<E, D, WIDE>(x, next, k_row);
             __builtin_amdgcn_sched_barrier(0);
             V8 hi[RT], low[RT];
 #pragma unroll
@@ -245,11 +277,6 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
                 }
 #pragma unroll
                 for (int i = 0; i < 8; i++) top = fmaxf(top, sc[rt][i >> 2][i & 3]);
-                if (plan.scores && unit0 + (u - u0) < plan.score_units && rt * 16 + c < rows) {
-                    float* to = plan.scores + ((unit0 + (u - u0)) * plan.rows + rt * 16 + c) * kUnit + wave * 32 + g * 4;
-                    *(f32x4*)to = sc[rt][0];
-                    *(f32x4*)(to + 16) = sc[rt][1];
-                }
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float peak = fmaxf(m[rt], top);
@@ -292,9 +319,9 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
                     for (int i = 0; i < 8 * (D / 32); i++) {
                         const uint32_t pair = own[i * 64];
                         if (!odd_pair<E>(pair)) continue;
-                        const int at = i / (D / 32), j = base + (at >> 2) * 16 + g * 4 + (at & 3);
+                        const int at = i / (D / 32), off = (at >> 2) * 16 + g * 4 + (at & 3), j = base + off;
                         const uint32_t marks = odd_marks_of<E>(pair) << 4 * (i % (D / 32));
-                        for (int row = 0; row < rows; row++) {
+                        for (int row = 0; row < rows && (there >> off & 1); row++) {
                             const int r = r0 + row / G;
                             if ((!p.causal || j <= r) && (p.window == 0 || j > r - p.window)) atomicOr(&odd_marks[row][c], marks);
                         }
@@ -320,8 +347,20 @@ __global__ __launch_bounds__(256, (waves_per_simd<D, RT>())) void k_attend_rows(
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            load_v(x, next);
+            load_v<E, D, WIDE>(x, next, v_row);
             __builtin_amdgcn_sched_barrier(0);
+            // behind the loads: a wait for those is none for these
+            const int64_t unit = unit0 + (u - u0);
+            if (plan.scores && unit < plan.score_units) {
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++)
+                    if (rt * 16 + c < rows) {
+                        float* to = plan.scores + (unit * plan.rows + rt * 16 + c) * kUnit + wave * 32 + g * 4;
+                        *(f32x4*)to = sc[rt][0];
+                        *(f32x4*)(to + 16) = sc[rt][1];
+                    }
+                if (tid == 0) plan.units[unit] = make_int4(seq, s.q0 * p.heads + head * G, lo + u * kUnit, head | rows << 16);
+            }
             now = next;
         }
 
@@ -462,39 +501,41 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
 
 // The weights of these sequences' slots from the scores and the rows' final statistics: a wave
 // for half a unit, its rows in order.
-template <class E>
 __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan) {
     const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
-    const int64_t all = plan.first_unit[p.kv.seqs] * hk;
-    for (int64_t half = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); half < 2 * all; half += (int64_t)gridDim.x * 4) {
-        const int64_t unit = half >> 1;
-        if (unit >= plan.score_units) return;
-        const int lo = seq_of_unit(p, plan, unit);
-        const Seq s = seq_of(p.kv, lo);
-        const int64_t units = plan.first_unit[lo + 1] - plan.first_unit[lo], rel = unit - plan.first_unit[lo] * hk;
-        if (units <= 0 || s.n > p.kv.max_q) continue;
-        const int head = (int)(rel / units);
-        const int j = first_slot(p, s) + (int)(rel - head * units) * kUnit + (int)(half & 1) * 64 + lane;
-        const int row = j < s.len ? pool_row(p.kv, lo, j) : -1;
-        const float* sc = plan.scores + unit * plan.rows * kUnit + (half & 1) * 64 + lane;
-        float sum = 0.f;
-        for (int r = 0; r < s.n * G; r++) {
-            const int t = r / G;
-            const float lse = p.lse[(int64_t)(s.q0 + t) * p.heads + head * G + r - t * G] * 1.4426950408889634f;
-            if (lse != -INFINITY) sum += exp2_fast(sc[r * kUnit] - lse);
-        }
-        if (row >= 0) p.kv.weight[stat_index(p.kv, row, head)] += sum;
+    const int64_t half = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), unit = half >> 1;
+    if (unit >= plan.score_units || unit >= plan.first_unit[p.kv.seqs] * hk) return;
+    const int4 x = plan.units[unit];
+    const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + (int)(half & 1) * 64 + lane;
+    const int page = table_entry(p.kv, table_of(p.kv, x.x, zero_row()), j);
+    const float* sc = plan.scores + unit * plan.rows * kUnit + (half & 1) * 64 + lane;
+    float sum = 0.f;
+    for (int r = 0; r < rows; r++) {
+        const int t = r / G;
+        const float lse = p.lse[x.y + t * p.heads + r - t * G] * 1.4426950408889634f;
+        if (lse != -INFINITY) sum += exp2_fast(sc[r * kUnit] - lse);
     }
+    // a slot that is not there has scores of -inf only
+    const int row = entry_row(p.kv, page, j, sum != 0.f);
+    if (row >= 0) p.kv.weight[stat_index(p.kv, row, head)] += sum;
+}
+
+template <class E, int D, bool WIDE>
+void launch_tiles(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
+    if (plan.rows <= 16)
+        k_attend_rows<E, D, 1, WIDE><<<plan.groups, 256, 0, s>>>(a, plan);
+    else if constexpr (D <= 128)
+        k_attend_rows<E, D, 2, WIDE><<<plan.groups, 256, 0, s>>>(a, plan);
 }
 
 template <class E, int D>
 hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
-    if (plan.rows <= 16)
-        k_attend_rows<E, D, 1><<<plan.groups, 256, 0, s>>>(a, plan);
-    else if (plan.rows <= 32)
-        k_attend_rows<E, D, 2><<<plan.groups, 256, 0, s>>>(a, plan);
-    else if constexpr (D <= 128)
-        k_attend_rows<E, D, 4><<<plan.groups, 256, 0, s>>>(a, plan);
+    // Offsets of sixteen rows are 32 bits.
+    const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
+    if (a.kv.shift >= 4 && far < (int64_t(1) << 31))
+        launch_tiles<E, D, true>(a, plan, s);
+    else
+        launch_tiles<E, D, false>(a, plan, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t cap = (int64_t)a.kv.width << a.kv.shift;
@@ -508,20 +549,14 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.add_weight) k_weight_rows<E><<<2048, 256, 0, s>>>(a, plan);
+    if (a.add_weight && plan.score_units > 0) k_weight_rows<<<(unsigned)((plan.score_units + 1) / 2), 256, 0, s>>>(a, plan);
     return hipGetLastError();
-}
-
-// As many workgroups as the GPU holds at a time.
-int32_t most_groups(int32_t dim, int32_t rows) {
-    const int rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    return 256 * (dim * rt <= 64 ? 3 : dim * rt <= 128 ? 2 : 1);
 }
 
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
 struct Layout {
-    int64_t part, scores, units, bytes;
+    int64_t part, scores, descs, units, bytes;
     int32_t groups, rows;
 };
 
@@ -530,7 +565,7 @@ Layout layout(const AttendSizes& z) {
     const int64_t cap = (int64_t)z.width * z.page_size;
     const int64_t most = (int64_t)z.seqs * z.kv_heads * ((cap + kUnit - 1) / kUnit > 0 ? (cap + kUnit - 1) / kUnit : 1);
     y.rows = few_rows(z);
-    y.groups = most_groups(z.dim, y.rows);
+    y.groups = 256 * waves_per_simd(z.dim, y.rows <= 16 ? 1 : 2);  // what the GPU holds at a time
     if (most < y.groups) y.groups = (int32_t)most;
     y.part = round256((int64_t)(z.seqs + 1) * 8);
     y.scores = y.part + round256((int64_t)2 * y.groups * y.rows * (z.dim + 4) * 4);
@@ -540,16 +575,18 @@ Layout layout(const AttendSizes& z) {
         y.units = ((int64_t)z.num_pages * z.page_size / kUnit + z.seqs) * z.kv_heads;
         if (y.units > most) y.units = most;
     }
-    y.bytes = y.scores + round256(y.units * y.rows * kUnit * 4);
+    y.descs = y.scores + round256(y.units * y.rows * kUnit * 4);
+    y.bytes = y.descs + y.units * 16;
     return y;
 }
 
 }  // namespace
 
-// Rows that these kernels take: a whole batch's where no sequence has more than 64 (32 of 256 dimensions), else
-// single tokens' (or 16, whichever is more).
+// Rows that these kernels take: a whole batch's where no sequence has more than 32 (16 of 256 dimensions), else
+// single tokens' (or 16, whichever is more).  With 32 query heads on 8 key heads of 128 dimensions and 8 sequences of
+// 8,000 slots, 20 rows take 63 us here and 71 as a tile of 128 rows, 40 rows 75 and 72, 64 rows 82 and 72.
 int32_t few_rows(const AttendSizes& z) {
-    const int32_t G = z.heads / z.kv_heads, most = z.dim <= 128 ? 64 : 32;
+    const int32_t G = z.heads / z.kv_heads, most = z.dim <= 128 ? 32 : 16;
     const int64_t want = (int64_t)z.max_q * G;
     if (want <= most) return (int32_t)(want < 1 ? 1 : want);
     const int32_t single = G > 16 ? G : 16;
@@ -567,6 +604,7 @@ hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipS
     plan.first_unit = one_launch(z) ? nullptr : (int64_t*)ws;
     plan.part = (float*)(ws + y.part);
     plan.scores = a.add_weight ? (float*)(ws + y.scores) : nullptr;
+    plan.units = (int4*)(ws + y.descs);
     plan.score_units = y.units;
     plan.groups = y.groups;
     plan.rows = y.rows;
