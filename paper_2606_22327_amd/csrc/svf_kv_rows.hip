@@ -60,7 +60,7 @@ __device__ inline uint64_t from_lane(uint64_t x, int lane) {
     return (uint64_t)hi << 32 | lo;
 }
 
-// ``rows``: bytes from one row to the next, 0 in the zeros.
+// Each is read once by its key head's rows: past the caches (256 sequences with weights: 278 us and 299 through them).
 template <class E, int D, bool WIDE>
 __device__ inline void load_k(Tile<E, D>& x, const Where& w, uint32_t row_bytes) {
     typedef const __attribute__((address_space(1))) char* Global;
@@ -71,7 +71,7 @@ __device__ inline void load_k(Tile<E, D>& x, const Where& w, uint32_t row_bytes)
         if constexpr (WIDE) {
             const uint32_t off = (w.k[t] == (uint64_t)zero_row() ? 0 : c * row_bytes) + g * 16;
 #pragma unroll
-            for (int s = 0; s < D / 32; s++) x.k[t][s] = *(Global8)((Global)w.k[t] + off + s * 64);
+            for (int s = 0; s < D / 32; s++) x.k[t][s] = __builtin_nontemporal_load((Global8)((Global)w.k[t] + off + s * 64));
         } else {
             const uint64_t at = from_lane(w.k[0], t * 16 + c) + g * 16;
 #pragma unroll
@@ -91,7 +91,7 @@ __device__ inline void load_v(Tile<E, D>& x, const Where& w, uint32_t row_bytes)
         Row r;
         if constexpr (WIDE) {
             const uint32_t off = (w.v[j >> 2] == (uint64_t)zero_row() ? 0 : (g * 4 + (j & 3)) * row_bytes) + c * (D / 8);
-            r = *(GlobalRow)((Global)w.v[j >> 2] + off);
+            r = __builtin_nontemporal_load((GlobalRow)((Global)w.v[j >> 2] + off));
         } else {
             r = load_global<Row>(from_lane(w.v[0], (j >> 2) * 16 + g * 4 + (j & 3)) + c * (D / 8));
         }
@@ -499,25 +499,32 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
     }
 }
 
-// The weights of these sequences' slots from the scores and the rows' final statistics: a wave
-// for half a unit, its rows in order.
+// The weights of these sequences' slots from the scores and the rows' final statistics: a wave for a unit, two
+// slots a lane, the rows in order.
 __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan) {
     const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
-    const int64_t half = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), unit = half >> 1;
-    if (unit >= plan.score_units || unit >= plan.first_unit[p.kv.seqs] * hk) return;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= plan.score_units) return;
     const int4 x = plan.units[unit];
-    const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + (int)(half & 1) * 64 + lane;
-    const int page = table_entry(p.kv, table_of(p.kv, x.x, zero_row()), j);
-    const float* sc = plan.scores + unit * plan.rows * kUnit + (half & 1) * 64 + lane;
-    float sum = 0.f;
+    if (unit >= plan.first_unit[p.kv.seqs] * hk) return;
+    const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + 2 * lane;
+    const Table table = table_of(p.kv, x.x, zero_row());
+    const int page[2] = {table_entry(p.kv, table, j), table_entry(p.kv, table, j + 1)};
+    const float2* sc = (const float2*)(plan.scores + unit * plan.rows * kUnit) + lane;
+    float2 sum = {0.f, 0.f};
+#pragma unroll 4
     for (int r = 0; r < rows; r++) {
         const int t = r / G;
         const float lse = p.lse[x.y + t * p.heads + r - t * G] * 1.4426950408889634f;
-        if (lse != -INFINITY) sum += exp2_fast(sc[r * kUnit] - lse);
+        const float2 y = sc[r * (kUnit / 2)];
+        const float ref = lse == -INFINITY ? INFINITY : lse;  // a row that saw nothing adds nothing
+        sum.x += exp2_fast(y.x - ref);
+        sum.y += exp2_fast(y.y - ref);
     }
     // a slot that is not there has scores of -inf only
-    const int row = entry_row(p.kv, page, j, sum != 0.f);
-    if (row >= 0) p.kv.weight[stat_index(p.kv, row, head)] += sum;
+    const int row0 = entry_row(p.kv, page[0], j, sum.x != 0.f), row1 = entry_row(p.kv, page[1], j + 1, sum.y != 0.f);
+    if (row0 >= 0) p.kv.weight[stat_index(p.kv, row0, head)] += sum.x;
+    if (row1 >= 0) p.kv.weight[stat_index(p.kv, row1, head)] += sum.y;
 }
 
 template <class E, int D, bool WIDE>
@@ -549,7 +556,7 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.add_weight && plan.score_units > 0) k_weight_rows<<<(unsigned)((plan.score_units + 1) / 2), 256, 0, s>>>(a, plan);
+    if (a.add_weight && plan.score_units > 0) k_weight_rows<<<(unsigned)((plan.score_units + 3) / 4), 256, 0, s>>>(a, plan);
     return hipGetLastError();
 }
 
