@@ -181,7 +181,7 @@ int64_t svf_kv_attend_workspace(const svf_kv_cache *cache, const svf_kv_batch *b
  * value, weight and position.  Slots at or above the budget keep what they
  * held.  Each page at most once in the batch.
  *   next_position  int32 [num_seqs]: the position that the next token will have
- *   new_len        int32 [num_seqs]: min(kv_len, budget); may be kv_len itself
+ *   new_len        int32 [num_seqs]: min(kv_len, budget); not kv_len itself
  *   workspace      svf_kv_evict_workspace bytes, 256-byte aligned
  * Of the batch, q_offsets, num_tokens and max_q are not read.
  */

@@ -224,6 +224,7 @@ int svf_kv_evict(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_evic
     if (c->num_pages > 0 && (!c->weight || !c->position))
         return fail(SVF_EINVAL, "eviction needs the cache's weight and position");
     if (!a->next_position || !a->new_len) return fail(SVF_EINVAL, "next_position and new_len must not be NULL");
+    if (a->new_len == b->kv_len) return fail(SVF_EINVAL, "new_len must not be kv_len");
     const int64_t need = evict_bytes(c, b, a);
     if (a->workspace_bytes < need || !a->workspace || !aligned(a->workspace, 256))
         return fail(SVF_EINVAL, "workspace must have %lld bytes, aligned to 256", (long long)need);

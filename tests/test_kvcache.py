@@ -453,6 +453,12 @@ def test_evict_more_slots_than_are_held_in_lds():
     check_evict(s, 500, 64, 4, torch.tensor(lens, dtype=torch.int32))
 
 
+@pytest.mark.parametrize("lens,budget", [([5000, 4960, 4000], 4950), ([5000, 100], 2000), ([4096], 3000), ([4097], 4000)])
+def test_evict_either_way_of_moving_and_of_holding_keys(lens, budget):
+    s = evict_state(35, lens, 2, 64, 64)
+    check_evict(s, budget, 32, 4, torch.tensor(lens, dtype=torch.int32))
+
+
 def test_evict_again_and_again():
     """Lengths handed back, tokens appended in between by hand: what a program does over many steps."""
     lens = [90, 64]

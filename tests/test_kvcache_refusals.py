@@ -40,7 +40,7 @@ def attend(**kw):
 
 
 def evict(**kw):
-    f = dict(next=A, new_len=A, workspace=A, workspace_bytes=1 << 40, budget=32, recent=8, first=4)
+    f = dict(next=A, new_len=2 * A, workspace=A, workspace_bytes=1 << 40, budget=32, recent=8, first=4)
     f.update(kw)
     return C._EVICT.pack(*f.values())
 
@@ -101,7 +101,7 @@ def test_attend_needs_weights_and_workspace():
 
 @pytest.mark.parametrize("kw,text", [
     (dict(budget=0), "budget"), (dict(recent=-1), "budget"), (dict(first=25), "budget"), (dict(next=0), "NULL"),
-    (dict(new_len=0), "NULL"), (dict(workspace=0), "workspace"), (dict(workspace_bytes=8), "workspace"),
+    (dict(new_len=0), "NULL"), (dict(new_len=A), "must not be kv_len"), (dict(workspace=0), "workspace"), (dict(workspace_bytes=8), "workspace"),
 ])
 def test_evict_refuses(kw, text):
     assert S.load().svf_kv_evict(cache(), batch(), evict(**kw), None) == -1
