@@ -428,23 +428,39 @@ __device__ inline int seq_of_unit(const AttendArgs& p, const RowsPlan& plan, int
 }
 
 // The parts of the rows that were split over workgroups, in the order of their units.  One workgroup for
-// each boundary between two workgroups' runs: it does its work if the boundary is the first inside a key head's
-// units.  ``parts`` groups of 32 lanes share a row's parts.
+// each key head, or for each boundary between two workgroups' runs: then it does its work if the
+// boundary is the first inside a key head's units.  ``parts`` groups of 32 lanes share a row's parts.
 template <class E, int D>
-__global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, int parts) {
+__global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, int parts, bool by_head) {
     constexpr int VD = D / 32;
     const int hk = p.kv.kv_heads, G = p.heads / hk;
     const int64_t all = plan.first_unit[p.kv.seqs] * hk, groups = min((int64_t)plan.groups, all);
-    const int64_t w = (int64_t)blockIdx.x + 1;
-    if (w >= groups) return;
-    const int64_t cut = all * w / groups;
-    const int seq = seq_of_unit(p, plan, cut);
-    const int64_t first = plan.first_unit[seq], units = plan.first_unit[seq + 1] - first;
-    const int64_t rel = cut - first * hk;
-    const int head = (int)(rel / units);
-    const int64_t s0 = first * hk + head * units, s1 = s0 + units;
-    const int64_t w0 = w - 1;  // the workgroup that has the first unit
-    if (cut == s0 || all * w0 / groups > s0) return;
+    int seq, head;
+    int64_t units, s0, w0;  // the key head's units, its first and the workgroup that has it
+    if (by_head) {
+        seq = blockIdx.x / hk;
+        head = blockIdx.x - seq * hk;
+        const int64_t first = plan.first_unit[seq];
+        units = plan.first_unit[seq + 1] - first;
+        if (units < 2) return;
+        s0 = first * hk + head * units;
+        w0 = s0 * groups / all;
+        while (all * (w0 + 1) / groups <= s0) w0++;
+        while (all * w0 / groups > s0) w0--;
+        if (all * (w0 + 1) / groups >= s0 + units) return;
+    } else {
+        const int64_t w = (int64_t)blockIdx.x + 1;
+        if (w >= groups) return;
+        const int64_t cut = all * w / groups;
+        seq = seq_of_unit(p, plan, cut);
+        const int64_t first = plan.first_unit[seq];
+        units = plan.first_unit[seq + 1] - first;
+        head = (int)((cut - first * hk) / units);
+        s0 = first * hk + head * units;
+        w0 = w - 1;
+        if (cut == s0 || all * w0 / groups > s0) return;
+    }
+    const int64_t s1 = s0 + units;
     int64_t w1 = (s1 - 1) * groups / all;  // and the one that has the last
     while (all * (w1 + 1) / groups <= s1 - 1) w1++;
     while (all * w1 / groups > s1 - 1) w1--;
@@ -459,15 +475,34 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
 #pragma unroll
         for (int j = 0; j < VD; j++) acc[j] = 0.f;
         if (row < rows) {
-#pragma unroll 4
-            for (int64_t x = w0 + sub; x <= w1; x += parts) {
-                const float* q = plan.part + (2 * x + (x == w0 ? 1 : 0)) * stride;
-                const float pm = q[plan.rows * D + 2 * row], pl = q[plan.rows * D + 2 * row + 1];
-                const float now = fmaxf(top, pm), ref = now == -INFINITY ? 0.f : now;
-                const float keep = exp2_fast(top - ref), f = exp2_fast(pm - ref);
-                den = den * keep + pl * f;
+            // eight parts at a time, all their loads before the first is used
+            for (int64_t x0 = w0 + sub; x0 <= w1; x0 += 8 * parts) {
+                float pm[8], pl[8], pv[8][VD];
 #pragma unroll
-                for (int j = 0; j < VD; j++) acc[j] = acc[j] * keep + q[row * D + d0 + j] * f;
+                for (int i = 0; i < 8; i++) {
+                    const int64_t x = min(x0 + i * parts, w1);
+                    const float* q = plan.part + (2 * x + (x == w0 ? 1 : 0)) * stride;
+                    pm[i] = x0 + i * parts <= w1 ? q[plan.rows * D + 2 * row] : -INFINITY;
+                    pl[i] = q[plan.rows * D + 2 * row + 1];
+#pragma unroll
+                    for (int j = 0; j < VD; j++) pv[i][j] = q[row * D + d0 + j];
+                }
+                float now = top;
+#pragma unroll
+                for (int i = 0; i < 8; i++) now = fmaxf(now, pm[i]);
+                const float ref = now == -INFINITY ? 0.f : now, keep = exp2_fast(top - ref);
+                den *= keep;
+#pragma unroll
+                for (int j = 0; j < VD; j++) acc[j] *= keep;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    // a part that saw nothing, or is none, is left out, whatever it holds
+                    const float f = exp2_fast(pm[i] - ref);
+                    if (pm[i] == -INFINITY) continue;
+                    den += pl[i] * f;
+#pragma unroll
+                    for (int j = 0; j < VD; j++) acc[j] += pv[i][j] * f;
+                }
                 top = now;
             }
         }
@@ -552,7 +587,9 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
         const bool many = plan.groups >= 8 * (int64_t)a.kv.seqs * a.kv.kv_heads;
         int parts = 8;
         while (!many && parts > 1 && 8 / parts < plan.rows) parts >>= 1;
-        k_join_rows<E, D><<<dim3(plan.groups - 1, many ? plan.rows : 1), 256, 0, s>>>(a, plan, parts);
+const int64_t heads = (int64_t)a.kv.seqs * a.kv.kv_heads;
+        const bool by_head = heads < plan.groups - 1;
+        k_join_rows<E, D><<<dim3((unsigned)(by_head ? heads : plan.groups - 1), many ? plan.rows : 1), 256, 0, s>>>(a, plan, parts, by_head);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -572,7 +609,10 @@ Layout layout(const AttendSizes& z) {
     const int64_t cap = (int64_t)z.width * z.page_size;
     const int64_t most = (int64_t)z.seqs * z.kv_heads * ((cap + kUnit - 1) / kUnit > 0 ? (cap + kUnit - 1) / kUnit : 1);
     y.rows = few_rows(z);
-    y.groups = 256 * waves_per_simd(z.dim, y.rows <= 16 ? 1 : 2);  // what the GPU holds at a time
+    // What the GPU holds at a time, but eight units each where that still is one for every CU: the fewer parts a row has,
+    // the less there is to join (65,535 slots of one sequence: 512 workgroups 38 us, 256 34).
+    y.groups = 256 * waves_per_simd(z.dim, y.rows <= 16 ? 1 : 2);
+    if (most / 8 < y.groups) y.groups = (int32_t)(most / 8 > 256 ? most / 8 : 256);
     if (most < y.groups) y.groups = (int32_t)most;
     y.part = round256((int64_t)(z.seqs + 1) * 8);
     y.scores = y.part + round256((int64_t)2 * y.groups * y.rows * (z.dim + 4) * 4);
