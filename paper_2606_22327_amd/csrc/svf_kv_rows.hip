@@ -637,6 +637,8 @@ int32_t few_rows(const AttendSizes& z) {
     const int64_t want = (int64_t)z.max_q * G;
     if (want <= most) return (int32_t)(want < 1 ? 1 : want);
     const int32_t single = G > 16 ? G : 16;
+    // None, where every sequence must have more: what the others can leave of the tokens.
+    if (((int64_t)z.tokens - (int64_t)(z.seqs - 1) * z.max_q) * G > single) return 0;
     return single <= most ? single : 0;
 }
 
