@@ -23,7 +23,7 @@
  *     and may be recorded into a graph.  The current device must be the
  *     stream's.
  *   - Sizes, strides, alignment and flags are checked on the host before
- *     anything is enqueued (SVF_EINVAL, text from svf_last_error).  What lies in
+ *     anything is enqueued (SVF_EINVAL, text from svf_kv_last_error).  What lies in
  *     device memory cannot be: there, lengths are cut to [0, table_width *
  *     page_size], offsets to [0, num_tokens], and a slot whose page number is outside
  *     [0, num_pages) is not there (never written, invisible to attention,
@@ -168,6 +168,9 @@ int svf_kv_attend(const svf_kv_cache *cache, const svf_kv_batch *batch,
  * and add_weight are read); negative: the code of an error. */
 int64_t svf_kv_attend_workspace(const svf_kv_cache *cache, const svf_kv_batch *batch,
                                 const svf_kv_attend_args *args);
+
+/* Text of the calling thread's last error in one of these calls. */
+const char *svf_kv_last_error(void);
 
 /*
  * Shrink every sequence of more than ``budget`` slots to ``budget``, each key

@@ -7,9 +7,6 @@
 
 namespace svfk {
 
-// Set the text of the calling thread's last error; returns ``code``.
-int report(int code, const char* text);
-
 enum { POLICY_FCFS = 0, POLICY_SJF = 1, POLICY_SVF = 2, POLICY_SVF1BIT = 3 };
 enum { ADMIT_CURRENT = 0x100 };  // added to a policy code: next-step admission
 enum { STATUS_DONE = 0, STATUS_EXHAUSTED = 1, STATUS_RUNNING = 2 };

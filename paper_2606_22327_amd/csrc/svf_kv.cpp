@@ -12,14 +12,16 @@ using namespace svfk;
 
 namespace {
 
+// message of the calling thread's last failure
+thread_local char g_err[256];
+
 int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 int fail(int code, const char* fmt, ...) {
-    char text[256];
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(text, sizeof text, fmt, ap);
+    vsnprintf(g_err, sizeof g_err, fmt, ap);
     va_end(ap);
-    return report(code, text);
+    return code;
 }
 
 constexpr int64_t kLimit31 = int64_t(1) << 31;
@@ -128,6 +130,8 @@ int64_t evict_bytes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_e
 }  // namespace
 
 extern "C" {
+
+const char* svf_kv_last_error(void) { return g_err; }
 
 int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_append_args* a, void* hip_stream) {
     if (int rc = check_sizes(c, b)) return rc;

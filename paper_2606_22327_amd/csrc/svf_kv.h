@@ -9,9 +9,6 @@
 
 namespace svfk {
 
-// The text of the calling thread's last error; returns ``code`` (svf_runtime.cpp).
-int report(int code, const char* text);
-
 // A layer's cache and a call's sequences as the kernels see them.
 struct KvView {
     const char* k;

@@ -56,15 +56,6 @@ struct Timed {
 
 }  // namespace
 
-namespace svfk {
-
-// Last error of the calling thread, for the library's other host sources.
-int report(int code, const char* text) {
-    return fail(code, "%s", text);
-}
-
-}  // namespace svfk
-
 struct svf_batch {
     hipStream_t stream = nullptr;
     // Second stream (default priority) on which the per-step segments run

@@ -68,8 +68,13 @@ def _need(ok: bool, text: str):
         raise svfsim.SvfError(-1, text)
 
 
-def _ptr(t: Optional[torch.Tensor]) -> int:
-    return 0 if t is None else t.data_ptr()
+def last_error() -> str:
+    return svfsim.load().svf_kv_last_error().decode(errors="replace")
+
+
+def _check(rc: int):
+    if rc != 0:
+        raise svfsim.SvfError(rc, last_error())
 
 
 # A step is some microseconds on the GPU, so the checks are one expression each
@@ -159,7 +164,7 @@ def _call(fn, dev: int, *packed: bytes):
         with torch.cuda.device(dev):
             rc = fn(*packed, _raw_stream(dev))
     if rc != 0:
-        svfsim._check(rc)
+        _check(rc)
 
 
 def _raw_stream(dev: int) -> int:
@@ -172,7 +177,7 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream"):      # the same handle withou
 
 def _workspace(n: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     if n < 0:
-        svfsim._check(int(n))
+        _check(int(n))
     return like.new_empty(n, dtype=torch.uint8) if n else None
 
 

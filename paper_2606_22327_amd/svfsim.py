@@ -39,7 +39,7 @@ EXPORTS = ("svf_create", "svf_reset", "svf_step", "svf_run", "svf_read", "svf_st
            "svf_set_profiling", "svf_timings", "svf_shape", "svf_destroy",
            "svf_last_error", "svf_abi_version", "svf_opt_burst", "svf_opt_burst_batch",
            "svf_run_noalloc", "svf_kv_append", "svf_kv_attend", "svf_kv_attend_workspace",
-           "svf_kv_evict", "svf_kv_evict_workspace")
+           "svf_kv_evict", "svf_kv_evict_workspace", "svf_kv_last_error")
 
 
 class SvfError(RuntimeError):
@@ -123,8 +123,10 @@ def load(path: str = LIB_PATH):
     lib.svf_run_noalloc.argtypes = [ctypes.POINTER(BatchDesc), V, V, V, V, V, V]
     for name in ("svf_kv_append", "svf_kv_attend", "svf_kv_evict"):
         getattr(lib, name).argtypes = [V, V, V, V]
+    lib.svf_kv_last_error.argtypes = []
+    lib.svf_kv_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("svf_last_error",):
+        if name not in ("svf_last_error", "svf_kv_last_error"):
             getattr(lib, name).restype = ctypes.c_int
     for name in ("svf_kv_attend_workspace", "svf_kv_evict_workspace"):
         getattr(lib, name).argtypes = [V, V, V]

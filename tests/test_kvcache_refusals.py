@@ -59,13 +59,13 @@ def test_cache_and_batch_are_checked_by_every_call(fn, args):
     call = getattr(S.load(), fn)
     for kw, text in CACHE_BAD:
         assert call(cache(**kw), batch(), args(), None) == -1, kw
-        assert text in S.last_error(), (kw, S.last_error())
+        assert text in C.last_error(), (kw, C.last_error())
     for kw, text in BATCH_BAD:
         assert call(cache(), batch(**kw), args(), None) == -1, kw
-        assert text in S.last_error(), (kw, S.last_error())
+        assert text in C.last_error(), (kw, C.last_error())
     for bad in ((None, batch(), args()), (cache(), None, args()), (cache(), batch(), None)):
         assert call(*bad, None) == -1
-        assert "NULL" in S.last_error()
+        assert "NULL" in C.last_error()
 
 
 @pytest.mark.parametrize("kw,text", [
@@ -75,7 +75,7 @@ def test_cache_and_batch_are_checked_by_every_call(fn, args):
 ])
 def test_append_refuses(kw, text):
     assert S.load().svf_kv_append(cache(), batch(), append(**kw), None) == -1
-    assert text in S.last_error()
+    assert text in C.last_error()
 
 
 @pytest.mark.parametrize("kw,text", [
@@ -84,17 +84,17 @@ def test_append_refuses(kw, text):
 ])
 def test_attend_refuses(kw, text):
     assert S.load().svf_kv_attend(cache(), batch(), attend(**kw), None) == -1
-    assert text in S.last_error()
+    assert text in C.last_error()
 
 
 def test_attend_needs_weights_and_workspace():
     lib = S.load()
-    assert lib.svf_kv_attend(cache(weight=0), batch(), attend(add_weight=1), None) == -1 and "weight" in S.last_error()
+    assert lib.svf_kv_attend(cache(weight=0), batch(), attend(add_weight=1), None) == -1 and "weight" in C.last_error()
     need = lib.svf_kv_attend_workspace(cache(), batch(), attend(add_weight=1))
     assert need >= 0
     if need:
         assert lib.svf_kv_attend(cache(), batch(), attend(add_weight=1, workspace_bytes=need - 1), None) == -1
-        assert "workspace" in S.last_error()
+        assert "workspace" in C.last_error()
         assert lib.svf_kv_attend(cache(), batch(), attend(add_weight=1, workspace=A + 16), None) == -1
     assert lib.svf_kv_attend_workspace(cache(head_dim=3), batch(), attend()) == -1
 
@@ -105,13 +105,13 @@ def test_attend_needs_weights_and_workspace():
 ])
 def test_evict_refuses(kw, text):
     assert S.load().svf_kv_evict(cache(), batch(), evict(**kw), None) == -1
-    assert text in S.last_error()
+    assert text in C.last_error()
 
 
 def test_evict_needs_weight_and_position():
     lib = S.load()
-    assert lib.svf_kv_evict(cache(weight=0), batch(), evict(), None) == -1 and "weight" in S.last_error()
-    assert lib.svf_kv_evict(cache(position=0), batch(), evict(), None) == -1 and "position" in S.last_error()
+    assert lib.svf_kv_evict(cache(weight=0), batch(), evict(), None) == -1 and "weight" in C.last_error()
+    assert lib.svf_kv_evict(cache(position=0), batch(), evict(), None) == -1 and "position" in C.last_error()
     # room for min(budget, slots over it) pairs of each key head
     assert lib.svf_kv_evict_workspace(cache(), batch(), evict()) == 256 + 4 * 32 * 8
     assert lib.svf_kv_evict_workspace(cache(), batch(), evict(budget=60)) == 256 + 4 * 4 * 8
