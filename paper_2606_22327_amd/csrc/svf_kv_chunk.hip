@@ -93,6 +93,14 @@ __device__ inline int swizzle(int row) {
 // scores of a lane are, in order, the second product's operand for the slots 16 s + 4 h + {0..3, 8..11}
 // (h the half), and the values of those slots come transposed out of LDS, four slots a read.
 // Keys and values go from memory straight to LDS, the next tile's while this one is worked on.
+//
+// The probabilities are rounded to the inputs' type for the second product, once, their sum is not: an error of
+// the size of the output's own rounding.  A row's maximum is followed only when it has grown by more than kSlack.
+//
+// The products bound it: 2,048 tokens behind 12,001 (32 query heads on 8 key heads of 128 dimensions, 437 GFLOP) take
+// 460 us, 950 TFLOP/s where a large product of the library reaches 1,350; six prompts of 1,084 to 3,930 tokens 400 us,
+// 870 TFLOP/s.  Of a tile's time about a tenth goes to its loads' latency, the rest of what is missing to exponentials and
+// the waits between the two products, which two waves a SIMD do not fill.
 // WIDE: pages of 16 slots or more, so that the sixteen slots that a wave fetches lie in one page: their address is the same for
 // the whole wave but for an offset that stays the same all along (a tile costs a wave 8 loads and some scalar
 // instructions, and 100 vector instructions otherwise).
@@ -449,7 +457,8 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // The weights of these sequences' slots: scores once more, now against the rows' final statistics.
 // A workgroup has 256 slots, 64 for each wave, whose keys stay in registers while the rows'
 // queries pass through LDS, 64 at a time; a lane sums its own rows for 32 slots and the lanes
-// are added at the end, so nothing is added atomically.  The exponentials bound it.
+// are added at the end, so nothing is added atomically.  The exponentials bound it: 2,048 tokens over 14,049 slots
+// of 8 key heads (32 query heads, 218 GFLOP, 8.5e8 exponentials) take 350 us.
 constexpr int kWSlots = 256, kWRows = 64;
 
 __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
