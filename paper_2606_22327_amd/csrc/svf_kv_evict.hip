@@ -232,18 +232,18 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     int* counts = (int*)a.ws;
     int2* pairs = (int2*)(a.ws + (((int64_t)segs * 4 + 255) & ~int64_t(255)));
     // Up to 4,096 slots four workgroups of a CU side by side (64 prompts of 1,033 to 4,068 slots: 256 threads each 103 us,
-    // 512 threads 95, 1,024 threads 99); longer ones one, with up to 30,720 keys in 120 KB of its LDS.
+    // 512 threads 95, 1,024 threads 99); longer ones one, with up to 28,672 keys in 112 KB of its LDS.
     if (pairs_max <= kOwnPairs) {
         if (cap <= 4096)
             k_evict_select<512, 4096, true><<<segs, 512, 0, s>>>(a, pairs_max, pairs, counts);
         else
-            k_evict_select<1024, 30720, true><<<segs, 1024, 0, s>>>(a, pairs_max, pairs, counts);
+            k_evict_select<1024, 28672, true><<<segs, 1024, 0, s>>>(a, pairs_max, pairs, counts);
         return hipGetLastError();
     }
     if (cap <= 4096)
         k_evict_select<512, 4096, false><<<segs, 512, 0, s>>>(a, pairs_max, pairs, counts);
     else
-        k_evict_select<1024, 30720, false><<<segs, 1024, 0, s>>>(a, pairs_max, pairs, counts);
+        k_evict_select<1024, 28672, false><<<segs, 1024, 0, s>>>(a, pairs_max, pairs, counts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t blocks = (pairs_max + kMoveRows - 1) / kMoveRows;

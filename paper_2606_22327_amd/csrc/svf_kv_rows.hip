@@ -505,9 +505,8 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
                 for (int j = 0; j < VD; j++) acc[j] *= keep;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    // a part that saw nothing, or is none, is left out, whatever it holds
+                    if (x0 + i * parts > w1) continue;
                     const float f = exp2_fast(pm[i] - ref);
-                    if (pm[i] == -INFINITY) continue;
                     den += pl[i] * f;
 #pragma unroll
                     for (int j = 0; j < VD; j++) acc[j] += pv[i][j] * f;

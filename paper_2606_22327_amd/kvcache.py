@@ -273,7 +273,7 @@ def evict(batch: Batch, cache: Cache, budget: int, recent: int, next_position: t
     lib = svfsim.load()
     need = lib.svf_kv_evict_workspace(kv, seqs, _EVICT.pack(0, 0, 0, 0, *fixed))
     ws = _workspace(need, k)
-    a = _EVICT.pack(next_position.data_ptr(), new_len.data_ptr(), ws.data_ptr(), need, *fixed)
+    a = _EVICT.pack(next_position.data_ptr(), new_len.data_ptr(), ws.data_ptr() if need else 0, need, *fixed)
     _call(lib.svf_kv_evict, k.get_device(), kv, seqs, a)
     return new_len
 

@@ -235,6 +235,16 @@ def test_attend_few_row_tiles_are_split(dtype, heads, kv_heads, dim, causal, win
     assert torch.equal(out, a[0]) and torch.equal(lse, a[1]) and torch.equal(w, a[2])
 
 
+@pytest.mark.parametrize("new", [1, 60])
+def test_attend_parts_of_scores_that_are_not_numbers(new):
+    # every key of some units and tiles, so that a part of a split row has no other scores
+    s = make(21, [3000], [new], 4, 1, 128, 16, BF)
+    pg, row = P.slots_of(s["table"], 0, 3000, 16, s["k"].shape[0])
+    s["k"][pg[1024:1536], 0, row[1024:1536]] = float("nan")
+    out, lse, _ = check_attend(s)
+    assert out.isnan().all() and lse.isnan().all()
+
+
 def test_attend_split_tiles_and_values_that_are_not_numbers():
     s = make(19, [2000], [60], 4, 1, 128, 16, BF)
     pg, row = P.slots_of(s["table"], 0, 2000, 16, s["k"].shape[0])
@@ -269,6 +279,23 @@ def test_attend_no_tokens_and_no_sequences():
     b = C.Batch(torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"),
                 torch.zeros((0, 4), dtype=torch.int32, device="cuda"), 1)
     C.attend(s["q"].cuda(), b, C.Cache(s["k"].cuda(), s["v"].cuda()))
+
+
+def test_no_sequences_and_tables_without_a_page():
+    from paper_2606_22327_amd import kvcache as C
+    s = make(22, [30], [3], 8, 2, 128, 16, BF, stats=True)
+    ints = dict(dtype=torch.int32, device="cuda")
+    cache = C.Cache(*(s[n].cuda() for n in ("k", "v", "weight", "position")))
+    none = C.Batch(None, torch.zeros(0, **ints), torch.zeros((0, 4), **ints), 0)
+    assert C.evict(none, cache, 8, 0, torch.zeros(0, **ints)).shape == (0,)
+    # lengths are cut to what the table has: nothing
+    b = C.Batch(torch.tensor([0, 1, 3], **ints), torch.tensor([5, 9], **ints), torch.zeros((2, 0), **ints), 2)
+    out, lse = C.attend(s["q"].cuda(), b, cache, add_weight=True)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    assert C.evict(b, cache, 4, 0, torch.tensor([5, 9], **ints)).tolist() == [0, 0]
+    C.append(s["q"].cuda(), s["q"].cuda()[:, :2], s["q"].cuda()[:, :2], torch.zeros(3, **ints), None, b, cache)
+    for x, n in zip(cache, ("k", "v", "weight", "position")):
+        assert torch.equal(torch.nan_to_num(x.cpu().float()), torch.nan_to_num(s[n].float()))
 
 
 # -- append --------------------------------------------------------------------
