@@ -144,8 +144,8 @@ int svf_kv_append(const svf_kv_cache *cache, const svf_kv_batch *batch,
  *               the query heads of its key head (in an order that is the same
  *               every time).  Each page at most once in the batch then.
  *   q           [num_tokens][heads][head_dim], as in svf_kv_append
- *   out         the same, contiguous heads not required; 16-byte aligned,
- *               strides multiples of 8
+ *   out         the same, contiguous heads not required, apart from q; 16-byte
+ *               aligned, strides multiples of 8
  *   lse         float [num_tokens][heads]
  *   workspace   svf_kv_attend_workspace bytes, 256-byte aligned, nothing kept in it
  */

@@ -210,7 +210,8 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     k.scale = a->scale * 1.4426950408889634f;
     k.heads = a->heads;
     k.causal = a->causal != 0;
-    k.window = a->window;
+    // a window as wide as the table hides nothing, and a slot less than it is still an int
+    k.window = a->window < (int64_t)b->table_width * c->page_size ? a->window : 0;
     k.add_weight = a->add_weight != 0;
     k.q_wide = aligned(a->q, 16) && a->q_token_stride % 8 == 0 && a->q_head_stride % 8 == 0;
     return launched(launch_attend(k, sizes(c, b, a), static_cast<hipStream_t>(hip_stream)));

@@ -116,6 +116,15 @@ def test_attend_rows_without_a_slot():
     check_attend(s, causal=False, add_weight=True)
 
 
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 6, 64, 63])
+def test_attend_widest_windows(window):
+    # as wide as the numbers go, and as the table: with more new tokens than slots among them
+    s = make(24, [3, 0, 60, 64], [10, 4, 2, 64], 8, 2, 128, 16, BF, stats=True)
+    check_attend(s, window=window, add_weight=True)
+    s = make(25, [3, 0, 60, 64], [10, 4, 2, 1], 4, 2, 128, 16, BF, stats=True)
+    check_attend(s, window=window, add_weight=True)
+
+
 @pytest.mark.parametrize("new", [1, 2, 24, 90])
 @pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
 def test_attend_missing_pages_and_garbage(new, what):
