@@ -467,20 +467,14 @@ __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
 }
 
 template <class E, int D>
-__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(AttendArgs p) {
+__device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, int tile, int head) {
     using T = typename E::T;
     using V8 = typename E::V8;
     constexpr int KS = D / 16, CH = D / 8, PER = kWRows * CH / 256;
     __shared__ __align__(16) char lds[2][kWRows * D * 2];
     __shared__ float stat[2][kWRows];
-    __shared__ int64_t scan[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
-    const int G = p.heads / p.kv.kv_heads, hk = p.kv.kv_heads, head = blockIdx.x % hk;
-    int seq, tile;
-    if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles(p, s); }, scan,
-                   seq, tile))
-        return;
-    const Seq s = seq_of(p.kv, seq);
+    const int G = p.heads / p.kv.kv_heads;
     const int r0 = s.len - s.n;
     const int j0 = first_slot(p, s) + tile * kWSlots, j1 = min(j0 + kWSlots, s.len);
     // rows that see one of the slots: tokens t0 .. t1 - 1
@@ -623,6 +617,37 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
         }
 }
 
+// One tile a workgroup, of as many as the pool has slots for.
+template <class E, int D>
+__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(AttendArgs p) {
+    __shared__ int64_t scan[4];
+    const int hk = p.kv.kv_heads;
+    int seq, tile;
+    if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles(p, s); }, scan,
+                   seq, tile))
+        return;
+    weigh_slots<E, D>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
+}
+
+// Sequences with slots that have no page can have more tiles than that: those from ``first`` on, in a loop (a kernel of its own,
+// since the loop around it makes the one above spill registers).
+template <class E, int D>
+__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk_more(AttendArgs p, int64_t first) {
+    __shared__ int64_t scan[4];
+    const int hk = p.kv.kv_heads;
+    const int64_t begin = first + blockIdx.x / hk;
+    int64_t total = 0;
+    for (int64_t at = begin; at == begin || at < total; at += gridDim.x / hk) {
+        auto place = [&](int64_t all) {
+            total = all;
+            return at;
+        };
+        int seq, tile;
+        if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles(p, s); }, scan, seq, tile)) return;
+        weigh_slots<E, D>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
+    }
+}
+
 // Row tiles at least: those of the rows that sequences of few rows cannot have. With more than half as many as the
 // GPU holds workgroups none is split.
 int32_t split_groups(const AttendSizes& z, int32_t few) {
@@ -664,11 +689,14 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         if (e != hipSuccess) return e;
     }
     if (a.add_weight) {
-        // slot tiles at most: each page is in the batch once
+        // slot tiles at most, and where every slot has a page: each page is in the batch once
         const int64_t cap = (int64_t)z.width * z.page_size, most = seqs < z.seqs ? seqs : z.seqs;
-        int64_t tiles = (int64_t)z.num_pages * z.page_size / kWSlots + most;
-        if (tiles > most * ((cap + kWSlots - 1) / kWSlots)) tiles = most * ((cap + kWSlots - 1) / kWSlots);
+        const int64_t all = most * ((cap + kWSlots - 1) / kWSlots), pool = (int64_t)z.num_pages * z.page_size / kWSlots + most;
+        const int64_t tiles = all < pool ? all : pool, more = all - tiles < 64 ? all - tiles : 64;
         if (tiles > 0) k_weight_chunk<E, D><<<(unsigned)(tiles * z.kv_heads), 256, 0, s>>>(a);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (more > 0) k_weight_chunk_more<E, D><<<(unsigned)(more * z.kv_heads), 256, 0, s>>>(a, tiles);
     }
     return hipGetLastError();
 }

@@ -542,18 +542,51 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
     }
 }
 
+// The weights of a unit whose scores were not kept: they are formed again, two slots a lane. Right, not fast.
+template <class E, int D>
+__device__ void weigh_again(const AttendArgs& p, const RowsPlan& plan, int64_t unit) {
+    using T = typename E::T;
+    const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
+    const int seq = seq_of_unit(p, plan, unit);
+    const int64_t first = plan.first_unit[seq], units = plan.first_unit[seq + 1] - first, rel = unit - first * hk;
+    const int head = (int)(rel / units), u = (int)(rel - head * units);
+    const Seq s = seq_of(p.kv, seq);
+    if (s.n > p.kv.max_q) return;
+    const int r0 = s.len - s.n;
+    for (int x = 0; x < 2; x++) {
+        const int j = first_slot(p, s) + u * kUnit + 2 * lane + x;
+        const int at = j < s.len ? pool_row(p.kv, seq, j) : -1;
+        if (at < 0) continue;
+        const T* k = (const T*)(p.kv.k + head * p.kv.k_head + row_offset(at, p.kv.shift, p.kv.k_page, p.kv.k_row));
+        float sum = 0.f;
+        for (int r = 0; r < s.n * G; r++) {
+            const int t = r / G, h = head * G + r - t * G;
+            if ((p.causal && j > r0 + t) || (p.window > 0 && j <= r0 + t - p.window)) continue;
+            const T* q = (const T*)(p.q + (s.q0 + t) * p.q_tok + h * p.q_head);
+            float dot = 0.f;
+#pragma unroll 8
+            for (int d = 0; d < D; d++) dot = fmaf((float)q[d], (float)k[d], dot);
+            const float lse = p.lse[(int64_t)(s.q0 + t) * p.heads + h] * 1.4426950408889634f;
+            sum += exp2_fast(dot * p.scale - (lse == -INFINITY ? INFINITY : lse));
+        }
+        p.kv.weight[stat_index(p.kv, at, head)] += sum;
+    }
+}
+
 // The weights of these sequences' slots from the scores and the rows' final statistics: a wave for a unit, two
 // slots a lane, the rows in order. (256 sequences, 255,882 slots of 8 key heads: 15 us for 32 MB of scores and 16 MB of weights.)
+// There is room for the scores of as many slots as the pool has; sequences with slots that have no page can have more units.
+template <class E, int D>
 __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan) {
     const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= plan.score_units) return;
-    const int4 x = plan.units[unit];
-    if (unit >= plan.first_unit[p.kv.seqs] * hk) return;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = plan.first_unit[p.kv.seqs] * hk;
+    for (int64_t unit = plan.score_units + wave; unit < all; unit += (int64_t)gridDim.x * 4) weigh_again<E, D>(p, plan, unit);
+    if (wave >= min(all, plan.score_units)) return;
+    const int4 x = plan.units[wave];
     const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + 2 * lane;
     const Table table = table_of(p.kv, x.x, zero_row());
     const int page[2] = {table_entry(p.kv, table, j), table_entry(p.kv, table, j + 1)};
-    const float2* sc = (const float2*)(plan.scores + unit * plan.rows * kUnit) + lane;
+    const float2* sc = (const float2*)(plan.scores + wave * plan.rows * kUnit) + lane;
     float2 sum = {0.f, 0.f};
 #pragma unroll 4
     for (int r = 0; r < rows; r++) {
@@ -595,13 +628,13 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
         const bool many = plan.groups >= 8 * (int64_t)a.kv.seqs * a.kv.kv_heads;
         int parts = 8;
         while (!many && parts > 1 && 8 / parts < plan.rows) parts >>= 1;
-const int64_t heads = (int64_t)a.kv.seqs * a.kv.kv_heads;
+        const int64_t heads = (int64_t)a.kv.seqs * a.kv.kv_heads;
         const bool by_head = heads < plan.groups - 1;
         k_join_rows<E, D><<<dim3((unsigned)(by_head ? heads : plan.groups - 1), many ? plan.rows : 1), 256, 0, s>>>(a, plan, parts, by_head);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.add_weight && plan.score_units > 0) k_weight_rows<<<(unsigned)((plan.score_units + 3) / 4), 256, 0, s>>>(a, plan);
+    if (a.add_weight && plan.score_units > 0) k_weight_rows<E, D><<<(unsigned)((plan.score_units + 3) / 4), 256, 0, s>>>(a, plan);
     return hipGetLastError();
 }
 
@@ -624,7 +657,8 @@ Layout layout(const AttendSizes& z) {
     if (most < y.groups) y.groups = (int32_t)most;
     y.part = round256((int64_t)(z.seqs + 1) * 8);
     y.scores = y.part + round256((int64_t)2 * y.groups * y.rows * (z.dim + 4) * 4);
-    // every page once at most: the pool's slots, and a unit that is not full for each sequence
+    // every page once at most: the pool's slots, and a unit that is not full for each sequence (more where slots have no
+    // page: those units' scores are formed again)
     y.units = 0;
     if (z.add_weight) {
         y.units = ((int64_t)z.num_pages * z.page_size / kUnit + z.seqs) * z.kv_heads;

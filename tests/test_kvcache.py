@@ -138,6 +138,27 @@ def test_attend_missing_pages_and_garbage(new, what):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [2, 3, 1, 4], [40, 90, 1, 70]])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1500)])
+def test_attend_weights_where_most_slots_have_no_page(dtype, new, causal, window):
+    # a pool of far fewer slots than the sequences' lengths: the last sequences' slots count as the first's
+    lens = [1000, 2100, 500, 1400]
+    s = make(23, lens, new, 8, 2, 128, 16, dtype, stats=True)
+    keep = []
+    for i, n in enumerate(lens):
+        pages = -(-n // 16)
+        for x in range(pages):
+            if x in (1, pages // 2, pages - 1):
+                keep.append(int(s["table"][i, x]))
+                s["table"][i, x] = len(keep) - 1
+            else:
+                s["table"][i, x] = -1
+    for x in ("k", "v", "weight", "position"):
+        s[x] = s[x][keep].contiguous()
+    check_attend(s, causal=causal, window=window, add_weight=True)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("new,heads", [(2, 4), (4, 8), (8, 2), (40, 4), (100, 8)])
 @pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
 def test_attend_values_that_are_not_numbers_behind_the_mask(dtype, new, heads, what):
