@@ -1,5 +1,7 @@
 // svf_kv_chunk.hip -- attention over the paged cache of sequences with many rows
 // (new tokens times query heads of a key head): prompts and their pieces.
+#include <type_traits>
+
 #include "svf_kv_attend.h"
 
 namespace svfk {
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         koff[i] = (uint32_t)r * (uint32_t)p.kv.k_row + x;
         voff[i] = (uint32_t)r * (uint32_t)p.kv.v_row + x;
     }
-    auto look = [&](int it) {
+    auto look = [&](int it) __attribute__((always_inline)) {
         page_all = table_entry(p.kv, table, lo + it * kTile + lane);
         if constexpr (!WIDE) {
 #pragma unroll
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (Lds)to, 16, 0, 0);
     };
     uint64_t there, there_next;
-    auto fetch = [&](int it, char* kto, char* vto) {
+    auto fetch = [&](int it, char* kto, char* vto) __attribute__((always_inline)) {
         const int j0 = lo + it * kTile;
         there_next = __ballot((unsigned)page_all < (unsigned)p.kv.num_pages && j0 + lane < hi);
         kto += wave * NI * 1024;
@@ -252,7 +254,11 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     // Where the tile's rows do not all see the same slots, a value that is no finite number would reach those
     // that do not see it (0 times infinity): it counts as 0, and the rows that see it get it
     // from their marks.  Each wave looks through the values of sixteen slots.
-    auto clean = [&](char* vb, int base) {
+    // A tile whose slots all rows see is not looked through at first.  There such a value meets probabilities that have
+    // become 0, which makes no number of what is infinite; but it also leaves a sum that is no finite number, and
+    // then the row tile is worked through once more, with every tile looked through (``careful``; in a loop of its own: one loop
+    // for both spills registers where a head has 256 dimensions).
+    auto clean = [&](char* vb, int base) __attribute__((always_inline)) {
         u16x2 size = {0, 0};
         uint32_t* words = (uint32_t*)(vb + wave * 16 * D * 2) + lane;
         for (int x = 0; x < 8 * D; x += 64) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, words[x] & 0x7fff7fffu));
@@ -291,19 +297,9 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             asm volatile("" : "+v"(va[d][i]));
         }
 
-    float m = -INFINITY, l = 0.f;
+    float m, l;
     f32x16 o[DT];
-#pragma unroll
-    for (int d = 0; d < DT; d++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) o[d][i] = 0.f;
-
-    if (tiles > 0) {
-        look(0);
-        fetch(0, k0, v0);
-        look(1);
-    }
-    auto step = [&](int it, char* kb, char* vb, char* knext, char* vnext) {
+    auto step = [&](auto careful, int it, char* kb, char* vb, char* knext, char* vnext) __attribute__((always_inline)) {
         // this tile is there once every wave's loads have arrived, and the other buffers free
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
         __syncthreads();
@@ -313,7 +309,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             look(it + 2);
         }
         const int base = lo + it * kTile;
-        if (!(base + kTile - 1 <= block_last && base >= block_from && ~there == 0)) {
+        if (careful.value || !(base + kTile - 1 <= block_last && base >= block_from && ~there == 0)) {
             clean(vb, base);
             __syncthreads();
         }
@@ -394,9 +390,31 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 3, 1);
     };
-    for (int it = 0; it < tiles; it += 2) {
-        step(it, k0, v0, k1, v1);
-        if (it + 1 < tiles) step(it + 1, k1, v1, k0, v0);
+    auto pass = [&](auto careful) __attribute__((always_inline)) {
+        m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+        if (tiles > 0) {
+            look(0);
+            fetch(0, k0, v0);
+            look(1);
+        }
+        for (int it = 0; it < tiles; it += 2) {
+            step(careful, it, k0, v0, k1, v1);
+            if (it + 1 < tiles) step(careful, it + 1, k1, v1, k0, v0);
+        }
+    };
+    pass(std::false_type());
+    {
+        // 0 times a finite number is 0; where the row's own sum is none, so is its result, whatever the values
+        float zero = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
+        if (__syncthreads_or(zero != 0.f && l * 0.f == 0.f)) pass(std::true_type());
     }
 
     l += __shfl_xor(l, 32);
