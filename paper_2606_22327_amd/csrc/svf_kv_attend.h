@@ -59,12 +59,12 @@ __device__ inline uint32_t odd_marks_of(uint32_t w) {
     }
     return marks;
 }
-// Adds what the marks of n values stand for.
-__device__ inline void add_marks(uint32_t marks, float* acc, int n) {
+// n sums of which some have marks: what those are, whatever is added to it.
+__device__ inline void set_marked(uint32_t marks, float* acc, int n) {
     if (marks == 0) return;
     for (int i = 0; i < n; i++) {
-        if (marks >> 2 * i & 1) acc[i] += INFINITY;
-        if (marks >> 2 * i & 2) acc[i] -= INFINITY;
+        const uint32_t m = marks >> 2 * i & 3;
+        if (m) acc[i] = m == 1 ? INFINITY : m == 2 ? -INFINITY : __builtin_nanf("");
     }
 }
 

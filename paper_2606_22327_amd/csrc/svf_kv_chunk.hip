@@ -1,7 +1,5 @@
 // svf_kv_chunk.hip -- attention over the paged cache of sequences with many rows
 // (new tokens times query heads of a key head): prompts and their pieces.
-#include <type_traits>
-
 #include "svf_kv_attend.h"
 
 namespace svfk {
@@ -21,6 +19,12 @@ struct ChunkPlan {
     int32_t* items;  // row tiles over all key heads, 0 where none is split
     Item* item;      // [groups / 2]
     float* part;     // [groups][kRows][D + 4]
+};
+
+// The arguments of k_attend_chunk as they lie in memory.
+struct ChunkCall {
+    AttendArgs p;
+    ChunkPlan plan;
 };
 
 // Whether these kernels take the sequence, and not those of few rows.
@@ -207,7 +211,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         koff[i] = (uint32_t)r * (uint32_t)p.kv.k_row + x;
         voff[i] = (uint32_t)r * (uint32_t)p.kv.v_row + x;
     }
-    auto look = [&](int it) __attribute__((always_inline)) {
+    auto look = [&](int it) {
         page_all = table_entry(p.kv, table, lo + it * kTile + lane);
         if constexpr (!WIDE) {
 #pragma unroll
@@ -220,7 +224,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (Lds)to, 16, 0, 0);
     };
     uint64_t there, there_next;
-    auto fetch = [&](int it, char* kto, char* vto) __attribute__((always_inline)) {
+    auto fetch = [&](int it, char* kto, char* vto) {
         const int j0 = lo + it * kTile;
         there_next = __ballot((unsigned)page_all < (unsigned)p.kv.num_pages && j0 + lane < hi);
         kto += wave * NI * 1024;
@@ -251,14 +255,19 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             }
         }
     };
+    // The marks of two values of a slot for the rows that see it.
+    auto mark = [&](int j, int w, uint32_t marks) {
+        for (int y = 0; y <= last_row - first_row; y++) {
+            const int t = r0 + (first_row + y) / G;
+            if ((!p.causal || j <= t) && (p.window == 0 || j > t - p.window)) atomicOr(&odd_marks[y][w >> 3], marks << 4 * (w & 7));
+        }
+    };
     // Where the tile's rows do not all see the same slots, a value that is no finite number would reach those
     // that do not see it (0 times infinity): it counts as 0, and the rows that see it get it
     // from their marks.  Each wave looks through the values of sixteen slots.
-    // A tile whose slots all rows see is not looked through at first.  There such a value meets probabilities that have
-    // become 0, which makes no number of what is infinite; but it also leaves a sum that is no finite number, and
-    // then the row tile is worked through once more, with every tile looked through (``careful``; in a loop of its own: one loop
-    // for both spills registers where a head has 256 dimensions).
-    auto clean = [&](char* vb, int base) __attribute__((always_inline)) {
+    // A tile whose slots all rows see is not looked through: there such a value can make no number of a sum, but only of sums that
+    // it decides, and those are found at the end by being no finite numbers.
+    auto clean = [&](char* vb, int base) {
         u16x2 size = {0, 0};
         uint32_t* words = (uint32_t*)(vb + wave * 16 * D * 2) + lane;
         for (int x = 0; x < 8 * D; x += 64) size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, words[x] & 0x7fff7fffu));
@@ -268,12 +277,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             if (!odd_pair<E>(pair)) continue;
             const int r = wave * 16 + (x + lane) / (D / 2), at = (x + lane) % (D / 2);
             const int w = ((at >> 2) ^ swizzle<D>(r)) * 4 + (at & 3);  // the dimensions 2 w and 2 w + 1
-            const uint32_t marks = odd_marks_of<E>(pair) << 4 * (w & 7);
-            for (int y = 0; y <= last_row - first_row; y++) {
-                const int t = r0 + (first_row + y) / G;
-                if ((there >> r & 1) && (!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window))
-                    atomicOr(&odd_marks[y][w >> 3], marks);
-            }
+            if (there >> r & 1) mark(base + r, w, odd_marks_of<E>(pair));
             words[x] = finite_pair<E>(pair);
         }
     };
@@ -297,9 +301,19 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             asm volatile("" : "+v"(va[d][i]));
         }
 
-    float m, l;
+    float m = -INFINITY, l = 0.f;
     f32x16 o[DT];
-    auto step = [&](auto careful, int it, char* kb, char* vb, char* knext, char* vnext) __attribute__((always_inline)) {
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+
+    if (tiles > 0) {
+        look(0);
+        fetch(0, k0, v0);
+        look(1);
+    }
+    auto step = [&](int it, char* kb, char* vb, char* knext, char* vnext) {
         // this tile is there once every wave's loads have arrived, and the other buffers free
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
         __syncthreads();
@@ -309,7 +323,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             look(it + 2);
         }
         const int base = lo + it * kTile;
-        if (careful.value || !(base + kTile - 1 <= block_last && base >= block_from && ~there == 0)) {
+        if (!(base + kTile - 1 <= block_last && base >= block_from && ~there == 0)) {
             clean(vb, base);
             __syncthreads();
         }
@@ -390,40 +404,42 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 3, 1);
     };
-    auto pass = [&](auto careful) __attribute__((always_inline)) {
-        m = -INFINITY, l = 0.f;
+    for (int it = 0; it < tiles; it += 2) {
+        step(it, k0, v0, k1, v1);
+        if (it + 1 < tiles) step(it + 1, k1, v1, k0, v0);
+    }
+
+    // What is needed from here on only is read from here on only: kept in registers through the loop, it costs the loop its schedule
+    // (the arguments lie in memory in this order).
+    typedef const __attribute__((address_space(4))) ChunkCall* Call;
+    Call call = (Call)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(call));
+    const AttendArgs& z = ((const ChunkCall*)call)->p;
+    // Rows with a sum that is no finite number (0 times a finite one is 0), though the row's own sum of probabilities is one: which values
+    // that are none the rows see.
+    float zero = 0.f;
 #pragma unroll
-        for (int d = 0; d < DT; d++)
+    for (int d = 0; d < DT; d++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) o[d][i] = 0.f;
-        if (tiles > 0) {
-            look(0);
-            fetch(0, k0, v0);
-            look(1);
+        for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
+    if (__syncthreads_or(zero != 0.f && l * 0.f == 0.f)) {
+        const int w = tid % (D / 2);  // the dimensions 2 w and 2 w + 1
+        for (int j = lo + tid / (D / 2); j < hi; j += 256 / (D / 2)) {
+            const int at = entry_row(z.kv, table_entry(z.kv, table, j), j, true);
+            if (at < 0) continue;
+            const uint32_t pair = load_global<uint32_t>(vbase + row_offset(at, z.kv.shift, z.kv.v_page, z.kv.v_row) + w * 4);
+            if (odd_pair<E>(pair)) mark(j, w, odd_marks_of<E>(pair));
         }
-        for (int it = 0; it < tiles; it += 2) {
-            step(careful, it, k0, v0, k1, v1);
-            if (it + 1 < tiles) step(careful, it + 1, k1, v1, k0, v0);
-        }
-    };
-    pass(std::false_type());
-    {
-        // 0 times a finite number is 0; where the row's own sum is none, so is its result, whatever the values
-        float zero = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; d++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
-        if (__syncthreads_or(zero != 0.f && l * 0.f == 0.f)) pass(std::true_type());
+        __syncthreads();
     }
 
     l += __shfl_xor(l, 32);
     if (row >= rows) return;
     const int hq = head * G + row - t * G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    char* out = p.out + (s.q0 + t) * p.o_tok + hq * p.o_head;
+    char* out = z.out + (s.q0 + t) * z.o_tok + hq * z.o_head;
     float* to = nullptr;
-    if (parts > 1) to = plan.part + ((int64_t)blockIdx.x * kRows + wave * 32 + c) * (D + 4);
+    if (parts > 1) to = ((const ChunkCall*)call)->plan.part + ((int64_t)blockIdx.x * kRows + wave * 32 + c) * (D + 4);
     typedef T V4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int d = 0; d < DT; d++)
@@ -431,7 +447,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         for (int b = 0; b < 4; b++) {
             const int dim = d * 32 + b * 8 + h * 4;
             float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
-            add_marks(odd_marks[wave * 32 + c][dim >> 4] >> 2 * (dim & 15), x, 4);
+            set_marked(odd_marks[wave * 32 + c][dim >> 4] >> 2 * (dim & 15), x, 4);
             if (to)
                 *(f32x4*)(to + dim) = f32x4{x[0], x[1], x[2], x[3]};
             else
@@ -441,7 +457,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         if (to)
             to[D] = m, to[D + 1] = l;
         else
-            p.lse[(int64_t)(s.q0 + t) * p.heads + hq] = (m - E::kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+            z.lse[(int64_t)(s.q0 + t) * z.heads + hq] = (m - E::kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
     }
 }
 

@@ -404,7 +404,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
 #pragma unroll
                     for (int j = 0; j < VD; j++) acc[j] += red[w][rr][d0 + j] * f;
                 }
-                add_marks(odd_marks[row][tid & 15], acc, VD);
+                set_marked(odd_marks[row][tid & 15], acc, VD);
                 if (whole) {
                     const int t = row / G, h = head * G + row - t * G;
                     write_row<E, VD>(p, s.q0 + t, h, d0, acc, den, top);
