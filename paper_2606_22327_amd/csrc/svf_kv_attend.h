@@ -18,6 +18,13 @@ struct BF16M : BF16 {
     static constexpr float kShift = 0.f;
     static constexpr uint16_t kInf = 0x7f80;
     static constexpr float kSlack = 8.f;
+    // Two numbers, each as the sum of two of the type, as words of two: the upper 16 bits of each, and what is left, rounded.
+    static __device__ inline void split(float a, float b, uint32_t& hi, uint32_t& low) {
+        typedef __bf16 V2 __attribute__((ext_vector_type(2)));
+        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+        hi = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        low = __builtin_bit_cast(uint32_t, V2{(__bf16)(a - __uint_as_float(x & 0xffff0000u)), (__bf16)(b - __uint_as_float(y & 0xffff0000u))});
+    }
     static __device__ inline f32x4 mfma16(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ inline f32x16 mfma32(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
@@ -25,6 +32,11 @@ struct F16M : F16 {
     static constexpr float kShift = 14.f;
     static constexpr uint16_t kInf = 0x7c00;
     static constexpr float kSlack = 1.f;
+    static __device__ inline void split(float a, float b, uint32_t& hi, uint32_t& low) {
+        const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+        hi = __builtin_bit_cast(uint32_t, h);
+        low = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a - (float)h.x, b - (float)h.y));
+    }
     static __device__ inline f32x4 mfma16(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ inline f32x16 mfma32(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
