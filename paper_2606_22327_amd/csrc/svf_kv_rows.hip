@@ -579,11 +579,12 @@ __device__ void weigh_again(const AttendArgs& p, const RowsPlan& plan, int64_t u
 template <class E, int D>
 __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan) {
     const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = plan.first_unit[p.kv.seqs] * hk;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), all = plan.first_unit[p.kv.seqs] * hk;
     for (int64_t unit = plan.score_units + wave; unit < all; unit += (int64_t)gridDim.x * 4) weigh_again<E, D>(p, plan, unit);
     if (wave >= min(all, plan.score_units)) return;
     const int4 x = plan.units[wave];
     const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + 2 * lane;
+    const Seq s = seq_of(p.kv, x.x);
     const Table table = table_of(p.kv, x.x, zero_row());
     const int page[2] = {table_entry(p.kv, table, j), table_entry(p.kv, table, j + 1)};
     const float2* sc = (const float2*)(plan.scores + wave * plan.rows * kUnit) + lane;
@@ -594,11 +595,12 @@ __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan
         const float lse = p.lse[x.y + t * p.heads + r - t * G] * 1.4426950408889634f;
         const float2 y = sc[r * (kUnit / 2)];
         const float ref = lse == -INFINITY ? INFINITY : lse;  // a row that saw nothing adds nothing
-        sum.x += exp2_fast(y.x - ref);
-        sum.y += exp2_fast(y.y - ref);
+        // only to slots that the row sees: a statistic that is no number makes one of every score, also of the -inf of the others
+        const int own = s.len - s.n + t, last = p.causal ? own : s.len - 1, from = p.window > 0 ? own - p.window + 1 : 0;
+        sum.x += j <= last && j >= from ? exp2_fast(y.x - ref) : 0.f;
+        sum.y += j < last && j + 1 >= from ? exp2_fast(y.y - ref) : 0.f;
     }
-    // a slot that is not there has scores of -inf only
-    const int row0 = entry_row(p.kv, page[0], j, sum.x != 0.f), row1 = entry_row(p.kv, page[1], j + 1, sum.y != 0.f);
+    const int row0 = entry_row(p.kv, page[0], j, j < s.len && sum.x != 0.f), row1 = entry_row(p.kv, page[1], j + 1, j + 1 < s.len && sum.y != 0.f);
     if (row0 >= 0) p.kv.weight[stat_index(p.kv, row0, head)] += sum.x;
     if (row1 >= 0) p.kv.weight[stat_index(p.kv, row1, head)] += sum.y;
 }

@@ -45,3 +45,53 @@ def test_outputs_keep_their_bits_whatever_the_number_of_rows(dtype, heads, kv_he
     kept = P.out_tolerance(dtype, dim, out, tol, length) - 1.01 * P.UNIT[dtype] * tol["absv"]
     kept = kept + (2.0 ** -15 if dtype == BF else 2.0 ** -21) * tol["absv"]
     assert ((got.cpu().double() - out).abs() <= kept).all()
+
+
+def added_weights(s, causal, window):
+    """What attention adds to each slot's weight, in 64 bits: the softmax of every row over the slots that it sees, and of no others."""
+    q, k, (T, H, D) = s["q"].double(), s["k"].double(), s["q"].shape
+    pages, hk, page = k.shape[:3]
+    weight = torch.zeros((pages, hk, page), dtype=torch.float64)
+    for i in range(len(s["kv_len"])):
+        a, b = int(s["offsets"][i]), int(s["offsets"][i + 1])
+        pg, row = P.slots_of(s["table"], i, s["kv_len"][i], page, pages)
+        j = torch.arange(len(pg))
+        for t in range(a, b):
+            own = len(pg) - (b - t)
+            w = (pg >= 0) & (j <= own if causal else j >= 0) & (j > own - window if window else j >= 0)
+            for h in range(H):
+                g = h // (H // hk)
+                x = D ** -0.5 * (k[pg[w], g, row[w]] @ q[t, h])
+                e = torch.exp(x - x.max()) if len(x) else x
+                weight[pg[w], g, row[w]] += e / e.sum()
+    return weight
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new", [1, 4, 8, 40])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 30)])
+@pytest.mark.parametrize("what", ["query", "key", "infinite key", "first slot's key"])
+def test_weights_of_rows_that_are_not_numbers_stay_with_the_slots_they_see(dtype, new, causal, window, what):
+    """A row whose statistic is no number, in a sequence whose table is filled up with another's pages: that one's weights, and those
+    of slots which the row does not see, are what they are without it."""
+    from paper_2606_22327_amd import kvcache as C
+    s = make(52, [100, 75, 200, 40], [new] * 4, 8, 2, 64, 16, dtype, stats=True)
+    tol = P.attend(s["q"], s["k"], s["v"], s["offsets"], s["kv_len"], s["table"], causal, window, 64 ** -0.5)[3]
+    for i in (0, 1, 3):
+        used = -(-int(s["kv_len"][i]) // 16)
+        s["table"][i, used:] = s["table"][2, 3:3 + s["table"].shape[1] - used]
+    pg, row = P.slots_of(s["table"], 1, 75, 16, s["k"].shape[0])
+    if what == "query":
+        s["q"][2 * new - 1, 5, 7] = math.nan
+    else:
+        at = {"key": 74, "infinite key": 73 if new > 1 else 74, "first slot's key": 75 - new}[what]
+        s["k"][pg[at], 1, row[at], 3] = math.inf if what == "infinite key" else math.nan
+    add = added_weights(s, causal, window)
+    w = s["weight"].cuda()
+    C.attend(s["q"].cuda(), C.Batch(s["offsets"].cuda(), s["kv_len"].cuda(), s["table"].cuda(), new),
+             C.Cache(s["k"].cuda(), s["v"].cuda(), w), causal=causal, window=window, add_weight=True)
+    z = w.cpu().double() - s["weight"].double()
+    assert torch.equal(z.isnan(), add.isnan()) and add.isnan().any() and not add.isnan().all()
+    ok = (z - add).abs() <= P.weight_tolerance(64, s["weight"].double(), add, tol, 4 * new)
+    assert (ok | add.isnan()).all()
