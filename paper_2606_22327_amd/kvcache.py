@@ -307,8 +307,7 @@ def rope_table(positions: int, rot: int, base: float = 10000.0, scaling: str = "
         _need(original > 0 and fast > slow > 0, "scaling 'by-parts' needs original > 0 and fast > slow > 0")
         # the pair that turns x times within the original context
         pair = lambda x: rot * math.log(original / (x * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
-        lo, hi = math.floor(pair(fast)), math.ceil(pair(slow))
-        lo, hi = max(lo, 0), min(hi, rot // 2 - 1)
+        lo, hi = math.floor(pair(fast)), math.ceil(pair(slow))     # which need not be pairs that there are
         ramp = ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
         freq = freq * (1 - ramp) + freq / factor * ramp
         size = 0.1 * math.log(factor) + 1.0

@@ -95,3 +95,25 @@ def test_weights_of_rows_that_are_not_numbers_stay_with_the_slots_they_see(dtype
     assert torch.equal(z.isnan(), add.isnan()) and add.isnan().any() and not add.isnan().all()
     ok = (z - add).abs() <= P.weight_tolerance(64, s["weight"].double(), add, tol, 4 * new)
     assert (ok | add.isnan()).all()
+
+
+@pytest.mark.parametrize("rot,base,original", [(128, 10000.0, 4096), (128, 10000.0, 65536), (64, 500000.0, 8192), (128, 10000.0, 262144),
+                                               (64, 10000.0, 100), (32, 10000.0, 5), (64, 10000.0, 3000000)])
+def test_rope_by_parts_follows_its_turns_for_short_and_long_contexts(rot, base, original):
+    """Pairs by their turns within the original context: more than ``fast`` stay, fewer than ``slow`` are divided by the factor, and between
+    them there is one straight ramp, wherever it ends.  (Angles of position 1 from the table: 2^-24 of rounding.)"""
+    from paper_2606_22327_amd import kvcache as C
+    factor, fast, slow = 4.0, 32.0, 1.0
+    t = C.rope_table(2, rot, base=base, scaling="by-parts", factor=factor, original=original, device="cpu").double()
+    freq = base ** (-2.0 * torch.arange(rot // 2, dtype=torch.float64) / rot)
+    part = (1 - torch.atan2(t[1, rot // 2:], t[1, :rot // 2]) / freq) / (1 - 1 / factor)      # 0: stays, 1: divided
+    err = 2.0 ** -22 / freq
+    turns = original * freq / (2 * math.pi)
+    assert (part.abs() <= err)[turns >= fast].all() and ((part - 1).abs() <= err)[turns <= slow].all()
+    step = 2 * math.log(base) / rot                     # in ln turns, from a pair to the next
+    x = torch.log(turns) / step                         # falls by one a pair
+    # the ramp begins at the last pair position that turns at least fast, and ends at the first that turns at most slow
+    lo = math.floor(x[0].item() - math.log(fast) / step + 1e-9)
+    hi = math.ceil(x[0].item() - math.log(slow) / step - 1e-9)
+    want = ((torch.arange(rot // 2, dtype=torch.float64) - lo) / (hi - lo)).clamp(0, 1)
+    assert ((part - want).abs() <= err).all()
