@@ -80,6 +80,9 @@ __device__ inline void set_marked(uint32_t marks, float* acc, int n) {
     }
 }
 
+// A part's sum by the part's factor.  One that marked values decide stays, also where the factor has become 0.
+__device__ inline float scaled(float x, float f) { return fabsf(x) == INFINITY ? x : x * f; }
+
 // The first slot that any row of the sequence sees, or one of the fifteen before it: pages of 16 slots and more
 // are read from a multiple of 16.
 __device__ inline int first_slot(const AttendArgs& p, const Seq& s) {

@@ -496,7 +496,7 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
         const float keep = exp2_fast(top - ref), f = exp2_fast(from[D] - ref);
         den = den * keep + from[D + 1] * f;
 #pragma unroll
-        for (int j = 0; j < VD; j++) acc[j] = acc[j] * keep + from[d0 + j] * f;
+        for (int j = 0; j < VD; j++) acc[j] = scaled(acc[j], keep) + scaled(from[d0 + j], f);
         top = now;
     }
     const int t = at / G;

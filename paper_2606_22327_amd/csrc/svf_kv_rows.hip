@@ -502,14 +502,14 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
                 const float ref = now == -INFINITY ? 0.f : now, keep = exp2_fast(top - ref);
                 den *= keep;
 #pragma unroll
-                for (int j = 0; j < VD; j++) acc[j] *= keep;
+                for (int j = 0; j < VD; j++) acc[j] = scaled(acc[j], keep);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     if (x0 + i * parts > w1) continue;
                     const float f = exp2_fast(pm[i] - ref);
                     den += pl[i] * f;
 #pragma unroll
-                    for (int j = 0; j < VD; j++) acc[j] += pv[i][j] * f;
+                    for (int j = 0; j < VD; j++) acc[j] += scaled(pv[i][j], f);
                 }
                 top = now;
             }
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
                     const float f = exp2_fast(red_m[g0 + x] - ref);
                     den += red_l[g0 + x] * f;
 #pragma unroll
-                    for (int j = 0; j < VD; j++) acc[j] += red[g0 + x][d0 + j] * f;
+                    for (int j = 0; j < VD; j++) acc[j] += scaled(red[g0 + x][d0 + j], f);
                 }
             }
         }

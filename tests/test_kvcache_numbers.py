@@ -117,3 +117,18 @@ def test_rope_by_parts_follows_its_turns_for_short_and_long_contexts(rot, base, 
     hi = math.ceil(x[0].item() - math.log(slow) / step - 1e-9)
     want = ((torch.arange(rot // 2, dtype=torch.float64) - lo) / (hi - lo)).clamp(0, 1)
     assert ((part - want).abs() <= err).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("slot", [5, 1500, 2900])
+@pytest.mark.parametrize("what", [math.inf, -math.inf])
+def test_infinite_values_pass_the_join_of_split_rows(dtype, new, slot, what):
+    """The part that has the value has scores far below the others', so that its factor becomes 0."""
+    s = far_below(53, 3000, new, dtype, slot, what)
+    pg, row = P.slots_of(s["table"], 0, 3000, 16, s["k"].shape[0])
+    part = torch.arange(3000) // 500 == slot // 500
+    s["k"][pg[part], 0, row[part], 0] = -200
+    out, _, _ = check_attend(s)
+    assert (out[..., 7] == what).all()
