@@ -139,7 +139,8 @@ int svf_kv_append(const svf_kv_cache *cache, const svf_kv_batch *batch,
  *   out = sum_j softmax_j(scale q.k_j) v_j,   lse = ln sum_j exp(scale q.k_j),
  * and a row that sees none, or only scores of -inf, has out = 0 and
  * lse = -inf.  What lies in slots that a row does not see, NaN and infinities
- * among it, has no effect on that row.
+ * among it, has no effect on that row; an infinite or NaN element of a value that it
+ * sees decides its output however small the slot's softmax is.
  *   add_weight  1: weight[j] += the sum of slot j's softmax over the tokens and
  *               the query heads of its key head (in an order that is the same
  *               every time).  Each page at most once in the batch then.

@@ -112,15 +112,15 @@ __device__ inline void load_query(typename E::V8* q, const char* at, int g, bool
 }
 
 // N of a row's dimensions from d0: the sums over the softmax's denominator, rounded once, and with the
-// first of them the row's statistic.
+// first of them the row's statistic.  A row without a probability has zeros, whatever its values.
 template <class E, int N>
 __device__ inline void write_row(const AttendArgs& p, int token, int h, int d0, const float* acc, float den, float top) {
     using T = typename E::T;
     typedef T V __attribute__((ext_vector_type(N)));
-    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const float inv = 1.f / den;
     V v;
 #pragma unroll
-    for (int j = 0; j < N; j++) v[j] = (T)(acc[j] * inv);
+    for (int j = 0; j < N; j++) v[j] = (T)(den == 0.f ? 0.f : acc[j] * inv);
     *(V*)(p.out + token * p.o_tok + h * p.o_head + d0 * 2) = v;
     if (d0 == 0) p.lse[(int64_t)token * p.heads + h] = (top - E::kShift + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
 }

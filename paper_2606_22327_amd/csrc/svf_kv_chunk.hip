@@ -451,7 +451,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     l += __shfl_xor(l, 32);
     if (row >= rows) return;
     const int hq = head * G + row - t * G;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = 1.f / l;
     char* out = z.out + (s.q0 + t) * z.o_tok + hq * z.o_head;
     float* to = nullptr;
     if (parts > 1) to = ((const ChunkCall*)call)->plan.part + ((int64_t)blockIdx.x * kRows + wave * 32 + c) * (D + 4);
@@ -463,10 +463,14 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             const int dim = d * 32 + b * 8 + h * 4;
             float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
             set_marked(odd_marks[wave * 32 + c][dim >> 4] >> 2 * (dim & 15), x, 4);
-            if (to)
+            if (to) {
                 *(f32x4*)(to + dim) = f32x4{x[0], x[1], x[2], x[3]};
-            else
-                *(V4*)(out + dim * 2) = V4{(T)(x[0] * inv), (T)(x[1] * inv), (T)(x[2] * inv), (T)(x[3] * inv)};
+            } else {
+                V4 y;
+#pragma unroll
+                for (int i = 0; i < 4; i++) y[i] = (T)(l == 0.f ? 0.f : x[i] * inv);
+                *(V4*)(out + dim * 2) = y;
+            }
         }
     if (h == 0) {
         if (to)

@@ -132,3 +132,16 @@ def test_infinite_values_pass_the_join_of_split_rows(dtype, new, slot, what):
     s["k"][pg[part], 0, row[part], 0] = -200
     out, _, _ = check_attend(s)
     assert (out[..., 7] == what).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("length", [100, 3000])
+@pytest.mark.parametrize("new", [1, 40])
+def test_rows_of_infinitely_small_scores_are_zero_whatever_their_values(dtype, length, new):
+    from paper_2606_22327_amd import kvcache as C
+    s = far_below(54, length, new, dtype, 5, math.inf)
+    s["k"][..., 0] = -math.inf
+    out, lse = C.attend(s["q"].cuda(), C.Batch(s["offsets"].cuda(), s["kv_len"].cuda(), s["table"].cuda(), new),
+                        C.Cache(s["k"].cuda(), s["v"].cuda()))
+    assert (out == 0).all() and (lse == -math.inf).all()
