@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     __syncthreads();
 
     const uint64_t kbase = (uint64_t)(p.kv.k + head * p.kv.k_head), vbase = (uint64_t)(p.kv.v + head * p.kv.v_head);
-    const Table table = table_of(p.kv, seq, zero_row());
+    const Table table = table_of(p.kv, seq, s.len, zero_row());
     const int mask = (1 << p.kv.shift) - 1;
     // A wave fetches sixteen of a tile's slots, 64 / CH of them with an instruction; a lane's
     // slot of instruction i is own + i * 64 / CH.

@@ -60,16 +60,17 @@ __device__ inline int pool_row(const KvView& kv, int seq, int j) {
 }
 
 // The same in two steps, so that the load can be on its way while the row before it is used: the
-// table's entry, of the nearest slot that the table has (there is no branch in it: at its end the
-// compiler would wait for every load on its way) ...
+// table's entry, of the nearest slot that the sequence has (there is no branch in it: at its end the
+// compiler would wait for every load on its way; entries behind its length are not read, and where it has no slot
+// ``zero`` is read instead) ...
 struct Table {
     uint64_t base;
     int last;
 };
-__device__ inline Table table_of(const KvView& kv, int seq, const void* zero) {
+__host__ __device__ inline Table table_of(const KvView& kv, int seq, int len, const void* zero) {
     Table t;
-    t.last = kv.width > 0 ? kv.width - 1 : 0;
-    t.base = kv.width > 0 ? (uint64_t)(kv.table + (int64_t)seq * kv.table_stride) : (uint64_t)zero;
+    t.last = len > 0 ? (len - 1) >> kv.shift : 0;
+    t.base = len > 0 ? (uint64_t)(kv.table + (int64_t)seq * kv.table_stride) : (uint64_t)zero;
     return t;
 }
 __device__ inline int table_entry(const KvView& kv, const Table& t, int j) {

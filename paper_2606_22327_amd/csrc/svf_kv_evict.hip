@@ -82,7 +82,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_select(EvictArgs p, int64_t p
     __shared__ int found_rank;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int recent_from = (int)max((int64_t)p.next[seq] - p.recent, (int64_t)INT32_MIN);
-    const Table table = table_of(p.kv, seq, p.next);
+    const Table table = table_of(p.kv, seq, len, p.next);
     // N slots THREADS apart: their loads go together, the table's first and then what it leads to
     auto keys_of = [&](int j0, auto count, uint32_t* out) {
         constexpr int N = decltype(count)::value;

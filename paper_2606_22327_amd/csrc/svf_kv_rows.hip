@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
             for (int j = 0; j < VD; j++) o[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         const int slot0 = lo + wave * 32 + (lane & 31);
-        const Table table = table_of(p.kv, seq, zero_row());
+        const Table table = table_of(p.kv, seq, s.len, zero_row());
         auto entry = [&](int u) { return table_entry(p.kv, table, slot0 + u * kUnit); };
         auto where = [&](int u, int page) {
             const int j = slot0 + u * kUnit, row = entry_row(p.kv, page, j, u < u1 && j < s.len);
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan
     const int4 x = plan.units[wave];
     const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + 2 * lane;
     const Seq s = seq_of(p.kv, x.x);
-    const Table table = table_of(p.kv, x.x, zero_row());
+    const Table table = table_of(p.kv, x.x, s.len, zero_row());
     const int page[2] = {table_entry(p.kv, table, j), table_entry(p.kv, table, j + 1)};
     const float2* sc = (const float2*)(plan.scores + wave * plan.rows * kUnit) + lane;
     float2 sum = {0.f, 0.f};
