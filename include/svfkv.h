@@ -98,7 +98,7 @@ typedef struct svf_kv_batch {
  * Rotary positions on new queries and keys, and the new tokens' slots.
  *   q, k, v     [num_tokens][heads or kv_heads][head_dim]; strides of token and
  *               head in elements, head_dim contiguous; any alignment
- *   q_out       the same shape as q; may be q itself with the same strides
+ *   q_out       the same shape as q; q itself with the same strides, or apart from it
  *   positions   int32 [num_tokens]
  *   rope        float [rope_rows][rot]: rot/2 cosines, then rot/2 sines, of
  *               each position; whatever stretches positions for long

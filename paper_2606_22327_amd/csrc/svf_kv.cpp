@@ -94,6 +94,39 @@ int check_heads(const svf_kv_cache* c, int32_t heads) {
     return SVF_OK;
 }
 
+// A tensor [tokens][heads][dim] of 16-bit elements, strides in elements.
+struct Rows {
+    const void* at;
+    int64_t token, head;
+};
+
+// Whether two tensors of one shape share an element: exactly where their strides are equal and rows lie side by side, so that
+// parts of one buffer are apart; else by the first and the last address.
+bool overlap(Rows a, Rows b, int64_t tokens, int64_t heads, int64_t dim) {
+    typedef __int128 Wide;
+    if (tokens == 1) a.token = b.token = 0;
+    if (heads == 1) a.head = b.head = 0;
+    const Wide row = dim * 2, delta = (Wide)reinterpret_cast<uintptr_t>(b.at) - (Wide)reinterpret_cast<uintptr_t>(a.at);
+    auto span = [&](const Rows& x) { return ((Wide)x.token * (tokens - 1) + (Wide)x.head * (heads - 1)) * 2 + row; };
+    if (delta >= span(a) || -delta >= span(b)) return false;
+    const bool outer_token = a.token >= a.head;
+    const Wide so = (outer_token ? a.token : a.head) * (Wide)2, si = (outer_token ? a.head : a.token) * (Wide)2;
+    const int64_t no = outer_token ? tokens : heads, ni = outer_token ? heads : tokens;
+    const bool apart = (ni == 1 || si >= row) && (no == 1 || so >= si * (ni - 1) + row);
+    if (a.token != b.token || a.head != b.head || !apart) return true;
+    // delta = x so + y si + less than a row either way
+    auto below = [](Wide n, Wide d) { return n >= 0 ? n / d : -((-n + d - 1) / d); };
+    for (Wide x = no > 1 ? below(delta, so) : 0, x1 = no > 1 ? x + 1 : 0; x <= x1; x++) {
+        if (x <= -no || x >= no) continue;
+        const Wide rest = delta - x * so;
+        for (Wide y = ni > 1 ? below(rest, si) : 0, y1 = ni > 1 ? y + 1 : 0; y <= y1; y++) {
+            const Wide off = rest - y * si;
+            if (y > -ni && y < ni && off > -row && off < row) return true;
+        }
+    }
+    return false;
+}
+
 int launched(hipError_t e) {
     return e == hipSuccess ? SVF_OK : fail(SVF_EHIP, "kernel launch: %s", hipGetErrorString(e));
 }
@@ -152,6 +185,9 @@ int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_app
     if (b->num_tokens == 0 || b->num_seqs == 0) return SVF_OK;
     if (!b->q_offsets || !a->q || !a->k || !a->v || !a->q_out || !a->positions)
         return fail(SVF_EINVAL, "q_offsets, q, k, v, q_out and positions must not be NULL");
+    const Rows q = {a->q, a->q_token_stride, a->q_head_stride}, q_out = {a->q_out, a->out_token_stride, a->out_head_stride};
+    if (a->q != a->q_out && overlap(q, q_out, b->num_tokens, a->heads, c->head_dim))
+        return fail(SVF_EINVAL, "q_out must be q itself or apart from it");
     if (a->rot > 0 && (!a->rope || a->rope_rows < 1)) return fail(SVF_EINVAL, "the table of positions must not be empty");
     if ((int64_t)b->num_tokens * (a->heads + 2 * c->kv_heads) > kGridLimit)
         return fail(SVF_EINVAL, "num_tokens * heads is too large");
@@ -199,6 +235,8 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     const int64_t need = svf_kv_attend_workspace(c, b, a);
     if (a->workspace_bytes < need || (need > 0 && !a->workspace) || !aligned(a->workspace, 256))
         return fail(SVF_EINVAL, "workspace must have %lld bytes, aligned to 256", (long long)need);
+    const Rows q = {a->q, a->q_token_stride, a->q_head_stride}, out = {a->out, a->out_token_stride, a->out_head_stride};
+    if (overlap(q, out, b->num_tokens, a->heads, c->head_dim)) return fail(SVF_EINVAL, "out must be apart from q");
     AttendArgs k;
     k.kv = view(c, b);
     k.q = static_cast<const char*>(a->q);

@@ -1,0 +1,99 @@
+"""More of what the paged cache's entry points refuse: on the CPU calls that are refused, on the GPU such that are taken."""
+
+import random
+
+import pytest
+import torch
+
+from paper_2606_22327_amd import kvcache as C
+from paper_2606_22327_amd import svfsim as S
+from test_kvcache_refusals import A, append, attend, batch, cache
+
+
+def refused(call, *args):
+    assert call(*args, None) == -1
+    return C.last_error()
+
+
+# q and out as offsets, strides and sizes in elements: two tensors of [tokens, heads, 128], and whether they are apart
+PLACES = [
+    (dict(q=0, out=0), False),                                          # in place
+    (dict(q=0, out=2048), True), (dict(q=2048, out=0), True),           # one behind the other
+    (dict(q=0, out=2040), False), (dict(q=0, out=1024), False),
+    (dict(q=0, out=1024, qt=2048, ot=2048), True),                      # the halves of each token of one buffer
+    (dict(q=1024, out=0, qt=2048, ot=2048), True), (dict(q=0, out=1016, qt=2048, ot=2048), False),
+    (dict(q=0, out=128, qh=256, oh=256, qt=2048, ot=2048), True),       # every other head
+    (dict(q=0, out=120, qh=256, oh=256, qt=2048, ot=2048), False),
+    (dict(q=0, out=128, qt=128, ot=128, qh=256, oh=256), False),        # heads outside, tokens inside
+    (dict(q=0, out=256, qt=128, ot=128, qh=512, oh=512), True),
+    (dict(q=0, out=1024, tokens=1, qt=8, ot=4096), True),               # one token: its stride does not count
+    (dict(q=0, out=1024, qt=2048, ot=1024), False),                     # strides that differ: by their ranges
+]
+
+
+def place(q, out, tokens=2, qt=1024, qh=128, ot=1024, oh=128):
+    return dict(q=A + 2 * q, out=A + 2 * out, qt=qt, qh=qh, ot=ot, oh=oh), tokens
+
+
+@pytest.mark.parametrize("kw", [x for x, apart in PLACES if not apart])
+def test_attend_refuses_out_over_q(kw):
+    at, tokens = place(**kw)
+    assert "apart" in refused(S.load().svf_kv_attend, cache(), batch(num_tokens=tokens), attend(**at))
+
+
+def test_append_refuses_q_out_over_a_part_of_q():
+    for off in (8, 1024, 2040):
+        assert "apart" in refused(S.load().svf_kv_append, cache(), batch(), append(q_out=A + 2 * off))
+
+
+def views(q, out, tokens=2, qt=1024, qh=128, ot=1024, oh=128, heads=8, dim=128):
+    buf = torch.randn(20000, device="cuda").to(torch.bfloat16)
+    return (buf.as_strided((tokens, heads, dim), (qt, qh, 1), q), buf.as_strided((tokens, heads, dim), (ot, oh, 1), out))
+
+
+def taken(q, out):
+    """Whether attend and append take these; what they take has to be right."""
+    tokens, heads, dim = q.shape
+    ints = dict(dtype=torch.int32, device="cuda")
+    k = torch.randn((4, 2, 16, dim), device="cuda").to(torch.bfloat16)
+    b = C.Batch(torch.tensor([0, tokens], **ints), torch.tensor([40], **ints), torch.tensor([[2, 0, 1]], **ints), tokens)
+    want = C.attend(q.clone(), b, C.Cache(k, k))[0]
+    held = q.clone()
+    same = out.data_ptr() == q.data_ptr() and out.stride() == q.stride()
+    try:
+        C.attend(q, b, C.Cache(k, k), out=out)
+    except S.SvfError as e:
+        assert "apart" in str(e)
+        if not same:
+            with pytest.raises(S.SvfError):
+                C.append(q, k[:tokens, :, 0], k[:tokens, :, 0], torch.zeros(tokens, **ints), None, b, C.Cache(k, k), q_out=out)
+        return False
+    assert torch.equal(out, want) and torch.equal(q, held)
+    C.append(q, k[:tokens, :, 0], k[:tokens, :, 0], torch.zeros(tokens, **ints), None, b, C.Cache(k, k), q_out=out)
+    assert torch.equal(out, held)
+    return True
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw,apart", PLACES)
+def test_outputs_beside_queries_in_one_buffer(kw, apart):
+    assert taken(*views(**kw)) == apart
+
+
+@pytest.mark.gpu
+def test_outputs_and_queries_of_random_strides_against_every_element():
+    rng = random.Random(3)
+    seen = {True: 0, False: 0}
+    for _ in range(200):
+        tokens, heads = rng.randint(1, 4), rng.choice((2, 4))
+        token_outer = rng.random() < 0.5
+        n = heads if token_outer else tokens
+        si = 64 * rng.randint(1, 3)
+        so = si * (n - 1) + 64 + 64 * rng.randint(0, 2)
+        ts, hs = (so, si) if token_outer else (si, so)
+        q, out = rng.randrange(0, 2000, 8), rng.randrange(0, 2000, 8)
+        rows = lambda at: {at + t * ts + h * hs + d for t in range(tokens) for h in range(heads) for d in range(64)}  # noqa: E731
+        apart = not (rows(q) & rows(out))
+        assert taken(*views(q, out, tokens, ts, hs, ts, hs, heads, 64)) == apart, (tokens, heads, ts, hs, q, out)
+        seen[apart] += 1
+    assert min(seen.values()) > 20, seen
