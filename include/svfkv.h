@@ -28,6 +28,9 @@
  *     page_size], offsets to [0, num_tokens], and a slot whose page number is outside
  *     [0, num_pages) is not there (never written, invisible to attention,
  *     evicted first).
+ *   - A launch has fewer than 2^32 threads; sizes that need more are refused
+ *     (some 2^26 tokens in svf_kv_append, 2^22 sequences times key heads in svf_kv_evict,
+ *     2^31 rows or 2^24 sequences times key heads with chunks in svf_kv_attend).
  *   - Return codes are those of svfsim.h.
  */
 #ifndef SVFKV_H

@@ -27,6 +27,7 @@ int fail(int code, const char* fmt, ...) {
 constexpr int64_t kLimit31 = int64_t(1) << 31;
 constexpr int64_t kStrideLimit = int64_t(1) << 40;  // elements: products with an index stay in 64 bits
 constexpr int64_t kGridLimit = kLimit31 - 1;
+constexpr int64_t kThreadLimit = int64_t(1) << 32;  // of a launch: what HIP supports is below
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -131,18 +132,20 @@ int launched(hipError_t e) {
     return e == hipSuccess ? SVF_OK : fail(SVF_EHIP, "kernel launch: %s", hipGetErrorString(e));
 }
 
+AttendSizes sizes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
+    return {c->num_pages,  c->page_size, c->kv_heads,    a->heads, c->head_dim, c->dtype,
+            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0};
+}
+
 int check_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
     if (int rc = check_sizes(c, b)) return rc;
     if (!a) return fail(SVF_EINVAL, "args must not be NULL");
     if (int rc = check_heads(c, a->heads)) return rc;
     if (a->window < 0) return fail(SVF_EINVAL, "window must be >= 0");
     if ((int64_t)b->num_tokens * a->heads > kGridLimit) return fail(SVF_EINVAL, "num_tokens * heads is too large");
+    if (attend_threads(sizes(c, b, a)) >= kThreadLimit)
+        return fail(SVF_EINVAL, "num_tokens * heads, num_seqs * kv_heads or the pool is too large for one launch");
     return SVF_OK;
-}
-
-AttendSizes sizes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
-    return {c->num_pages,  c->page_size, c->kv_heads,    a->heads, c->head_dim, c->dtype,
-            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0};
 }
 
 int check_evict(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_evict_args* a) {
@@ -211,6 +214,7 @@ int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_app
     k.half_layout = a->layout == SVF_KV_ROPE_HALF;
     k.rope_rows = a->rope_rows;
     k.dim = c->head_dim;
+    if (append_threads(k, wide) >= kThreadLimit) return fail(SVF_EINVAL, "num_tokens is too large (%d)", b->num_tokens);
     return launched(launch_append(k, c->dtype, wide, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -280,6 +284,7 @@ int svf_kv_evict(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_evic
     k.recent = a->recent;
     k.first = a->first;
     k.row_bytes = c->head_dim * 2;
+    if (evict_threads(k) >= kThreadLimit) return fail(SVF_EINVAL, "num_seqs * kv_heads is too large");
     return launched(launch_evict(k, static_cast<hipStream_t>(hip_stream)));
 }
 

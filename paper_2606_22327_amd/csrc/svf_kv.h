@@ -64,10 +64,15 @@ hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStrea
 hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 int64_t attend_workspace(const AttendSizes& z);
+// Threads of the largest launch.
+int64_t append_threads(const AppendArgs& a, bool wide);
+int64_t attend_threads(const AttendSizes& z);
+int64_t evict_threads(const EvictArgs& a);
 
 // The kernels of few rows (svf_kv_rows.hip).
 int32_t few_rows(const AttendSizes& z);
 int64_t rows_workspace(const AttendSizes& z);
+int64_t rows_blocks(const AttendSizes& z);
 hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s);
 
 // Pairs (hole, mover) that one sequence's key head can have.

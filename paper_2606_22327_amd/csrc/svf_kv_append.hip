@@ -167,23 +167,37 @@ __global__ __launch_bounds__(64) void k_append_any(AppendArgs p) {
     }
 }
 
+// How the wide kernel's work is dealt out.
+struct Wide {
+    int units, groups, per;
+    int64_t blocks;
+};
+
+Wide wide_grid(const AppendArgs& a) {
+    Wide w;
+    w.units = a.dim / 16;
+    const int lanes = 64 / w.units, steps = (a.heads + 2 * a.kv.kv_heads + lanes - 1) / lanes;
+    // Heads that a lane walks over: all of a token's once 8,192 waves are there
+    // without splitting a token, fewer for fewer tokens.
+    const int64_t per = ((int64_t)a.kv.tokens * steps + 8191) / 8192;
+    w.per = per < 1 ? 1 : per > steps ? steps : (int)per;
+    w.groups = (steps + w.per - 1) / w.per;
+    w.blocks = ((int64_t)a.kv.tokens * w.groups + 3) / 4;
+    return w;
+}
+
 }  // namespace
+
+int64_t append_threads(const AppendArgs& a, bool wide) { return wide ? wide_grid(a).blocks * 256 : (int64_t)a.kv.tokens * 64; }
 
 hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStream_t s) {
     if (wide) {
-        const int units = a.dim / 16, lanes = 64 / units;
-        const int steps = (a.heads + 2 * a.kv.kv_heads + lanes - 1) / lanes;
-        // Heads that a lane walks over: all of a token's once 8,192 waves are there
-        // without splitting a token, fewer for fewer tokens.
-        int per = (int)(((int64_t)a.kv.tokens * steps + 8191) / 8192);
-        per = per < 1 ? 1 : (per > steps ? steps : per);
-        const int groups = (steps + per - 1) / per;
-        const int64_t waves = (int64_t)a.kv.tokens * groups;
-        const dim3 grid((unsigned)((waves + 3) / 4));
+        const Wide w = wide_grid(a);
+        const dim3 grid((unsigned)w.blocks);
         if (dtype == SVF_KV_BF16)
-            k_append_wide<BF16><<<grid, 256, 0, s>>>(a, units, groups, per);
+            k_append_wide<BF16><<<grid, 256, 0, s>>>(a, w.units, w.groups, w.per);
         else
-            k_append_wide<F16><<<grid, 256, 0, s>>>(a, units, groups, per);
+            k_append_wide<F16><<<grid, 256, 0, s>>>(a, w.units, w.groups, w.per);
     } else {
         if (dtype == SVF_KV_BF16)
             k_append_any<BF16><<<a.kv.tokens, 64, 0, s>>>(a);

@@ -714,6 +714,27 @@ int64_t chunk_workspace(const AttendSizes& z, int32_t few) {
     return groups ? 256 + groups / 2 * (int64_t)sizeof(Item) + (int64_t)groups * kRows * (z.dim + 4) * 4 : 0;
 }
 
+// Workgroups of the launches for these sizes.
+struct ChunkGrids {
+    int64_t blocks, tiles, more;
+};
+
+ChunkGrids grids(const AttendSizes& z, int32_t few) {
+    ChunkGrids g;
+    // Row tiles at most: the full ones of all tokens, and one more for each sequence that is long enough to come here.
+    const int64_t rows = (int64_t)z.tokens * (z.heads / z.kv_heads), long_enough = rows / (few + 1);
+    const int64_t seqs = long_enough < z.seqs ? long_enough : z.seqs;
+    g.blocks = (rows / kRows + seqs) * z.kv_heads;
+    if (g.blocks < split_groups(z, few)) g.blocks = split_groups(z, few);
+    // slot tiles at most, and where every slot has a page: each page is in the batch once
+    const int64_t cap = (int64_t)z.width * z.page_size, all = seqs * ((cap + kWSlots - 1) / kWSlots);
+    const int64_t pool = (int64_t)z.num_pages * z.page_size / kWSlots + seqs;
+    g.tiles = z.add_weight ? (all < pool ? all : pool) : 0;
+    g.more = !z.add_weight ? 0 : all - g.tiles < 64 ? all - g.tiles : 64;
+    g.tiles *= z.kv_heads, g.more *= z.kv_heads;
+    return g;
+}
+
 template <class E, int D>
 hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {
     ChunkPlan plan{split_groups(z, a.few), nullptr, nullptr, nullptr};
@@ -722,17 +743,14 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         plan.item = (Item*)(ws + 256);
         plan.part = (float*)(ws + 256 + plan.groups / 2 * sizeof(Item));
     }
-    // Row tiles at most: the full ones of all tokens, and one more for each sequence that is long enough to come here.
-    const int64_t rows = (int64_t)z.tokens * (z.heads / z.kv_heads), seqs = rows / (a.few + 1);
-    int64_t blocks = (rows / kRows + (seqs < z.seqs ? seqs : z.seqs)) * z.kv_heads;
-    if (blocks < plan.groups) blocks = plan.groups;
-    if (blocks > 0) {
+    const ChunkGrids g = grids(z, a.few);
+    if (g.blocks > 0) {
         // Offsets of sixteen rows are 32 bits.
         const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
         if (z.page_size >= 16 && far < (int64_t(1) << 31))
-            k_attend_chunk<E, D, true><<<(unsigned)blocks, 256, 0, s>>>(a, plan);
+            k_attend_chunk<E, D, true><<<(unsigned)g.blocks, 256, 0, s>>>(a, plan);
         else
-            k_attend_chunk<E, D, false><<<(unsigned)blocks, 256, 0, s>>>(a, plan);
+            k_attend_chunk<E, D, false><<<(unsigned)g.blocks, 256, 0, s>>>(a, plan);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -741,16 +759,10 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.add_weight) {
-        // slot tiles at most, and where every slot has a page: each page is in the batch once
-        const int64_t cap = (int64_t)z.width * z.page_size, most = seqs < z.seqs ? seqs : z.seqs;
-        const int64_t all = most * ((cap + kWSlots - 1) / kWSlots), pool = (int64_t)z.num_pages * z.page_size / kWSlots + most;
-        const int64_t tiles = all < pool ? all : pool, more = all - tiles < 64 ? all - tiles : 64;
-        if (tiles > 0) k_weight_chunk<E, D><<<(unsigned)(tiles * z.kv_heads), 256, 0, s>>>(a);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        if (more > 0) k_weight_chunk_more<E, D><<<(unsigned)(more * z.kv_heads), 256, 0, s>>>(a, tiles);
-    }
+    if (g.tiles > 0) k_weight_chunk<E, D><<<(unsigned)g.tiles, 256, 0, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (g.more > 0) k_weight_chunk_more<E, D><<<(unsigned)g.more, 256, 0, s>>>(a, g.tiles / z.kv_heads);
     return hipGetLastError();
 }
 
@@ -761,6 +773,17 @@ bool has_chunks(const AttendSizes& z) { return (int64_t)z.max_q * (z.heads / z.k
 
 int64_t attend_workspace(const AttendSizes& z) {
     return ((rows_workspace(z) + 255) & ~int64_t(255)) + (has_chunks(z) ? chunk_workspace(z, few_rows(z)) : 0);
+}
+
+int64_t attend_threads(const AttendSizes& z) {
+    int64_t most = rows_blocks(z);
+    if (has_chunks(z)) {
+        const ChunkGrids g = grids(z, few_rows(z));
+        if (g.blocks > most) most = g.blocks;
+        if (g.tiles > most) most = g.tiles;
+        if (g.more > most) most = g.more;
+    }
+    return most * 256;
 }
 
 hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s) {

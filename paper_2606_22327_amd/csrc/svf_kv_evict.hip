@@ -225,6 +225,10 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs p, int64_t pairs_m
 
 }  // namespace
 
+int64_t evict_threads(const EvictArgs& a) {
+    return (int64_t)a.kv.seqs * a.kv.kv_heads * (((int64_t)a.kv.width << a.kv.shift) <= 4096 ? 512 : 1024);
+}
+
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     const int segs = a.kv.seqs * a.kv.kv_heads;
     const int64_t cap = (int64_t)a.kv.width << a.kv.shift;

@@ -689,6 +689,12 @@ int32_t few_rows(const AttendSizes& z) {
 // One launch does where every row has its slots in one unit and no weights are kept.
 bool one_launch(const AttendSizes& z) { return (int64_t)z.width * z.page_size <= kUnit && !z.add_weight; }
 
+int64_t rows_blocks(const AttendSizes& z) {
+    if (!few_rows(z)) return 0;
+    const Layout y = layout(z);
+    return (y.units + 3) / 4 > y.groups ? (y.units + 3) / 4 : y.groups;
+}
+
 int64_t rows_workspace(const AttendSizes& z) { return few_rows(z) && !one_launch(z) ? layout(z).bytes : 0; }
 
 hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {

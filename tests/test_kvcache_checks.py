@@ -97,3 +97,19 @@ def test_outputs_and_queries_of_random_strides_against_every_element():
         assert taken(*views(q, out, tokens, ts, hs, ts, hs, heads, 64)) == apart, (tokens, heads, ts, hs, q, out)
         seen[apart] += 1
     assert min(seen.values()) > 20, seen
+
+
+def test_launches_of_too_many_threads_are_refused():
+    """Sizes within the limits of their numbers whose launch would have 2^32 threads."""
+    from test_kvcache_refusals import evict
+    lib, many = S.load(), 1 << 26
+    for kw in (dict(), dict(qt=1025)):                  # 16 bytes a lane, and element by element
+        assert "too large" in refused(lib.svf_kv_append, cache(kv_heads=1), batch(num_tokens=many),
+                                      append(heads=1, q_out=A + (1 << 60), **kw))
+    big = batch(num_seqs=1 << 21)
+    assert "too large" in refused(lib.svf_kv_evict, cache(page_size=4096), big, evict(workspace_bytes=1 << 62))
+    seqs = batch(num_seqs=1 << 24, num_tokens=1 << 28, max_q=100)
+    assert lib.svf_kv_attend_workspace(cache(), seqs, attend(heads=2)) == -1 and "too large" in C.last_error()
+    assert "too large" in refused(lib.svf_kv_attend, cache(), seqs, attend(heads=2, out=A + (1 << 60), workspace_bytes=1 << 62))
+    # one less is within the limits, as far as the workspace goes
+    assert lib.svf_kv_attend_workspace(cache(), batch(num_seqs=1 << 20, num_tokens=1 << 20, max_q=100), attend(heads=2)) > 0
