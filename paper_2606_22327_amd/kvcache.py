@@ -10,7 +10,8 @@ steps does to a layer's cache on the GPU:
 
 Argument marshalling only: every step runs in the HIP kernels of
 ``libsvfsim.so``, on torch's current stream of the tensors' device.  All tensors are
-on one GPU.  Arguments that can be checked on the host are, and raise
+on one GPU.  There are no backward passes: where gradients are recorded, tensors that
+require one are refused.  Arguments that can be checked on the host are, and raise
 ``svfsim.SvfError`` (``SVF_EINVAL``); what lengths, offsets and page numbers in
 device memory do is said in ``svfkv.h``.
 """
@@ -167,6 +168,12 @@ def _call(fn, dev: int, *packed: bytes):
         _check(rc)
 
 
+def _gradient():
+    """Called where a tensor requires a gradient, which would be lost without a word."""
+    _need(not torch.is_grad_enabled(),
+          "these calls have no backward pass: tensors must not require a gradient (or use torch.no_grad())")
+
+
 def _raw_stream(dev: int) -> int:
     return torch.cuda.current_stream(dev).cuda_stream
 
@@ -189,6 +196,9 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     ``q``).  ``rope`` is a table of ``rope_table`` (None: nothing is rotated);
     its width is the rotated part of a head.  Views with any strides of
     tokens and heads are taken, such as the parts of one projection's output."""
+    if (q.requires_grad or k.requires_grad or v.requires_grad or cache.k.requires_grad or cache.v.requires_grad
+            or (rope is not None and rope.requires_grad) or (q_out is not None and q_out.requires_grad)):
+        _gradient()
     kind, kv_heads = _kind(cache)
     dev = kind[1]
     qt, qh = _rows(q, "q", *kind)
@@ -229,6 +239,10 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     slots up to its own.  ``add_weight`` adds every slot's softmax, summed
     over the tokens and the query heads that share its key head, to
     ``cache.weight``.  A token that sees no slot has out = 0, lse = -inf."""
+    if (q.requires_grad or cache.k.requires_grad or cache.v.requires_grad
+            or (add_weight and cache.weight is not None and cache.weight.requires_grad)
+            or (out is not None and out.requires_grad)):
+        _gradient()
     kind, _ = _kind(cache)
     qt, qh = _rows(q, "q", *kind)
     if batch.q_offsets is None:
@@ -262,6 +276,8 @@ def evict(batch: Batch, cache: Cache, budget: int, recent: int, next_position: t
     before ``next_position`` (int32 [seqs]) and the rest by largest ``cache.weight``
     (ties to the lower slot).  Rows move inside the cache; returns the new lengths."""
     k, kv_len = cache.k, batch.kv_len
+    if k.requires_grad or cache.v.requires_grad or (cache.weight is not None and cache.weight.requires_grad):
+        _gradient()
     kv, seqs = _pack(cache, batch, 0)
     if cache.weight is None or cache.position is None:
         _need(False, "evict needs the cache's weight and position")

@@ -113,3 +113,36 @@ def test_launches_of_too_many_threads_are_refused():
     assert "too large" in refused(lib.svf_kv_attend, cache(), seqs, attend(heads=2, out=A + (1 << 60), workspace_bytes=1 << 62))
     # one less is within the limits, as far as the workspace goes
     assert lib.svf_kv_attend_workspace(cache(), batch(num_seqs=1 << 20, num_tokens=1 << 20, max_q=100), attend(heads=2)) > 0
+
+
+def host_call(name, grad):
+    """A call with host tensors of which ``grad`` requires a gradient; refused either way, by this check or by the next."""
+    x = {n: torch.zeros(shape, dtype=torch.bfloat16) for n, shape in
+         (("q", (1, 8, 128)), ("k", (1, 2, 128)), ("v", (1, 2, 128)), ("out", (1, 8, 128)), ("keys", (4, 2, 16, 128)),
+          ("values", (4, 2, 16, 128)))}
+    x["weight"], x["rope"] = torch.zeros((4, 2, 16)), torch.zeros((9, 128))
+    if grad:
+        x[grad].requires_grad_()
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    b = C.Batch(ints(0, 1), ints(5), ints(0)[None], 1)
+    held = C.Cache(x["keys"], x["values"], x["weight"], torch.zeros((4, 2, 16), dtype=torch.int32))
+    with pytest.raises(S.SvfError) as e:
+        if name == "append":
+            C.append(x["q"], x["k"], x["v"], ints(4), x["rope"], b, held, q_out=x["out"])
+        elif name == "attend":
+            C.attend(x["q"], b, held, add_weight=True, out=x["out"])
+        else:
+            C.evict(b, held, 4, 1, ints(5))
+    assert e.value.name == "SVF_EINVAL"
+    return "backward" in str(e.value)
+
+
+@pytest.mark.parametrize("name,tensors", [("append", ("q", "k", "v", "rope", "keys", "values", "out")),
+                                          ("attend", ("q", "keys", "values", "weight", "out")),
+                                          ("evict", ("keys", "values", "weight"))])
+def test_gradients_are_refused_where_they_would_be_lost(name, tensors):
+    for x in tensors:
+        assert host_call(name, x), x
+        with torch.no_grad():
+            assert not host_call(name, x), x
+    assert not host_call(name, None)
