@@ -144,6 +144,7 @@ int svf_kv_append(const svf_kv_cache *cache, const svf_kv_batch *batch,
  * lse = -inf.  What lies in slots that a row does not see, NaN and infinities
  * among it, has no effect on that row; an infinite or NaN element of a value that it
  * sees decides its output however small the slot's softmax is.
+ *   scale       finite, below 2^127
  *   add_weight  1: weight[j] += the sum of slot j's softmax over the tokens and
  *               the query heads of its key head (in an order that is the same
  *               every time).  Each page at most once in the batch then.

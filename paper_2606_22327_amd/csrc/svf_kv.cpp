@@ -231,7 +231,8 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     if (!stride_ok(a->out_token_stride) || !stride_ok(a->out_head_stride) || a->out_token_stride % 8 ||
         a->out_head_stride % 8)
         return fail(SVF_EINVAL, "strides of out must be multiples of 8, 0 .. 2^40");
-    if (!(a->scale == a->scale)) return fail(SVF_EINVAL, "scale must be a number");
+    const float scale = a->scale * 1.4426950408889634f;  // for powers of two
+    if (!(scale - scale == 0.f)) return fail(SVF_EINVAL, "scale must be a finite number below 2^127");
     if (a->add_weight && !c->weight && c->num_pages > 0) return fail(SVF_EINVAL, "add_weight needs the cache's weight");
     if (b->num_tokens == 0 || b->num_seqs == 0) return SVF_OK;
     if (!b->q_offsets || !a->q || !a->out || !a->lse) return fail(SVF_EINVAL, "q_offsets, q, out and lse must not be NULL");
@@ -249,7 +250,7 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     k.ws = static_cast<char*>(a->workspace);
     k.q_tok = a->q_token_stride * 2, k.q_head = a->q_head_stride * 2;
     k.o_tok = a->out_token_stride * 2, k.o_head = a->out_head_stride * 2;
-    k.scale = a->scale * 1.4426950408889634f;
+    k.scale = scale;
     k.heads = a->heads;
     k.causal = a->causal != 0;
     // a window as wide as the table hides nothing, and a slot less than it is still an int

@@ -109,11 +109,18 @@ def _pack(cache: Cache, batch: Batch, tokens: int) -> Tuple[bytes, bytes]:
     stride = table.stride(0)
     if seqs < 2 and stride < width:
         stride = width
-    return (_CACHE.pack(k.data_ptr(), v.data_ptr(), 0 if weight is None else weight.data_ptr(),
-                        0 if position is None else position.data_ptr(), ks[0], ks[1], ks[2],
-                        vs[0], vs[1], vs[2], pages, size, heads, dim, DTYPE[dtype]),
-            _BATCH.pack(0 if offsets is None else offsets.data_ptr(), kv_len.data_ptr(), table.data_ptr(), stride,
-                        seqs, tokens, width, max_q))
+    try:
+        return (_CACHE.pack(k.data_ptr(), v.data_ptr(), 0 if weight is None else weight.data_ptr(),
+                            0 if position is None else position.data_ptr(), ks[0], ks[1], ks[2],
+                            vs[0], vs[1], vs[2], pages, size, heads, dim, DTYPE[dtype]),
+                _BATCH.pack(0 if offsets is None else offsets.data_ptr(), kv_len.data_ptr(), table.data_ptr(), stride,
+                            seqs, tokens, width, max_q))
+    except struct.error as e:
+        raise _no_fit(e, "max_q and the sizes of tensors") from None
+
+
+def _no_fit(e: struct.error, what: str) -> svfsim.SvfError:
+    return svfsim.SvfError(-1, f"{what} must be 32-bit integers ({e})")
 
 
 def _refuse(cache: Cache, batch: Batch):
@@ -259,7 +266,10 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     fixed = (qt, qh, ot, oh, scale, heads, bool(causal), int(window), bool(add_weight))
     at = (q.data_ptr(), out.data_ptr(), lse.data_ptr())
     lib = svfsim.load()
-    a = _ATTEND.pack(*at, 0, 0, *fixed)
+    try:
+        a = _ATTEND.pack(*at, 0, 0, *fixed)
+    except struct.error as e:
+        raise _no_fit(e, "window and heads") from None
     need = lib.svf_kv_attend_workspace(kv, seqs, a)
     ws = None
     if need:
@@ -287,7 +297,11 @@ def evict(batch: Batch, cache: Cache, budget: int, recent: int, next_position: t
     new_len = torch.empty_like(kv_len)
     fixed = (int(budget), int(recent), int(first))
     lib = svfsim.load()
-    need = lib.svf_kv_evict_workspace(kv, seqs, _EVICT.pack(0, 0, 0, 0, *fixed))
+    try:
+        a = _EVICT.pack(0, 0, 0, 0, *fixed)
+    except struct.error as e:
+        raise _no_fit(e, "budget, recent and first") from None
+    need = lib.svf_kv_evict_workspace(kv, seqs, a)
     ws = _workspace(need, k)
     a = _EVICT.pack(next_position.data_ptr(), new_len.data_ptr(), ws.data_ptr() if need else 0, need, *fixed)
     _call(lib.svf_kv_evict, k.get_device(), kv, seqs, a)

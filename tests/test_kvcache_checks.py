@@ -146,3 +146,25 @@ def test_gradients_are_refused_where_they_would_be_lost(name, tensors):
         with torch.no_grad():
             assert not host_call(name, x), x
     assert not host_call(name, None)
+
+
+@pytest.mark.parametrize("scale", [float("inf"), -float("inf"), 1e300, 3e38])
+def test_scales_that_are_not_finite_in_32_bits_are_refused(scale):
+    assert "scale" in refused(S.load().svf_kv_attend, cache(), batch(), attend(scale=scale))
+
+
+@pytest.mark.gpu
+def test_numbers_past_32_bits_are_refused_as_arguments():
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    k = torch.zeros((4, 2, 16, 128), dtype=torch.bfloat16, device="cuda")
+    held = C.Cache(k, k.clone(), torch.zeros((4, 2, 16), device="cuda"), torch.zeros((4, 2, 16), dtype=torch.int32, device="cuda"))
+    b, q = C.Batch(ints(0, 1), ints(20), ints(0, 1)[None], 1), torch.zeros((1, 8, 128), dtype=torch.bfloat16, device="cuda")
+    calls = [lambda: C.attend(q, b, held, window=2 ** 31), lambda: C.attend(q, b._replace(max_q=2 ** 40), held),
+             lambda: C.attend(q, b._replace(max_q=1.5), held), lambda: C.attend(q, b, held, scale=1e300),
+             lambda: C.evict(b, held, 2 ** 31, 0, ints(20)), lambda: C.evict(b, held, 10, -2 ** 31 - 1, ints(20)),
+             lambda: C.append(q, k[:1, :, 0], k[:1, :, 0], ints(0), None, b._replace(max_q=2 ** 40), held)]
+    for call in calls:
+        with pytest.raises(S.SvfError) as e:
+            call()
+        assert e.value.name == "SVF_EINVAL"
+    C.attend(q, b, held, window=2 ** 31 - 1)
