@@ -194,17 +194,9 @@ hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStrea
     if (wide) {
         const Wide w = wide_grid(a);
         const dim3 grid((unsigned)w.blocks);
-        if (dtype == SVF_KV_BF16)
-            k_append_wide<BF16><<<grid, 256, 0, s>>>(a, w.units, w.groups, w.per);
-        else
-            k_append_wide<F16><<<grid, 256, 0, s>>>(a, w.units, w.groups, w.per);
-    } else {
-        if (dtype == SVF_KV_BF16)
-            k_append_any<BF16><<<a.kv.tokens, 64, 0, s>>>(a);
-        else
-            k_append_any<F16><<<a.kv.tokens, 64, 0, s>>>(a);
+        return run(dtype == SVF_KV_BF16 ? k_append_wide<BF16> : k_append_wide<F16>, grid, 256, s, a, w.units, w.groups, w.per);
     }
-    return hipGetLastError();
+    return run(dtype == SVF_KV_BF16 ? k_append_any<BF16> : k_append_any<F16>, dim3(a.kv.tokens), 64, s, a);
 }
 
 }  // namespace svfk

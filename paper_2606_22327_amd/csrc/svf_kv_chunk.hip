@@ -744,26 +744,23 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         plan.part = (float*)(ws + 256 + plan.groups / 2 * sizeof(Item));
     }
     const ChunkGrids g = grids(z, a.few);
+    hipError_t e;
     if (g.blocks > 0) {
         // Offsets of sixteen rows are 32 bits.
         const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
-        if (z.page_size >= 16 && far < (int64_t(1) << 31))
-            k_attend_chunk<E, D, true><<<(unsigned)g.blocks, 256, 0, s>>>(a, plan);
-        else
-            k_attend_chunk<E, D, false><<<(unsigned)g.blocks, 256, 0, s>>>(a, plan);
-    }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (plan.groups) {
-        k_join_chunk<E, D><<<plan.groups / 2 * (kRows / 8), 256, 0, s>>>(a, plan);
-        e = hipGetLastError();
+        const bool wide = z.page_size >= 16 && far < (int64_t(1) << 31);
+        e = run(wide ? k_attend_chunk<E, D, true> : k_attend_chunk<E, D, false>, dim3((unsigned)g.blocks), 256, s, a, plan);
         if (e != hipSuccess) return e;
     }
-    if (g.tiles > 0) k_weight_chunk<E, D><<<(unsigned)g.tiles, 256, 0, s>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (g.more > 0) k_weight_chunk_more<E, D><<<(unsigned)g.more, 256, 0, s>>>(a, g.tiles / z.kv_heads);
-    return hipGetLastError();
+    if (plan.groups) {
+        e = run(k_join_chunk<E, D>, dim3(plan.groups / 2 * (kRows / 8)), 256, s, a, plan);
+        if (e != hipSuccess) return e;
+    }
+    if (g.tiles > 0) {
+        e = run(k_weight_chunk<E, D>, dim3((unsigned)g.tiles), 256, s, a);
+        if (e != hipSuccess) return e;
+    }
+    return g.more > 0 ? run(k_weight_chunk_more<E, D>, dim3((unsigned)g.more), 256, s, a, g.tiles / z.kv_heads) : hipSuccess;
 }
 
 }  // namespace

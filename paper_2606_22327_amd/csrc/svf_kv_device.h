@@ -8,6 +8,19 @@
 
 namespace svfk {
 
+// A launch with its own error: hipGetLastError would also report one that a call before has left.
+template <class X>
+struct As {
+    typedef X Type;
+};
+template <class... P>
+inline hipError_t run(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t s, typename As<P>::Type... args) {
+    void* at[] = {&args...};
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, s);
+    if (e != hipSuccess) (void)hipGetLastError();  // reported here
+    return e;
+}
+
 // A load that the compiler knows to be of global memory, whatever the address was chosen from.
 template <class V>
 __device__ inline V load_global(uint64_t at) {

@@ -237,23 +237,14 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     int2* pairs = (int2*)(a.ws + (((int64_t)segs * 4 + 255) & ~int64_t(255)));
     // Up to 4,096 slots four workgroups of a CU side by side (64 prompts of 1,033 to 4,068 slots: 256 threads each 103 us,
     // 512 threads 95, 1,024 threads 99); longer ones one, with up to 28,672 keys in 112 KB of its LDS.
-    if (pairs_max <= kOwnPairs) {
-        if (cap <= 4096)
-            k_evict_select<512, 4096, true><<<segs, 512, 0, s>>>(a, pairs_max, pairs, counts);
-        else
-            k_evict_select<1024, 28672, true><<<segs, 1024, 0, s>>>(a, pairs_max, pairs, counts);
-        return hipGetLastError();
-    }
-    if (cap <= 4096)
-        k_evict_select<512, 4096, false><<<segs, 512, 0, s>>>(a, pairs_max, pairs, counts);
-    else
-        k_evict_select<1024, 28672, false><<<segs, 1024, 0, s>>>(a, pairs_max, pairs, counts);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    const bool move = pairs_max <= kOwnPairs;
+    const hipError_t e =
+        cap <= 4096 ? run(move ? k_evict_select<512, 4096, true> : k_evict_select<512, 4096, false>, dim3(segs), 512, s, a, pairs_max, pairs, counts)
+                    : run(move ? k_evict_select<1024, 28672, true> : k_evict_select<1024, 28672, false>, dim3(segs), 1024, s, a, pairs_max, pairs, counts);
+    if (e != hipSuccess || move) return e;
     const int64_t blocks = (pairs_max + kMoveRows - 1) / kMoveRows;
     const unsigned y = (unsigned)(blocks < 1 ? 1 : blocks > 4096 ? 4096 : blocks);
-    k_evict_move<<<dim3(segs, y), 256, 0, s>>>(a, pairs_max, pairs, counts);
-    return hipGetLastError();
+    return run(k_evict_move, dim3(segs, y), 256, s, a, pairs_max, pairs, counts);
 }
 
 }  // namespace svfk

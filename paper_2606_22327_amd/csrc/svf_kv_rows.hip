@@ -606,22 +606,19 @@ __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan
 }
 
 template <class E, int D, bool WIDE>
-void launch_tiles(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
-    if (plan.rows <= 16)
-        k_attend_rows<E, D, 1, WIDE><<<plan.groups, 256, 0, s>>>(a, plan);
-    else if constexpr (D <= 128)
-        k_attend_rows<E, D, 2, WIDE><<<plan.groups, 256, 0, s>>>(a, plan);
+hipError_t launch_tiles(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
+    if constexpr (D <= 128) {
+        if (plan.rows > 16) return run(k_attend_rows<E, D, 2, WIDE>, dim3(plan.groups), 256, s, a, plan);
+    }
+    return run(k_attend_rows<E, D, 1, WIDE>, dim3(plan.groups), 256, s, a, plan);
 }
 
 template <class E, int D>
 hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
     // Offsets of sixteen rows are 32 bits.
     const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
-    if (a.kv.shift >= 4 && far < (int64_t(1) << 31))
-        launch_tiles<E, D, true>(a, plan, s);
-    else
-        launch_tiles<E, D, false>(a, plan, s);
-    hipError_t e = hipGetLastError();
+    const bool wide = a.kv.shift >= 4 && far < (int64_t(1) << 31);
+    hipError_t e = wide ? launch_tiles<E, D, true>(a, plan, s) : launch_tiles<E, D, false>(a, plan, s);
     if (e != hipSuccess) return e;
     const int64_t cap = (int64_t)a.kv.width << a.kv.shift;
     if (cap > kUnit && plan.groups > 1) {  // else no row has a second unit
@@ -632,12 +629,11 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
         while (!many && parts > 1 && 8 / parts < plan.rows) parts >>= 1;
         const int64_t heads = (int64_t)a.kv.seqs * a.kv.kv_heads;
         const bool by_head = heads < plan.groups - 1;
-        k_join_rows<E, D><<<dim3((unsigned)(by_head ? heads : plan.groups - 1), many ? plan.rows : 1), 256, 0, s>>>(a, plan, parts, by_head);
-        e = hipGetLastError();
+        e = run(k_join_rows<E, D>, dim3((unsigned)(by_head ? heads : plan.groups - 1), many ? plan.rows : 1), 256, s, a, plan, parts, by_head);
         if (e != hipSuccess) return e;
     }
-    if (a.add_weight && plan.score_units > 0) k_weight_rows<E, D><<<(unsigned)((plan.score_units + 3) / 4), 256, 0, s>>>(a, plan);
-    return hipGetLastError();
+    return a.add_weight && plan.score_units > 0 ? run(k_weight_rows<E, D>, dim3((unsigned)((plan.score_units + 3) / 4)), 256, s, a, plan)
+                                                : hipSuccess;
 }
 
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t(255); }

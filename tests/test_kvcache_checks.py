@@ -168,3 +168,25 @@ def test_numbers_past_32_bits_are_refused_as_arguments():
             call()
         assert e.value.name == "SVF_EINVAL"
     C.attend(q, b, held, window=2 ** 31 - 1)
+
+
+@pytest.mark.gpu
+def test_an_error_that_another_call_has_left_is_not_these_calls():
+    import ctypes
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    k = torch.randn((4, 2, 16, 128), device="cuda").to(torch.bfloat16)
+    held = C.Cache(k, k.clone(), torch.zeros((4, 2, 16), device="cuda"), torch.zeros((4, 2, 16), dtype=torch.int32, device="cuda"))
+    b, q = C.Batch(ints(0, 1), ints(20), ints(0, 1)[None], 1), torch.randn((1, 8, 128), device="cuda").to(torch.bfloat16)
+    many = C.Batch(ints(0, 20), ints(20), ints(0, 1)[None], 20)
+    qs, new = q.expand(20, 8, 128).contiguous(), ints(20)
+    hip = S.load()
+    hip.hipSetDevice.argtypes = [ctypes.c_int]
+    for call in (lambda: C.attend(q, b, held, add_weight=True), lambda: C.attend(qs, many, held, add_weight=True),
+                 lambda: C.append(q, k[:1, :, 3], k[:1, :, 3], ints(0), None, b, held), lambda: C.evict(b, held, 10, 0, new)):
+        call()                                          # torch has what it hands out, and asks for no more
+        torch.cuda.synchronize()
+        assert hip.hipSetDevice(1 << 20) != 0           # refused; leaves its error for whoever asks
+        try:
+            call()
+        finally:
+            hip.hipGetLastError()
