@@ -10,12 +10,13 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // Sixteen 16-bit elements' worth of a matrix product, and the type's constants.
-// kShift: probabilities are scaled by 2^kShift, which cancels against their sum,
-// so that the small ones of a 16-bit float stay above its subnormal numbers.
+// kShift: probabilities are scaled by 2^kShift, which cancels against their sum: float16's up, so that the
+// small ones stay above its subnormal numbers, bfloat16's down, so that sums of values as large as the
+// type has stay finite in 32 bits before they are divided (2^24 of them with kSlack).
 // kSlack: powers of two by which a row's scores may pass the maximum that its
 // probabilities are taken against before the row's sums are scaled down to a new one.
 struct BF16M : BF16 {
-    static constexpr float kShift = 0.f;
+    static constexpr float kShift = -32.f, kUnshift = 4294967296.f;
     static constexpr uint16_t kInf = 0x7f80;
     static constexpr float kSlack = 8.f;
     // Two numbers, each as the sum of two of the type, as words of two: the upper 16 bits of each, and what is left, rounded.
@@ -29,7 +30,7 @@ struct BF16M : BF16 {
     static __device__ inline f32x16 mfma32(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16M : F16 {
-    static constexpr float kShift = 14.f;
+    static constexpr float kShift = 14.f, kUnshift = 1.f / 16384.f;
     static constexpr uint16_t kInf = 0x7c00;
     static constexpr float kSlack = 1.f;
     static __device__ inline void split(float a, float b, uint32_t& hi, uint32_t& low) {
@@ -122,7 +123,7 @@ __device__ inline void write_row(const AttendArgs& p, int token, int h, int d0, 
 #pragma unroll
     for (int j = 0; j < N; j++) v[j] = (T)(den == 0.f ? 0.f : acc[j] * inv);
     *(V*)(p.out + token * p.o_tok + h * p.o_head + d0 * 2) = v;
-    if (d0 == 0) p.lse[(int64_t)token * p.heads + h] = (top - E::kShift + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
+    if (d0 == 0) p.lse[(int64_t)token * p.heads + h] = (top + __builtin_amdgcn_logf(den * E::kUnshift)) * 0.69314718055994531f;
 }
 
 // Rows of one key head of a sequence that has more new tokens than it may.

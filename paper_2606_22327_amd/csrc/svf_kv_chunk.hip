@@ -476,7 +476,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         if (to)
             to[D] = m, to[D + 1] = l;
         else
-            z.lse[(int64_t)(s.q0 + t) * z.heads + hq] = (m - E::kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+            z.lse[(int64_t)(s.q0 + t) * z.heads + hq] = (m + __builtin_amdgcn_logf(l * E::kUnshift)) * 0.69314718055994531f;
     }
 }
 

@@ -145,3 +145,16 @@ def test_rows_of_infinitely_small_scores_are_zero_whatever_their_values(dtype, l
     out, lse = C.attend(s["q"].cuda(), C.Batch(s["offsets"].cuda(), s["kv_len"].cuda(), s["table"].cuda(), new),
                         C.Cache(s["k"].cuda(), s["v"].cuda()))
     assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("length,new", [(100, 1), (3000, 1), (300, 40), (3000, 40)])
+def test_values_at_the_types_limit(dtype, length, new):
+    """Means of the type's largest numbers are finite, sums before they are divided must be as well."""
+    s = make(55, [length], [new], 4, 1, 64, 16, dtype)
+    pg, row = P.slots_of(s["table"], 0, length, 16, s["k"].shape[0])
+    s["v"][pg, 0, row, 7] = torch.finfo(dtype).max
+    s["v"][pg, 0, row, 8] = torch.finfo(dtype).min
+    out, _, _ = check_attend(s)
+    assert (out[..., 7] == torch.finfo(dtype).max).all() and (out[..., 8] == torch.finfo(dtype).min).all()
