@@ -27,7 +27,7 @@
  *     device memory cannot be: there, lengths are cut to [0, table_width *
  *     page_size], offsets to [0, num_tokens], and a slot whose page number is outside
  *     [0, num_pages) is not there (never written, invisible to attention,
- *     evicted first).
+ *     evicted before any with a weight).
  *   - A launch has fewer than 2^32 threads; sizes that need more are refused
  *     (some 2^26 tokens in svf_kv_append, 2^22 sequences times key heads in svf_kv_evict,
  *     2^31 rows or 2^24 sequences times key heads with chunks in svf_kv_attend).
@@ -182,12 +182,13 @@ const char *svf_kv_last_error(void);
  * head for itself.  Kept are the slots of the ``first`` lowest positions of the
  * text (position < first), of the ``recent`` newest tokens (position >=
  * next_position[i] - recent), and of the others those of largest weight; ties
- * go to the lower slot, NaN counts as less than any weight.  (first + recent
+ * go to the lower slot; NaN counts as less than any weight, a slot without a
+ * page as NaN.  (first + recent
  * <= budget.  Should positions repeat, so that more are protected, the lower
  * slots of those stay.)  The kept slots at or above the budget, in rising
  * order, move into the slots below it that are not kept, in rising order: key,
- * value, weight and position.  Slots at or above the budget keep what they
- * held.  Each page at most once in the batch.
+ * value, weight and position (where the place has no page, they are lost).  Slots
+ * at or above the budget keep what they held.  Each page at most once in the batch.
  *   next_position  int32 [num_seqs]: the position that the next token will have
  *   new_len        int32 [num_seqs]: min(kv_len, budget); not kv_len itself
  *   workspace      svf_kv_evict_workspace bytes, 256-byte aligned

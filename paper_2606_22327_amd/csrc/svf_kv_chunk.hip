@@ -101,13 +101,14 @@ __device__ inline int swizzle(int row) {
 // Keys and values go from memory straight to LDS, the next tile's while this one is worked on.
 //
 // The probabilities enter the second product as the sum of two numbers of the type, as with few rows: in one, their rounding would be an
-// error of the size of the output's own (2.3e-3 in place of 1.7e-3 of the outputs' norm in bfloat16, for 412 us in place of 518 of
+// error of the size of the output's own (2.3e-3 in place of 1.7e-3 of the outputs' norm in bfloat16, for 412 us in place of 512 of
 // six prompts).  A row's maximum is followed only when it has grown by more than kSlack.
 //
-// The products bound it: 2,048 tokens behind 12,001 (32 query heads on 8 key heads of 128 dimensions, 437 GFLOP) take
-// 460 us, 950 TFLOP/s where a large product of the library reaches 1,350; six prompts of 1,084 to 3,930 tokens 400 us,
-// 870 TFLOP/s.  Of a tile's time about a tenth goes to its loads' latency, the rest of what is missing to exponentials and
-// the waits between the two products, which two waves a SIMD do not fill.
+// Products and exponentials bound it together: 2,048 tokens behind 12,001 (32 query heads on 8 key heads of 128 dimensions, 437 GFLOP,
+// 656 with the second product's two halves) take 590 us, six prompts of 1,084 to 3,930 tokens (348, 522 with both) 505 us in a row of
+// calls and 549 under the profiler: 950 to 1,110 TFLOP/s of products carried out, where a large one of the library reaches 1,350.
+// Counters of the prompts: the matrix units are busy for 0.48 of the cycles, other vector instructions take 0.36 at four cycles
+// each, and exponentials, at sixteen, 0.12 more; two waves a SIMD do not fill the waits between.
 // WIDE: pages of 16 slots or more, so that the sixteen slots that a wave fetches lie in one page: their address is the same for
 // the whole wave but for an offset that stays the same all along (a tile costs a wave 8 loads and some scalar
 // instructions, and 100 vector instructions otherwise).
@@ -154,7 +155,9 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     int hi = p.causal ? min(s.len, r0 + last_row / G + 1) : s.len;
     int tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
     if (parts > 1) {
-        // no part of fewer than four tiles: it would cost more to join than it saves
+        // No part of fewer than four tiles: it would cost more to join than it saves.  (40 tokens of 32 query heads on 8 key heads behind
+        // 2,000 slots: parts of one tile and more 28.0 us, of two 23.0, of four 21.8, of eight 26.1; behind 4,000: 28.8, 30.2, 27.5,
+        // 30.1; behind 500, where one is best: 17.6, 18.5, 21.2, 26.6.)
         parts = max(1, min(parts, tiles / 4));
         if (part >= parts) return;
         if (part == 0 && tid == 0) plan.item[item] = Item{s.q0, first_row, rows, parts};
@@ -510,8 +513,9 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // The weights of these sequences' slots: scores once more, now against the rows' final statistics.
 // A workgroup has 256 slots, 64 for each wave, whose keys stay in registers while the rows'
 // queries pass through LDS, 64 at a time; a lane sums its own rows for 32 slots and the lanes
-// are added at the end, so nothing is added atomically.  The exponentials bound it: 2,048 tokens over 14,049 slots
-// of 8 key heads (32 query heads, 218 GFLOP, 8.5e8 exponentials) take 350 us.
+// are added at the end, so nothing is added atomically.  2,048 tokens over 14,049 slots of 8 key heads (32 query heads, 218
+// GFLOP, 8.5e8 exponentials) take 326 us; nothing bounds it alone: the matrix units are busy for 0.27 of the cycles, other vector
+// instructions take 0.33, exponentials 0.2 more, and products and exponentials of a tile follow each other.
 constexpr int kWSlots = 256, kWRows = 64;
 
 __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {

@@ -44,9 +44,9 @@ __device__ inline int units_of(const AttendArgs& p, const Seq& s, int rows) {
 // values while the next one's are.
 //
 // Keys and values, read once, bound it: 127 sequences of up to 900 slots (32 query heads on 8 key heads of
-// 128 dimensions, 249 MB) take 59 us, 4.2 TB/s where a kernel that only reads reaches 6.2; one sequence of
-// 65,535 slots (134 MB) 27 us.  What is left is the start of each key head's run, two of them in a
-// workgroup's seven units in the first case.
+// 128 dimensions, 249 MB) take 60 us, 4.1 TB/s where a kernel that only reads reaches 6.2; 64 sequences of 2,000 slots
+// 5.7 TB/s with all launches, one sequence of 65,535 slots (134 MB) 27 us.  What is left is the start of each key head's run, two of
+// them in a workgroup's seven units in the first case.  Not WIDE, pages of 8 slots 97 us where pages of 16 take 86, of one slot 105.
 template <class E, int D>
 struct Tile {
     typename E::V8 k[2][D / 32];
@@ -623,7 +623,11 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
     const int64_t cap = (int64_t)a.kv.width << a.kv.shift;
     if (cap > kUnit && plan.groups > 1) {  // else no row has a second unit
         // Few key heads are split over many workgroups: a row's parts over 8 groups of lanes, a workgroup for each
-        // row.  Many are split over two or three: a workgroup for all rows, its groups on as many rows as there are.
+        // row (one sequence of 65,535 slots on 4 key heads: 32.4 us, the other way 39.3).  Many are split over two or three: a workgroup
+        // for all rows, its groups on as many rows as there are (16 sequences of 4,000 slots with 8 new tokens: 56.9 us, the
+        // other way 65.1; 127 sequences of up to 900 slots: 65.1 and 69.5).
+        // A workgroup for each key head where those are fewer than the boundaries between workgroups, which need a search: 4 sequences of
+        // 16,000 slots 53.1 us by key head and 54.8 by boundary, 127 sequences 66.4 and 65.2.
         const bool many = plan.groups >= 8 * (int64_t)a.kv.seqs * a.kv.kv_heads;
         int parts = 8;
         while (!many && parts > 1 && 8 / parts < plan.rows) parts >>= 1;
@@ -670,8 +674,9 @@ Layout layout(const AttendSizes& z) {
 }  // namespace
 
 // Rows that these kernels take: a whole batch's where no sequence has more than 32 (16 of 256 dimensions), else
-// single tokens' (or 16, whichever is more).  With 32 query heads on 8 key heads of 128 dimensions and 8 sequences of
-// 8,000 slots, 20 rows take 63 us here and 71 as a tile of 128 rows, 40 rows 75 and 72, 64 rows 82 and 72.
+// single tokens' (or 16, whichever is more).  8 sequences of 8,000 slots, here and as a tile of 128 rows: 32 query heads on 8 key heads
+// of 128 dimensions, 20 rows 57 us and 75, 32 rows 58 and 68; of 64 dimensions, 20 rows 42 and 45, 32 rows 45 and 44; of 256
+// dimensions, 16 rows 103 and 142.  More rows than that would need registers that a wave does not have.
 int32_t few_rows(const AttendSizes& z) {
     const int32_t G = z.heads / z.kv_heads, most = z.dim <= 128 ? 32 : 16;
     const int64_t want = (int64_t)z.max_q * G;
