@@ -259,13 +259,6 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             }
         }
     };
-    // The marks of two values of a slot for the rows that see it.
-    auto mark = [&](int j, int w, uint32_t marks) {
-        for (int y = 0; y <= last_row - first_row; y++) {
-            const int t = r0 + (first_row + y) / G;
-            if ((!p.causal || j <= t) && (p.window == 0 || j > t - p.window)) atomicOr(&odd_marks[y][w >> 3], marks << 4 * (w & 7));
-        }
-    };
     // Where the tile's rows do not all see the same slots, a value that is no finite number would reach those
     // that do not see it (0 times infinity): it counts as 0, and the rows that see it get it
     // from their marks.  Each wave looks through the values of sixteen slots.
@@ -281,7 +274,12 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             if (!odd_pair<E>(pair)) continue;
             const int r = wave * 16 + (x + lane) / (D / 2), at = (x + lane) % (D / 2);
             const int w = ((at >> 2) ^ swizzle<D>(r)) * 4 + (at & 3);  // the dimensions 2 w and 2 w + 1
-            if (there >> r & 1) mark(base + r, w, odd_marks_of<E>(pair));
+            const uint32_t marks = odd_marks_of<E>(pair) << 4 * (w & 7);
+            for (int y = 0; y <= last_row - first_row; y++) {
+                const int t = r0 + (first_row + y) / G;
+                if ((there >> r & 1) && (!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window))
+                    atomicOr(&odd_marks[y][w >> 3], marks);
+            }
             words[x] = finite_pair<E>(pair);
         }
     };
@@ -433,8 +431,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     Call call = (Call)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(call));
     const AttendArgs& z = ((const ChunkCall*)call)->p;
-    // Rows with a sum that is no finite number (0 times a finite one is 0), though the row's own sum of probabilities is one: which values
-    // that are none the rows see.
+    // Rows with a sum that is no finite number (0 times a finite one is 0), though the row's own sum of probabilities is one: a tile that
+    // all rows see has a value that is none. Each thread looks through two dimensions of the slots that all rows see.
     float zero = 0.f;
 #pragma unroll
     for (int d = 0; d < DT; d++)
@@ -442,12 +440,16 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
     if (__syncthreads_or(zero != 0.f && l * 0.f == 0.f)) {
         const int w = tid % (D / 2);  // the dimensions 2 w and 2 w + 1
-        for (int j = lo + tid / (D / 2); j < hi; j += 256 / (D / 2)) {
+        const int first = max(lo, block_from), end = min(hi - 1, block_last) + 1;
+        uint32_t marks = 0;
+#pragma unroll 8
+        for (int j = first + tid / (D / 2); j < end; j += 256 / (D / 2)) {
             const int at = entry_row(z.kv, table_entry(z.kv, table, j), j, true);
-            if (at < 0) continue;
-            const uint32_t pair = load_global<uint32_t>(vbase + row_offset(at, z.kv.shift, z.kv.v_page, z.kv.v_row) + w * 4);
-            if (odd_pair<E>(pair)) mark(j, w, odd_marks_of<E>(pair));
+            const uint64_t from = at < 0 ? (uint64_t)zero_row() : vbase + row_offset(at, z.kv.shift, z.kv.v_page, z.kv.v_row);
+            marks |= odd_marks_of<E>(load_global<uint32_t>(from + w * 4));
         }
+        if (marks)
+            for (int y = 0; y < kRows; y++) atomicOr(&odd_marks[y][w >> 3], marks << 4 * (w & 7));
         __syncthreads();
     }
 

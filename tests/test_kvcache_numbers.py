@@ -158,3 +158,19 @@ def test_values_at_the_types_limit(dtype, length, new):
     s["v"][pg, 0, row, 8] = torch.finfo(dtype).min
     out, _, _ = check_attend(s)
     assert (out[..., 7] == torch.finfo(dtype).max).all() and (out[..., 8] == torch.finfo(dtype).min).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("length,new,window", [(700, 1, 0), (700, 100, 0), (3000, 40, 0), (3000, 40, 900), (700, 100, 100)])
+def test_values_that_are_no_numbers_all_over(dtype, length, new, window):
+    """Whole dimensions of them, of one kind and of two, over tiles that all rows see and tiles that some do not."""
+    s = make(56, [length], [new], 4, 1, 128, 16, dtype)
+    pg, row = P.slots_of(s["table"], 0, length, 16, s["k"].shape[0])
+    for d, what in ((3, math.nan), (4, math.inf), (77, -math.inf)):
+        s["v"][pg, 0, row, d] = what
+    s["v"][pg[::2], 0, row[::2], 126] = math.inf
+    s["v"][pg[1::2], 0, row[1::2], 126] = -math.inf
+    out, _, _ = check_attend(s, window=window)
+    assert out[..., 3].isnan().all() and (out[..., 4] == math.inf).all() and (out[..., 77] == -math.inf).all() and out[..., 126].isnan().all()
+    assert torch.isfinite(out[..., :3]).all() and torch.isfinite(out[..., 127]).all()
