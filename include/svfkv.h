@@ -133,6 +133,27 @@ int svf_kv_append(const svf_kv_cache *cache, const svf_kv_batch *batch,
                   const svf_kv_append_args *args, void *hip_stream);
 
 /*
+ * The same for positions with several axes (time, height and width of an image's or a video's tokens): pair p
+ * of a head turns by row positions[t][of_pair[p]] of the table, and its cosine and sine are columns p and
+ * rot/2 + p of that row.  A position outside the table makes NaN of the pairs that turn by it and of no others.
+ *   positions   (of svf_kv_append_args) element (t, axis) at positions[t * token_stride + axis * axis_stride]
+ *   of_pair     the axis of each of the rot/2 pairs, below ``axes``
+ *   kept        int32 [num_tokens]: what the cache's position is set to, for eviction goes by the order of
+ *               the text; NULL: axis 0's position
+ */
+enum { SVF_KV_MOST_AXES = 4 };
+
+typedef struct svf_kv_axes {
+    const int32_t *kept;
+    int64_t token_stride, axis_stride;
+    int32_t axes;
+    uint8_t of_pair[128];
+} svf_kv_axes;
+
+int svf_kv_append_axes(const svf_kv_cache *cache, const svf_kv_batch *batch,
+                       const svf_kv_append_args *args, const svf_kv_axes *axes, void *hip_stream);
+
+/*
  * Attention of the new tokens over their sequences' slots.  Query head h
  * reads key head h / (heads / kv_heads).  Row (t, h) of sequence i, whose own
  * slot is r = kv_len - n + t, sees slot j if
@@ -168,6 +189,15 @@ typedef struct svf_kv_attend_args {
 
 int svf_kv_attend(const svf_kv_cache *cache, const svf_kv_batch *batch,
                   const svf_kv_attend_args *args, void *hip_stream);
+
+/*
+ * The same with first tokens that stay visible: row r also sees the slots j < first that its window
+ * hides (0 <= j < kv_len, j <= r when causal).  Slots that no row sees are not read, and the pages that hold nothing
+ * else may have been given back (no page there, a page number outside the pool).  Without a window, or where first is 0, it is
+ * svf_kv_attend; the workspace is that of svf_kv_attend.
+ */
+int svf_kv_attend_first(const svf_kv_cache *cache, const svf_kv_batch *batch,
+                        const svf_kv_attend_args *args, int32_t first, void *hip_stream);
 
 /* Bytes of workspace that svf_kv_attend needs for these sizes (only sizes
  * and add_weight are read); negative: the code of an error. */

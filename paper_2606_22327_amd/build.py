@@ -2,7 +2,7 @@
 
 The library holds every kernel of the simulator and the host runtime behind
 the C ABI of ``include/svfsim.h``, the paged cache's operators
-(``include/svfkv.h``) and the host-side exact optimum of tiny burst instances
+(``include/svfkv.h``), the scores of answers (``include/svflogprob.h``) and the host-side exact optimum of tiny burst instances
 (``include/svfopt.h``).  It is built in-tree so that the same file
 is loaded by the tests, the smoke check and the benchmark.
 """
@@ -26,7 +26,8 @@ GPU_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-mllvm", "-structurizecfg-skip-uniform-regions"]
 # The cache's kernels are ordinary vector code: the same without the branch flag.
 KV_GPU_FLAGS = GPU_FLAGS[:4]
-KV_KERNELS = ("svf_kv_append", "svf_kv_rows", "svf_kv_chunk", "svf_kv_evict")
+KV_KERNELS = ("svf_kv_append", "svf_kv_rows", "svf_kv_chunk", "svf_kv_evict", "svf_logprob")
+HOST = ("svf_kv", "svf_logprob_host", "svf_runtime", "svf_opt")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-I", INCLUDE, "-I", CSRC]
 
 
@@ -34,28 +35,31 @@ def _run(cmd):
     subprocess.check_call(cmd)
 
 
+def _run_all(cmds):
+    """Runs them side by side, at most one for each CPU; all have ended when it raises."""
+    running, failed, todo = [], None, list(cmds)
+    while running or todo:
+        while todo and failed is None and len(running) < max(1, min(os.cpu_count() or 1, 16)):
+            running.append((todo[0], subprocess.Popen(todo.pop(0))))
+        if not running:
+            break
+        cmd, p = running.pop(0)
+        if p.wait() != 0 and failed is None:
+            failed = subprocess.CalledProcessError(p.returncode, cmd)
+    if failed is not None:
+        raise failed
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    kern_o = os.path.join(BUILD, "svf_kernels.o")
-    rt_o = os.path.join(BUILD, "svf_runtime.o")
-    _run(["hipcc", f"--offload-arch={ARCH}", *COMMON, *GPU_FLAGS, "-c",
-          os.path.join(CSRC, "svf_kernels.hip"), "-o", kern_o])
-    na_o = os.path.join(BUILD, "svf_noalloc.o")
-    _run(["hipcc", f"--offload-arch={ARCH}", *COMMON, *GPU_FLAGS, "-c",
-          os.path.join(CSRC, "svf_noalloc.hip"), "-o", na_o])
-    kv_o = []
-    for name in KV_KERNELS:
-        kv_o.append(os.path.join(BUILD, name + ".o"))
-        _run(["hipcc", f"--offload-arch={ARCH}", *COMMON, *KV_GPU_FLAGS, "-c",
-              os.path.join(CSRC, name + ".hip"), "-o", kv_o[-1]])
-    kv_o.append(os.path.join(BUILD, "svf_kv.o"))
-    _run(["hipcc", *COMMON, "-c", os.path.join(CSRC, "svf_kv.cpp"), "-o", kv_o[-1]])
-    opt_o = os.path.join(BUILD, "svf_opt.o")
-    _run(["hipcc", *COMMON, "-c", os.path.join(CSRC, "svf_runtime.cpp"), "-o", rt_o])
-    _run(["hipcc", *COMMON, "-c", os.path.join(CSRC, "svf_opt.cpp"), "-o", opt_o])
+    gpu = [(name, KV_GPU_FLAGS) for name in KV_KERNELS] + [(name, GPU_FLAGS) for name in ("svf_kernels", "svf_noalloc")]
+    objects = [os.path.join(BUILD, name + ".o") for name in [n for n, _ in gpu] + list(HOST)]
+    _run_all([["hipcc", f"--offload-arch={ARCH}", *COMMON, *flags, "-c", os.path.join(CSRC, name + ".hip"),
+               "-o", os.path.join(BUILD, name + ".o")] for name, flags in gpu]
+             + [["hipcc", *COMMON, "-c", os.path.join(CSRC, name + ".cpp"), "-o", os.path.join(BUILD, name + ".o")]
+                for name in HOST])
     tmp = LIB + ".tmp"
-    _run(["hipcc", f"--offload-arch={ARCH}", "-shared", "-fPIC", kern_o, na_o, rt_o, opt_o, *kv_o,
-          "-pthread", "-o", tmp])
+    _run(["hipcc", f"--offload-arch={ARCH}", "-shared", "-fPIC", *objects, "-pthread", "-o", tmp])
     os.replace(tmp, LIB)
     if verbose:
         print(LIB)

@@ -132,18 +132,19 @@ int launched(hipError_t e) {
     return e == hipSuccess ? SVF_OK : fail(SVF_EHIP, "kernel launch: %s", hipGetErrorString(e));
 }
 
-AttendSizes sizes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
+AttendSizes sizes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first = 0) {
     return {c->num_pages,  c->page_size, c->kv_heads,    a->heads, c->head_dim, c->dtype,
-            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0};
+            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0, first};
 }
 
-int check_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
+int check_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first = 0) {
     if (int rc = check_sizes(c, b)) return rc;
     if (!a) return fail(SVF_EINVAL, "args must not be NULL");
     if (int rc = check_heads(c, a->heads)) return rc;
     if (a->window < 0) return fail(SVF_EINVAL, "window must be >= 0");
+    if (first < 0) return fail(SVF_EINVAL, "first must be >= 0");
     if ((int64_t)b->num_tokens * a->heads > kGridLimit) return fail(SVF_EINVAL, "num_tokens * heads is too large");
-    if (attend_threads(sizes(c, b, a)) >= kThreadLimit)
+    if (attend_threads(sizes(c, b, a, first)) >= kThreadLimit)
         return fail(SVF_EINVAL, "num_tokens * heads, num_seqs * kv_heads or the pool is too large for one launch");
     return SVF_OK;
 }
@@ -163,13 +164,8 @@ int64_t evict_bytes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_e
            segs * evict_pairs((int64_t)b->table_width * c->page_size, a->budget) * 8;
 }
 
-}  // namespace
-
-extern "C" {
-
-const char* svf_kv_last_error(void) { return g_err; }
-
-int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_append_args* a, void* hip_stream) {
+// svf_kv_append, and svf_kv_append_axes with ``axes``.
+int append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_append_args* a, const svf_kv_axes* axes, hipStream_t stream) {
     if (int rc = check_sizes(c, b)) return rc;
     if (!a) return fail(SVF_EINVAL, "args must not be NULL");
     if (int rc = check_buffers(c, b)) return rc;
@@ -184,6 +180,21 @@ int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_app
     for (int64_t s : strides) {
         if (!stride_ok(s)) return fail(SVF_EINVAL, "strides must be in 0 .. 2^40");
         wide = wide && s % 8 == 0;
+    }
+    AxesArgs x = {};
+    if (axes) {
+        if (axes->axes < 1 || axes->axes > SVF_KV_MOST_AXES)
+            return fail(SVF_EINVAL, "axes must be in 1 .. %d (%d)", SVF_KV_MOST_AXES, axes->axes);
+        if (!stride_ok(axes->token_stride) || !stride_ok(axes->axis_stride))
+            return fail(SVF_EINVAL, "strides of positions must be in 0 .. 2^40");
+        for (int i = 0; i < a->rot / 2; i++) {
+            if (axes->of_pair[i] >= axes->axes)
+                return fail(SVF_EINVAL, "of_pair must be below axes (pair %d: %d)", i, axes->of_pair[i]);
+            x.of_pair[i / 16] |= (uint32_t)axes->of_pair[i] << 2 * (i % 16);
+        }
+        x.kept = axes->kept;
+        x.token = axes->token_stride, x.axis = axes->axis_stride;
+        x.axes = axes->axes;
     }
     if (b->num_tokens == 0 || b->num_seqs == 0) return SVF_OK;
     if (!b->q_offsets || !a->q || !a->k || !a->v || !a->q_out || !a->positions)
@@ -214,17 +225,14 @@ int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_app
     k.half_layout = a->layout == SVF_KV_ROPE_HALF;
     k.rope_rows = a->rope_rows;
     k.dim = c->head_dim;
-    if (append_threads(k, wide) >= kThreadLimit) return fail(SVF_EINVAL, "num_tokens is too large (%d)", b->num_tokens);
-    return launched(launch_append(k, c->dtype, wide, static_cast<hipStream_t>(hip_stream)));
+    if ((axes ? append_axes_threads(k) : append_threads(k, wide)) >= kThreadLimit)
+        return fail(SVF_EINVAL, "num_tokens is too large (%d)", b->num_tokens);
+    return launched(axes ? launch_append_axes(k, x, c->dtype, stream) : launch_append(k, c->dtype, wide, stream));
 }
 
-int64_t svf_kv_attend_workspace(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
-    if (int rc = check_attend(c, b, a)) return rc;
-    return attend_workspace(sizes(c, b, a));
-}
-
-int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, void* hip_stream) {
-    if (int rc = check_attend(c, b, a)) return rc;
+// svf_kv_attend, and svf_kv_attend_first.
+int attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first, hipStream_t stream) {
+    if (int rc = check_attend(c, b, a, first)) return rc;
     if (int rc = check_buffers(c, b)) return rc;
     if (!stride_ok(a->q_token_stride) || !stride_ok(a->q_head_stride))
         return fail(SVF_EINVAL, "strides of q must be in 0 .. 2^40");
@@ -237,7 +245,7 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     if (b->num_tokens == 0 || b->num_seqs == 0) return SVF_OK;
     if (!b->q_offsets || !a->q || !a->out || !a->lse) return fail(SVF_EINVAL, "q_offsets, q, out and lse must not be NULL");
     if (!aligned(a->out, 16)) return fail(SVF_EINVAL, "out must be aligned to 16 bytes");
-    const int64_t need = svf_kv_attend_workspace(c, b, a);
+    const int64_t need = attend_workspace(sizes(c, b, a));
     if (a->workspace_bytes < need || (need > 0 && !a->workspace) || !aligned(a->workspace, 256))
         return fail(SVF_EINVAL, "workspace must have %lld bytes, aligned to 256", (long long)need);
     const Rows q = {a->q, a->q_token_stride, a->q_head_stride}, out = {a->out, a->out_token_stride, a->out_head_stride};
@@ -255,9 +263,40 @@ int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_att
     k.causal = a->causal != 0;
     // a window as wide as the table hides nothing, and a slot less than it is still an int
     k.window = a->window < (int64_t)b->table_width * c->page_size ? a->window : 0;
+    // without a window every token stays visible; the table has no more of them than this
+    k.first = k.window == 0 ? 0 : first < (int64_t)b->table_width * c->page_size ? first : b->table_width * c->page_size;
     k.add_weight = a->add_weight != 0;
     k.q_wide = aligned(a->q, 16) && a->q_token_stride % 8 == 0 && a->q_head_stride % 8 == 0;
-    return launched(launch_attend(k, sizes(c, b, a), static_cast<hipStream_t>(hip_stream)));
+    return launched(launch_attend(k, sizes(c, b, a, k.first), stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+const char* svf_kv_last_error(void) { return g_err; }
+
+int svf_kv_append(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_append_args* a, void* hip_stream) {
+    return append(c, b, a, nullptr, static_cast<hipStream_t>(hip_stream));
+}
+
+int svf_kv_append_axes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_append_args* a, const svf_kv_axes* axes,
+                       void* hip_stream) {
+    if (!axes) return fail(SVF_EINVAL, "axes must not be NULL");
+    return append(c, b, a, axes, static_cast<hipStream_t>(hip_stream));
+}
+
+int64_t svf_kv_attend_workspace(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a) {
+    if (int rc = check_attend(c, b, a)) return rc;
+    return attend_workspace(sizes(c, b, a));
+}
+
+int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, void* hip_stream) {
+    return attend(c, b, a, 0, static_cast<hipStream_t>(hip_stream));
+}
+
+int svf_kv_attend_first(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first, void* hip_stream) {
+    return attend(c, b, a, first, static_cast<hipStream_t>(hip_stream));
 }
 
 int64_t svf_kv_evict_workspace(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_evict_args* a) {

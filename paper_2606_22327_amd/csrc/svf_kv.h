@@ -34,6 +34,14 @@ struct AppendArgs {
     int32_t heads, rot, half_layout, rope_rows, dim;
 };
 
+// Positions with several axes.
+struct AxesArgs {
+    const int32_t* kept;  // or null: axis 0's
+    int64_t token, axis;  // strides of the positions, elements
+    int32_t axes;
+    uint32_t of_pair[8];  // two bits a pair
+};
+
 struct AttendArgs {
     KvView kv;
     const char* q;
@@ -43,13 +51,14 @@ struct AttendArgs {
     int64_t q_tok, q_head, o_tok, o_head;  // bytes
     float scale;  // times log2(e)
     int32_t heads, causal, window, add_weight;
+    int32_t first;   // slots that stay visible before the window
     int32_t q_wide;  // q can be read 16 bytes at a time
     int32_t few;     // rows of a key head up to which the kernels of few rows take a sequence
 };
 
 // The sizes that an attention call's workspace and launches go by.
 struct AttendSizes {
-    int32_t num_pages, page_size, kv_heads, heads, dim, dtype, tokens, seqs, width, max_q, add_weight;
+    int32_t num_pages, page_size, kv_heads, heads, dim, dtype, tokens, seqs, width, max_q, add_weight, first;
 };
 
 struct EvictArgs {
@@ -61,11 +70,13 @@ struct EvictArgs {
 };
 
 hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStream_t s);
+hipError_t launch_append_axes(const AppendArgs& a, const AxesArgs& x, int32_t dtype, hipStream_t s);
 hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 int64_t attend_workspace(const AttendSizes& z);
 // Threads of the largest launch.
 int64_t append_threads(const AppendArgs& a, bool wide);
+int64_t append_axes_threads(const AppendArgs& a);
 int64_t attend_threads(const AttendSizes& z);
 int64_t evict_threads(const EvictArgs& a);
 

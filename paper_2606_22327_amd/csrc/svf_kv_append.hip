@@ -167,6 +167,66 @@ __global__ __launch_bounds__(64) void k_append_any(AppendArgs p) {
     }
 }
 
+// Positions with several axes: a pair turns by its axis' position.  The row of the table that it takes its cosine and sine
+// from is another for each axis; an axis whose position is outside the table makes NaN of its own pairs alone.
+template <class E>
+__global__ __launch_bounds__(64) void k_axes_any(AppendArgs p, AxesArgs x) {
+    using T = typename E::T;
+    const int t = blockIdx.x, lane = threadIdx.x;
+    const int seq = find_seq(p.kv, t);
+    const Seq s = seq_of(p.kv, seq);
+    const int slot = s.len - s.n + (t - s.q0);
+    const bool ours = t >= s.q0 && t < s.q0 + s.n;
+    const int row = ours && slot >= 0 ? pool_row(p.kv, seq, slot) : -1;
+    const int hk = p.kv.kv_heads, half = p.rot >> 1, pairs = p.dim >> 1;
+    for (int i = lane; i < (p.heads + 2 * hk) * pairs; i += 64) {
+        const int h = i / pairs, u = i - h * pairs;
+        const T* src;
+        T* dst;
+        bool rotate = u < half;
+        if (h < p.heads) {
+            src = (const T*)(p.q + t * p.q_tok + h * p.q_head);
+            dst = (T*)(p.q_out + t * p.o_tok + h * p.o_head);
+        } else {
+            if (row < 0) continue;
+            const int g = h - p.heads;
+            if (g < hk) {
+                src = (const T*)(p.kn + t * p.k_tok + g * p.k_head);
+                dst = (T*)(const_cast<char*>(p.kv.k) + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row) +
+                           g * p.kv.k_head);
+            } else {
+                src = (const T*)(p.vn + t * p.v_tok + (g - hk) * p.v_head);
+                dst = (T*)(const_cast<char*>(p.kv.v) + row_offset(row, p.kv.shift, p.kv.v_page, p.kv.v_row) +
+                           (g - hk) * p.kv.v_head);
+                rotate = false;
+            }
+        }
+        const bool half_pair = u < half && p.half_layout;
+        const int ea = half_pair ? u : 2 * u, eb = half_pair ? u + half : 2 * u + 1;
+        const T a = src[ea], b = src[eb];
+        if (rotate) {
+            const int axis = x.of_pair[u >> 4] >> 2 * (u & 15) & 3;
+            const int pos = p.positions[t * x.token + axis * x.axis];
+            const bool known = (unsigned)pos < (unsigned)p.rope_rows;
+            const float* tab = p.rope + (int64_t)(known ? pos : 0) * p.rot + u;
+            const float c = known ? tab[0] : __builtin_nanf(""), sn = known ? tab[half] : __builtin_nanf("");
+            dst[ea] = (T)((float)a * c - (float)b * sn);
+            dst[eb] = (T)((float)b * c + (float)a * sn);
+        } else {
+            dst[ea] = a;
+            dst[eb] = b;
+        }
+    }
+    if (row >= 0) {
+        const int kept = x.kept ? x.kept[t] : p.positions[t * x.token];
+        for (int g = lane; g < hk; g += 64) {
+            const int64_t at = stat_index(p.kv, row, g);
+            if (p.kv.weight) p.kv.weight[at] = 0.f;
+            if (p.kv.position) p.kv.position[at] = kept;
+        }
+    }
+}
+
 // How the wide kernel's work is dealt out.
 struct Wide {
     int units, groups, per;
@@ -197,6 +257,12 @@ hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStrea
         return run(dtype == SVF_KV_BF16 ? k_append_wide<BF16> : k_append_wide<F16>, grid, 256, s, a, w.units, w.groups, w.per);
     }
     return run(dtype == SVF_KV_BF16 ? k_append_any<BF16> : k_append_any<F16>, dim3(a.kv.tokens), 64, s, a);
+}
+
+int64_t append_axes_threads(const AppendArgs& a) { return (int64_t)a.kv.tokens * 64; }
+
+hipError_t launch_append_axes(const AppendArgs& a, const AxesArgs& x, int32_t dtype, hipStream_t s) {
+    return run(dtype == SVF_KV_BF16 ? k_axes_any<BF16> : k_axes_any<F16>, dim3(a.kv.tokens), 64, s, a, x);
 }
 
 }  // namespace svfk

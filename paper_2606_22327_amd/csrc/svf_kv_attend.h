@@ -90,6 +90,26 @@ __device__ inline int first_slot(const AttendArgs& p, const Seq& s) {
     return p.window > 0 ? max(0, s.len - s.n - p.window + 1) & ~15 : 0;
 }
 
+// The slots that some row sees, one behind the other: place x is slot x below ``head`` and slot x + skip from there on.
+// With first tokens that stay visible (FIRST) ``head`` is their number rounded up to ``unit``, so that what takes
+// ``unit`` places at a time never has slots of both sides; 0 where the window begins before its end.
+struct Line {
+    int head, skip, places;
+};
+template <bool FIRST>
+__device__ inline Line line_of(const AttendArgs& p, const Seq& s, int unit) {
+    Line x;
+    x.head = FIRST ? (p.first + unit - 1) & ~(unit - 1) : 0;
+    x.skip = first_slot(p, s) - x.head;
+    if (FIRST && x.skip <= 0) x.head = x.skip = 0;
+    x.places = s.len - x.skip;
+    return x;
+}
+template <bool FIRST>
+__device__ inline int slot_of(const Line& x, int place) {
+    return FIRST && place < x.head ? place : place + x.skip;
+}
+
 // Where a lane reads a slot that is not there: a row of zeros, so that loads need no branch.
 static __device__ __align__(16) const char kZeroRow[512] = {};
 __device__ inline const char* zero_row() { return kZeroRow; }

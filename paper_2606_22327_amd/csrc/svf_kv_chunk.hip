@@ -112,7 +112,7 @@ __device__ inline int swizzle(int row) {
 // WIDE: pages of 16 slots or more, so that the sixteen slots that a wave fetches lie in one page: their address is the same for
 // the whole wave but for an offset that stays the same all along (a tile costs a wave 8 loads and some scalar
 // instructions, and 100 vector instructions otherwise).
-template <class E, int D, bool WIDE>
+template <class E, int D, bool WIDE, bool FIRST>
 __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(AttendArgs p, ChunkPlan plan) {
     using T = typename E::T;
     using V8 = typename E::V8;
@@ -154,6 +154,20 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     int lo = p.window > 0 ? max(0, r0 + first_row / G - p.window + 1) & ~15 : 0;
     int hi = p.causal ? min(s.len, r0 + last_row / G + 1) : s.len;
     int tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+    // With first tokens that stay visible: the tiles of those come first where the window does not reach back to them, and
+    // tile it begins at slot head_lo + it * kTile below head_tiles and at lo + it * kTile from there on.
+    int head_tiles = 0, head_lo = 0;
+    if constexpr (FIRST) {
+        const int head = (p.first + kTile - 1) / kTile;
+        if (head * kTile < lo) {
+            head_tiles = head;
+            tiles += head;
+            lo -= head * kTile;
+        } else if (lo > 0) {
+            lo = 0;
+            tiles = (hi + kTile - 1) / kTile;
+        }
+    }
     if (parts > 1) {
         // No part of fewer than four tiles: it would cost more to join than it saves.  (40 tokens of 32 query heads on 8 key heads behind
         // 2,000 slots: parts of one tile and more 28.0 us, of two 23.0, of four 21.8, of eight 26.1; behind 4,000: 28.8, 30.2, 27.5,
@@ -162,10 +176,15 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         if (part >= parts) return;
         if (part == 0 && tid == 0) plan.item[item] = Item{s.q0, first_row, rows, parts};
         const int from = (int)((int64_t)tiles * part / parts), to = (int)((int64_t)tiles * (part + 1) / parts);
-        hi = min(hi, lo + to * kTile);
+        if constexpr (FIRST)
+            head_tiles -= from, head_lo = from * kTile;
+        else
+            hi = min(hi, lo + to * kTile);
         lo += from * kTile;
         tiles = to - from;
     }
+
+    auto tile_slot = [&](int it) { return FIRST && it < head_tiles ? head_lo + it * kTile : lo + it * kTile; };
 
     // this lane's row, and the slots that all and any of the wave's rows see
     const int row = first_row + wave * 32 + c;
@@ -216,10 +235,11 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         voff[i] = (uint32_t)r * (uint32_t)p.kv.v_row + x;
     }
     auto look = [&](int it) {
-        page_all = table_entry(p.kv, table, lo + it * kTile + lane);
+        const int j0 = tile_slot(it);
+        page_all = table_entry(p.kv, table, j0 + lane);
         if constexpr (!WIDE) {
 #pragma unroll
-            for (int i = 0; i < NI; i++) page[i] = table_entry(p.kv, table, lo + it * kTile + own + i * PER);
+            for (int i = 0; i < NI; i++) page[i] = table_entry(p.kv, table, j0 + own + i * PER);
         }
     };
     typedef const __attribute__((address_space(1))) char* Global;
@@ -229,7 +249,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
     };
     uint64_t there, there_next;
     auto fetch = [&](int it, char* kto, char* vto) {
-        const int j0 = lo + it * kTile;
+        const int j0 = tile_slot(it);
         there_next = __ballot((unsigned)page_all < (unsigned)p.kv.num_pages && j0 + lane < hi);
         kto += wave * NI * 1024;
         vto += wave * NI * 1024;
@@ -277,7 +297,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             const uint32_t marks = odd_marks_of<E>(pair) << 4 * (w & 7);
             for (int y = 0; y <= last_row - first_row; y++) {
                 const int t = r0 + (first_row + y) / G;
-                if ((there >> r & 1) && (!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window))
+                if ((there >> r & 1) && (!p.causal || base + r <= t) && (p.window == 0 || base + r > t - p.window || (FIRST && base + r < p.first)))
                     atomicOr(&odd_marks[y][w >> 3], marks);
             }
             words[x] = finite_pair<E>(pair);
@@ -324,12 +344,13 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             fetch(it + 1, knext, vnext);
             look(it + 2);
         }
-        const int base = lo + it * kTile;
-        if (!(base + kTile - 1 <= block_last && base >= block_from && ~there == 0)) {
+        const int base = tile_slot(it);
+        const bool early = FIRST && base + kTile - 1 < p.first;  // every row sees all of the tile that is not behind it
+        if (!(base + kTile - 1 <= block_last && (base >= block_from || early) && ~there == 0)) {
             clean(vb, base);
             __syncthreads();
         }
-        if (base > any_last || base + kTile - 1 < any_from) return;
+        if (base > any_last || (base + kTile - 1 < any_from && !(FIRST && base < p.first))) return;
         f32x16 sc[2];
 #pragma unroll
         for (int st = 0; st < 2; st++)
@@ -348,9 +369,11 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-        if (!(base + kTile - 1 <= all_last && base >= all_from && ~there == 0)) {
+        if (!(base + kTile - 1 <= all_last && (base >= all_from || early) && ~there == 0)) {
             // bit (i / 4) * 8 + i % 4 of a word: whether the lane's row sees the slot of score i
-            const uint64_t seen = (there & bits_between(from - base, last - base)) >> (h * 4);
+            uint64_t sees = bits_between(from - base, last - base);
+            if constexpr (FIRST) sees |= bits_between(0, min(last, p.first - 1) - base);
+            const uint64_t seen = (there & sees) >> (h * 4);
 #pragma unroll
             for (int st = 0; st < 2; st++) {
                 const uint32_t word = (uint32_t)(seen >> (st * 32));
@@ -440,13 +463,23 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(Attend
         for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
     if (__syncthreads_or(zero != 0.f && l * 0.f == 0.f)) {
         const int w = tid % (D / 2);  // the dimensions 2 w and 2 w + 1
-        const int first = max(lo, block_from), end = min(hi - 1, block_last) + 1;
         uint32_t marks = 0;
+        auto look_through = [&](int first, int end) {
 #pragma unroll 8
-        for (int j = first + tid / (D / 2); j < end; j += 256 / (D / 2)) {
-            const int at = entry_row(z.kv, table_entry(z.kv, table, j), j, true);
-            const uint64_t from = at < 0 ? (uint64_t)zero_row() : vbase + row_offset(at, z.kv.shift, z.kv.v_page, z.kv.v_row);
-            marks |= odd_marks_of<E>(load_global<uint32_t>(from + w * 4));
+            for (int j = first + tid / (D / 2); j < end; j += 256 / (D / 2)) {
+                const int at = entry_row(z.kv, table_entry(z.kv, table, j), j, true);
+                const uint64_t from = at < 0 ? (uint64_t)zero_row() : vbase + row_offset(at, z.kv.shift, z.kv.v_page, z.kv.v_row);
+                marks |= odd_marks_of<E>(load_global<uint32_t>(from + w * 4));
+            }
+        };
+        if constexpr (FIRST) {
+            // the first tokens' tiles of this part, and the others
+            const int most = min(min(hi - 1, block_last) + 1, lo + tiles * kTile);
+            look_through(max(lo + max(head_tiles, 0) * kTile, block_from), most);
+            look_through(head_lo, min(z.first, min(most, head_lo + min(head_tiles, tiles) * kTile)));
+            if (head_tiles <= 0) look_through(lo, min(z.first, min(most, block_from)));
+        } else {
+            look_through(max(lo, block_from), min(hi - 1, block_last) + 1);
         }
         if (marks)
             for (int y = 0; y < kRows; y++) atomicOr(&odd_marks[y][w >> 3], marks << 4 * (w & 7));
@@ -520,12 +553,13 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // instructions take 0.33, exponentials 0.2 more, and products and exponentials of a tile follow each other.
 constexpr int kWSlots = 256, kWRows = 64;
 
+template <bool FIRST>
 __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
     if (s.n <= 0 || s.n > p.kv.max_q || !ours(p, s)) return 0;
-    return (s.len - first_slot(p, s) + kWSlots - 1) / kWSlots;
+    return (line_of<FIRST>(p, s, kWSlots).places + kWSlots - 1) / kWSlots;
 }
 
-template <class E, int D>
+template <class E, int D, bool FIRST>
 __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, int tile, int head) {
     using T = typename E::T;
     using V8 = typename E::V8;
@@ -535,10 +569,10 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const int G = p.heads / p.kv.kv_heads;
     const int r0 = s.len - s.n;
-    const int j0 = first_slot(p, s) + tile * kWSlots, j1 = min(j0 + kWSlots, s.len);
+    const int j0 = slot_of<FIRST>(line_of<FIRST>(p, s, kWSlots), tile * kWSlots), j1 = min(j0 + kWSlots, s.len);
     // rows that see one of the slots: tokens t0 .. t1 - 1
     const int t0 = p.causal ? max(0, j0 - r0) : 0;
-    const int t1 = p.window > 0 ? (int)max((int64_t)0, min((int64_t)s.n, (int64_t)j1 - 1 + p.window - r0)) : s.n;
+    const int t1 = p.window > 0 && !(FIRST && j0 < p.first) ? (int)max((int64_t)0, min((int64_t)s.n, (int64_t)j1 - 1 + p.window - r0)) : s.n;
     const int row0 = t0 * G, row1 = t1 * G;
 
     // this wave's slots and their keys
@@ -615,8 +649,10 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
         if (at + kWRows < row1) take(at + kWRows);
         // tokens of the first and the last row
         const int ta = at / G, tb = min(at + kWRows - 1, row1 - 1) / G;
-        const bool whole = (!p.causal || base + 63 <= r0 + ta) && (p.window == 0 || base > r0 + tb - p.window) && base + 63 < j1;
-        const bool none = (p.causal && base > r0 + tb) || (p.window > 0 && base + 63 <= r0 + ta - p.window) || base >= j1;
+        const bool whole = (!p.causal || base + 63 <= r0 + ta) && (p.window == 0 || base > r0 + tb - p.window || (FIRST && base + 63 < p.first)) &&
+                           base + 63 < j1;
+        const bool none = (p.causal && base > r0 + tb) || (p.window > 0 && base + 63 <= r0 + ta - p.window && !(FIRST && base < p.first)) ||
+                          base >= j1;
         if (!none) {
 #pragma unroll
             for (int rt = 0; rt < kWRows / 32; rt++) {
@@ -648,7 +684,9 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
                         for (int i = 0; i < 16; i++) sum[st][i] += exp2_fast(fmaf(sc[st][i], p.scale, -lse));
                 } else {
                     const int r = r0 + (at + rt * 32 + c) / G;
-                    const uint64_t seen = bits_between(p.window > 0 ? r - p.window + 1 - base : 0, p.causal ? r - base : 63) >> (h * 4);
+                    uint64_t sees = bits_between(p.window > 0 ? r - p.window + 1 - base : 0, p.causal ? r - base : 63);
+                    if constexpr (FIRST) sees |= bits_between(0, (p.causal ? min(r, p.first - 1) : p.first - 1) - base);
+                    const uint64_t seen = sees >> (h * 4);
 #pragma unroll
                     for (int st = 0; st < 2; st++) {
                         const uint32_t word = (uint32_t)(seen >> (st * 32));
@@ -677,20 +715,20 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
 }
 
 // One tile a workgroup, of as many as the pool has slots for.
-template <class E, int D>
+template <class E, int D, bool FIRST>
 __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(AttendArgs p) {
     __shared__ int64_t scan[4];
     const int hk = p.kv.kv_heads;
     int seq, tile;
-    if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles(p, s); }, scan,
+    if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan,
                    seq, tile))
         return;
-    weigh_slots<E, D>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
+    weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
 }
 
 // Sequences with slots that have no page can have more tiles than that: those from ``first`` on, in a loop (a kernel of its own,
 // since the loop around it makes the one above spill registers).
-template <class E, int D>
+template <class E, int D, bool FIRST>
 __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk_more(AttendArgs p, int64_t first) {
     __shared__ int64_t scan[4];
     const int hk = p.kv.kv_heads;
@@ -702,8 +740,8 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk_more(A
             return at;
         };
         int seq, tile;
-        if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles(p, s); }, scan, seq, tile)) return;
-        weigh_slots<E, D>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
+        if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan, seq, tile)) return;
+        weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
     }
 }
 
@@ -734,14 +772,15 @@ ChunkGrids grids(const AttendSizes& z, int32_t few) {
     if (g.blocks < split_groups(z, few)) g.blocks = split_groups(z, few);
     // slot tiles at most, and where every slot has a page: each page is in the batch once
     const int64_t cap = (int64_t)z.width * z.page_size, all = seqs * ((cap + kWSlots - 1) / kWSlots);
-    const int64_t pool = (int64_t)z.num_pages * z.page_size / kWSlots + seqs;
+    // (with first tokens a sequence has one more that is not full)
+    const int64_t pool = (int64_t)z.num_pages * z.page_size / kWSlots + seqs * (z.first > 0 ? 2 : 1);
     g.tiles = z.add_weight ? (all < pool ? all : pool) : 0;
     g.more = !z.add_weight ? 0 : all - g.tiles < 64 ? all - g.tiles : 64;
     g.tiles *= z.kv_heads, g.more *= z.kv_heads;
     return g;
 }
 
-template <class E, int D>
+template <class E, int D, bool FIRST>
 hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {
     ChunkPlan plan{split_groups(z, a.few), nullptr, nullptr, nullptr};
     if (plan.groups) {
@@ -755,7 +794,7 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         // Offsets of sixteen rows are 32 bits.
         const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
         const bool wide = z.page_size >= 16 && far < (int64_t(1) << 31);
-        e = run(wide ? k_attend_chunk<E, D, true> : k_attend_chunk<E, D, false>, dim3((unsigned)g.blocks), 256, s, a, plan);
+        e = run(wide ? k_attend_chunk<E, D, true, FIRST> : k_attend_chunk<E, D, false, FIRST>, dim3((unsigned)g.blocks), 256, s, a, plan);
         if (e != hipSuccess) return e;
     }
     if (plan.groups) {
@@ -763,10 +802,21 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         if (e != hipSuccess) return e;
     }
     if (g.tiles > 0) {
-        e = run(k_weight_chunk<E, D>, dim3((unsigned)g.tiles), 256, s, a);
+        e = run(k_weight_chunk<E, D, FIRST>, dim3((unsigned)g.tiles), 256, s, a);
         if (e != hipSuccess) return e;
     }
-    return g.more > 0 ? run(k_weight_chunk_more<E, D>, dim3((unsigned)g.more), 256, s, a, g.tiles / z.kv_heads) : hipSuccess;
+    return g.more > 0 ? run(k_weight_chunk_more<E, D, FIRST>, dim3((unsigned)g.more), 256, s, a, g.tiles / z.kv_heads) : hipSuccess;
+}
+
+template <bool FIRST>
+hipError_t launch_kind(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream_t s) {
+    if (z.dtype == SVF_KV_BF16)
+        return z.dim == 64    ? launch<BF16M, 64, FIRST>(a, z, ws, s)
+               : z.dim == 128 ? launch<BF16M, 128, FIRST>(a, z, ws, s)
+                              : launch<BF16M, 256, FIRST>(a, z, ws, s);
+    return z.dim == 64    ? launch<F16M, 64, FIRST>(a, z, ws, s)
+           : z.dim == 128 ? launch<F16M, 128, FIRST>(a, z, ws, s)
+                          : launch<F16M, 256, FIRST>(a, z, ws, s);
 }
 
 }  // namespace
@@ -797,9 +847,7 @@ hipError_t launch_attend(AttendArgs a, const AttendSizes& z, hipStream_t s) {
     }
     if (!has_chunks(z)) return hipSuccess;
     char* ws = a.ws + ((rows_workspace(z) + 255) & ~int64_t(255));
-    if (z.dtype == SVF_KV_BF16)
-        return z.dim == 64 ? launch<BF16M, 64>(a, z, ws, s) : z.dim == 128 ? launch<BF16M, 128>(a, z, ws, s) : launch<BF16M, 256>(a, z, ws, s);
-    return z.dim == 64 ? launch<F16M, 64>(a, z, ws, s) : z.dim == 128 ? launch<F16M, 128>(a, z, ws, s) : launch<F16M, 256>(a, z, ws, s);
+    return a.first > 0 ? launch_kind<true>(a, z, ws, s) : launch_kind<false>(a, z, ws, s);
 }
 
 }  // namespace svfk

@@ -13,7 +13,7 @@ struct RowsPlan {
     int64_t* first_unit;  // [seqs + 1]: units of a key head before each sequence; null where no launch follows
     float* part;          // [2 * groups][rows * (D + 4)]: partial results
     float* scores;        // [units][rows][kUnit] (add_weight): scores in log2 terms
-    int4* units;          // [units] (add_weight): sequence, index of the first row's statistic, first slot, head | rows << 16
+    int4* units;          // [units] (add_weight): sequence, index of the first row's statistic, first slot (place with first tokens), head | rows << 16
     int64_t score_units;  // units that scores has room for
     int32_t groups;       // workgroups over which the units are dealt out
     int32_t rows;         // rows of a sequence's key head at most
@@ -21,13 +21,13 @@ struct RowsPlan {
 
 // Units of one key head of a sequence, 0 where this kernel leaves it to another.
 // One without a slot still has its rows to write.
+template <bool FIRST>
 __device__ inline int units_of(const AttendArgs& p, const Seq& s, int rows) {
     if (s.n <= 0) return 0;
     const int G = p.heads / p.kv.kv_heads;
     if (s.n <= p.kv.max_q && (int64_t)s.n * G > rows) return 0;
     if (s.n > p.kv.max_q) return 1;
-    const int lo = first_slot(p, s);
-    const int u = (s.len - lo + kUnit - 1) / kUnit;
+    const int u = (line_of<FIRST>(p, s, 16).places + kUnit - 1) / kUnit;
     return u > 0 ? u : 1;
 }
 
@@ -113,7 +113,7 @@ __device__ inline void load_v(Tile<E, D>& x, const Where& w, uint32_t row_bytes)
 // 14 registers, though none that the loop needs, and take 78 us where they took 68.)
 constexpr int waves_per_simd(int dim, int rt) { return dim * rt <= 64 ? 3 : dim * rt <= 128 ? 2 : 1; }
 
-template <class E, int D, int RT, bool WIDE>
+template <class E, int D, int RT, bool WIDE, bool FIRST>
 __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(AttendArgs p, RowsPlan plan) {
     using T = typename E::T;
     using V8 = typename E::V8;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
     const int per = (p.kv.seqs + 255) / 256;
     const int i0 = min(tid * per, p.kv.seqs), i1 = min(i0 + per, p.kv.seqs);
     int64_t mine = 0;
-    for (int i = i0; i < i1; i++) mine += units_of(p, seq_of(p.kv, i), plan.rows);
+    for (int i = i0; i < i1; i++) mine += units_of<FIRST>(p, seq_of(p.kv, i), plan.rows);
     int64_t incl = mine;
     for (int d = 1; d < 64; d <<= 1) {
         const int64_t x = __shfl_up(incl, d);
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
         int64_t at = before;
         for (int i = i0; i < i1; i++) {
             plan.first_unit[i] = at;
-            at += units_of(p, seq_of(p.kv, i), plan.rows);
+            at += units_of<FIRST>(p, seq_of(p.kv, i), plan.rows);
         }
         if (tid == 0) plan.first_unit[p.kv.seqs] = total;
     }
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
         int64_t at = before;
         int i = i0;
         for (; i < i1; i++) {
-            const int u = units_of(p, seq_of(p.kv, i), plan.rows);
+            const int u = units_of<FIRST>(p, seq_of(p.kv, i), plan.rows);
             if (a < (at + u) * hk) break;
             at += u;
         }
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
 
     for (int64_t pos = a; pos < b && seq < p.kv.seqs;) {
         const Seq s = seq_of(p.kv, seq);
-        const int units = units_of(p, s, plan.rows);
+        const int units = units_of<FIRST>(p, s, plan.rows);
         if (pos >= (first + units) * hk) {  // a sequence done, or one without units
             first += units;
             seq++;
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
             if (plan.scores && unit0 < plan.score_units && tid == 0) plan.units[unit0] = make_int4(seq, 0, 0, head);
             continue;
         }
-        const int lo = first_slot(p, s);
+        const Line line = line_of<FIRST>(p, s, 16);
         const int r0 = s.len - s.n;  // the first new token's slot
         const uint64_t kbase = (uint64_t)(p.kv.k + head * p.kv.k_head), vbase = (uint64_t)(p.kv.v + head * p.kv.v_head);
 
@@ -216,11 +216,11 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
 #pragma unroll
             for (int j = 0; j < VD; j++) o[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int slot0 = lo + wave * 32 + (lane & 31);
+        const int place0 = wave * 32 + (lane & 31);
         const Table table = table_of(p.kv, seq, s.len, zero_row());
-        auto entry = [&](int u) { return table_entry(p.kv, table, slot0 + u * kUnit); };
+        auto entry = [&](int u) { return table_entry(p.kv, table, slot_of<FIRST>(line, place0 + u * kUnit)); };
         auto where = [&](int u, int page) {
-            const int j = slot0 + u * kUnit, row = entry_row(p.kv, page, j, u < u1 && j < s.len);
+            const int j = slot_of<FIRST>(line, place0 + u * kUnit), row = entry_row(p.kv, page, j, u < u1 && j < s.len);
             Where w;
             w.there = row >= 0;
             if constexpr (WIDE) {
@@ -255,7 +255,8 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
         for (int u = u0; u < u1; u++) {
             const Where next = where(u + 1, page_next);
             page_next = entry(u + 2);
-            const int base = lo + u * kUnit + wave * 32;
+            // slot of place x of the tile, without x: its two halves may lie apart
+            const int place = u * kUnit + wave * 32, base[2] = {slot_of<FIRST>(line, place), slot_of<FIRST>(line, place + 16) - 16};
             f32x4 sc[RT][2];
 #pragma unroll
             for (int rt = 0; rt < RT; rt++)
@@ -267,7 +268,10 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
                 }
             // which of the tile's slots are there: the same for every row
             const uint32_t there = (uint32_t)__ballot(now.there);
-            const bool all_seen = there == 0xffffffffu && (!p.causal || base + 31 <= r0) && (p.window == 0 || base > s.len - 1 - p.window);
+            bool all_seen = there == 0xffffffffu && (!p.causal || base[1] + 31 <= r0);
+#pragma unroll
+            for (int t = 0; t <= FIRST; t++)
+                all_seen = all_seen && (p.window == 0 || base[t] + 16 * t > s.len - 1 - p.window || (FIRST && base[t] + 16 * t + 15 < p.first));
             __builtin_amdgcn_sched_barrier(0);
             load_k<E, D, WIDE>(x, next, k_row);
             __builtin_amdgcn_sched_barrier(0);
@@ -280,8 +284,8 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
                 if (!all_seen) {
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
-                        const int off = (i >> 2) * 16 + g * 4 + (i & 3), j = base + off;
-                        if (!(there >> off & 1) || j > last[rt] || j < from[rt]) sc[rt][i >> 2][i & 3] = -INFINITY;
+                        const int off = (i >> 2) * 16 + g * 4 + (i & 3), j = base[i >> 2] + off;
+                        if (!(there >> off & 1) || j > last[rt] || (j < from[rt] && !(FIRST && j < p.first))) sc[rt][i >> 2][i & 3] = -INFINITY;
                     }
                 }
 #pragma unroll
@@ -328,11 +332,11 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
                     for (int i = 0; i < 8 * (D / 32); i++) {
                         const uint32_t pair = own[i * 64];
                         if (!odd_pair<E>(pair)) continue;
-                        const int at = i / (D / 32), off = (at >> 2) * 16 + g * 4 + (at & 3), j = base + off;
+                        const int at = i / (D / 32), off = (at >> 2) * 16 + g * 4 + (at & 3), j = base[at >> 2] + off;
                         const uint32_t marks = odd_marks_of<E>(pair) << 4 * (i % (D / 32));
                         for (int row = 0; row < rows && (there >> off & 1); row++) {
                             const int r = r0 + row / G;
-                            if ((!p.causal || j <= r) && (p.window == 0 || j > r - p.window)) atomicOr(&odd_marks[row][c], marks);
+                            if ((!p.causal || j <= r) && (p.window == 0 || j > r - p.window || (FIRST && j < p.first))) atomicOr(&odd_marks[row][c], marks);
                         }
                         own[i * 64] = finite_pair<E>(pair);
                     }
@@ -368,7 +372,7 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
                         *(f32x4*)to = sc[rt][0];
                         *(f32x4*)(to + 16) = sc[rt][1];
                     }
-                if (tid == 0) plan.units[unit] = make_int4(seq, s.q0 * p.heads + head * G, lo + u * kUnit, head | rows << 16);
+                if (tid == 0) plan.units[unit] = make_int4(seq, s.q0 * p.heads + head * G, FIRST ? u * kUnit : line.skip + u * kUnit, head | rows << 16);
             }
             now = next;
         }
@@ -543,7 +547,7 @@ __global__ __launch_bounds__(256) void k_join_rows(AttendArgs p, RowsPlan plan, 
 }
 
 // The weights of a unit whose scores were not kept: they are formed again, two slots a lane. Right, not fast.
-template <class E, int D>
+template <class E, int D, bool FIRST>
 __device__ void weigh_again(const AttendArgs& p, const RowsPlan& plan, int64_t unit) {
     using T = typename E::T;
     const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
@@ -554,14 +558,14 @@ __device__ void weigh_again(const AttendArgs& p, const RowsPlan& plan, int64_t u
     if (s.n > p.kv.max_q) return;
     const int r0 = s.len - s.n;
     for (int x = 0; x < 2; x++) {
-        const int j = first_slot(p, s) + u * kUnit + 2 * lane + x;
+        const int j = slot_of<FIRST>(line_of<FIRST>(p, s, 16), u * kUnit + 2 * lane + x);
         const int at = j < s.len ? pool_row(p.kv, seq, j) : -1;
         if (at < 0) continue;
         const T* k = (const T*)(p.kv.k + head * p.kv.k_head + row_offset(at, p.kv.shift, p.kv.k_page, p.kv.k_row));
         float sum = 0.f;
         for (int r = 0; r < s.n * G; r++) {
             const int t = r / G, h = head * G + r - t * G;
-            if ((p.causal && j > r0 + t) || (p.window > 0 && j <= r0 + t - p.window)) continue;
+            if ((p.causal && j > r0 + t) || (p.window > 0 && j <= r0 + t - p.window && !(FIRST && j < p.first))) continue;
             const T* q = (const T*)(p.q + (s.q0 + t) * p.q_tok + h * p.q_head);
             float dot = 0.f;
 #pragma unroll 8
@@ -576,15 +580,16 @@ __device__ void weigh_again(const AttendArgs& p, const RowsPlan& plan, int64_t u
 // The weights of these sequences' slots from the scores and the rows' final statistics: a wave for a unit, two
 // slots a lane, the rows in order. (256 sequences, 255,882 slots of 8 key heads: 15 us for 32 MB of scores and 16 MB of weights.)
 // There is room for the scores of as many slots as the pool has; sequences with slots that have no page can have more units.
-template <class E, int D>
+template <class E, int D, bool FIRST>
 __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan) {
     const int hk = p.kv.kv_heads, G = p.heads / hk, lane = threadIdx.x & 63;
     const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), all = plan.first_unit[p.kv.seqs] * hk;
-    for (int64_t unit = plan.score_units + wave; unit < all; unit += (int64_t)gridDim.x * 4) weigh_again<E, D>(p, plan, unit);
+    for (int64_t unit = plan.score_units + wave; unit < all; unit += (int64_t)gridDim.x * 4) weigh_again<E, D, FIRST>(p, plan, unit);
     if (wave >= min(all, plan.score_units)) return;
     const int4 x = plan.units[wave];
-    const int rows = x.w >> 16, head = x.w & 0xffff, j = x.z + 2 * lane;
+    const int rows = x.w >> 16, head = x.w & 0xffff;
     const Seq s = seq_of(p.kv, x.x);
+    const int j = FIRST ? slot_of<FIRST>(line_of<FIRST>(p, s, 16), x.z + 2 * lane) : x.z + 2 * lane;
     const Table table = table_of(p.kv, x.x, s.len, zero_row());
     const int page[2] = {table_entry(p.kv, table, j), table_entry(p.kv, table, j + 1)};
     const float2* sc = (const float2*)(plan.scores + wave * plan.rows * kUnit) + lane;
@@ -597,28 +602,28 @@ __global__ __launch_bounds__(256) void k_weight_rows(AttendArgs p, RowsPlan plan
         const float ref = lse == -INFINITY ? INFINITY : lse;  // a row that saw nothing adds nothing
         // only to slots that the row sees: a statistic that is no number makes one of every score, also of the -inf of the others
         const int own = s.len - s.n + t, last = p.causal ? own : s.len - 1, from = p.window > 0 ? own - p.window + 1 : 0;
-        sum.x += j <= last && j >= from ? exp2_fast(y.x - ref) : 0.f;
-        sum.y += j < last && j + 1 >= from ? exp2_fast(y.y - ref) : 0.f;
+        sum.x += j <= last && (j >= from || (FIRST && j < p.first)) ? exp2_fast(y.x - ref) : 0.f;
+        sum.y += j < last && (j + 1 >= from || (FIRST && j + 1 < p.first)) ? exp2_fast(y.y - ref) : 0.f;
     }
     const int row0 = entry_row(p.kv, page[0], j, j < s.len && sum.x != 0.f), row1 = entry_row(p.kv, page[1], j + 1, j + 1 < s.len && sum.y != 0.f);
     if (row0 >= 0) p.kv.weight[stat_index(p.kv, row0, head)] += sum.x;
     if (row1 >= 0) p.kv.weight[stat_index(p.kv, row1, head)] += sum.y;
 }
 
-template <class E, int D, bool WIDE>
+template <class E, int D, bool WIDE, bool FIRST>
 hipError_t launch_tiles(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
     if constexpr (D <= 128) {
-        if (plan.rows > 16) return run(k_attend_rows<E, D, 2, WIDE>, dim3(plan.groups), 256, s, a, plan);
+        if (plan.rows > 16) return run(k_attend_rows<E, D, 2, WIDE, FIRST>, dim3(plan.groups), 256, s, a, plan);
     }
-    return run(k_attend_rows<E, D, 1, WIDE>, dim3(plan.groups), 256, s, a, plan);
+    return run(k_attend_rows<E, D, 1, WIDE, FIRST>, dim3(plan.groups), 256, s, a, plan);
 }
 
-template <class E, int D>
+template <class E, int D, bool FIRST>
 hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
     // Offsets of sixteen rows are 32 bits.
     const int64_t far = 16 * (a.kv.k_row > a.kv.v_row ? a.kv.k_row : a.kv.v_row);
     const bool wide = a.kv.shift >= 4 && far < (int64_t(1) << 31);
-    hipError_t e = wide ? launch_tiles<E, D, true>(a, plan, s) : launch_tiles<E, D, false>(a, plan, s);
+    hipError_t e = wide ? launch_tiles<E, D, true, FIRST>(a, plan, s) : launch_tiles<E, D, false, FIRST>(a, plan, s);
     if (e != hipSuccess) return e;
     const int64_t cap = (int64_t)a.kv.width << a.kv.shift;
     if (cap > kUnit && plan.groups > 1) {  // else no row has a second unit
@@ -636,8 +641,19 @@ hipError_t launch(const AttendArgs& a, const RowsPlan& plan, hipStream_t s) {
         e = run(k_join_rows<E, D>, dim3((unsigned)(by_head ? heads : plan.groups - 1), many ? plan.rows : 1), 256, s, a, plan, parts, by_head);
         if (e != hipSuccess) return e;
     }
-    return a.add_weight && plan.score_units > 0 ? run(k_weight_rows<E, D>, dim3((unsigned)((plan.score_units + 3) / 4)), 256, s, a, plan)
+    return a.add_weight && plan.score_units > 0 ? run(k_weight_rows<E, D, FIRST>, dim3((unsigned)((plan.score_units + 3) / 4)), 256, s, a, plan)
                                                 : hipSuccess;
+}
+
+template <bool FIRST>
+hipError_t launch_kind(const AttendArgs& a, const RowsPlan& plan, const AttendSizes& z, hipStream_t s) {
+    if (z.dtype == SVF_KV_BF16)
+        return z.dim == 64    ? launch<BF16M, 64, FIRST>(a, plan, s)
+               : z.dim == 128 ? launch<BF16M, 128, FIRST>(a, plan, s)
+                              : launch<BF16M, 256, FIRST>(a, plan, s);
+    return z.dim == 64    ? launch<F16M, 64, FIRST>(a, plan, s)
+           : z.dim == 128 ? launch<F16M, 128, FIRST>(a, plan, s)
+                          : launch<F16M, 256, FIRST>(a, plan, s);
 }
 
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t(255); }
@@ -708,9 +724,7 @@ hipError_t launch_rows(const AttendArgs& a, const AttendSizes& z, char* ws, hipS
     plan.score_units = y.units;
     plan.groups = y.groups;
     plan.rows = y.rows;
-    if (z.dtype == SVF_KV_BF16)
-        return z.dim == 64 ? launch<BF16M, 64>(a, plan, s) : z.dim == 128 ? launch<BF16M, 128>(a, plan, s) : launch<BF16M, 256>(a, plan, s);
-    return z.dim == 64 ? launch<F16M, 64>(a, plan, s) : z.dim == 128 ? launch<F16M, 128>(a, plan, s) : launch<F16M, 256>(a, plan, s);
+    return a.first > 0 ? launch_kind<true>(a, plan, z, s) : launch_kind<false>(a, plan, z, s);
 }
 
 }  // namespace svfk

@@ -3,10 +3,11 @@
 A schedule of ``svfsim`` counts cache slots; these calls are what one of its
 steps does to a layer's cache on the GPU:
 
-``append``   rotary positions on new queries and keys, keys and values into pages
-``attend``   attention of new tokens (one or many for each sequence) over the pages
+``append``   rotary positions (with one axis or several) on new queries and keys, keys and values into pages
+``attend``   attention of new tokens (one or many for each sequence) over the pages: all, a window, or a window and the first tokens
 ``evict``    shrinks sequences to a number of slots by accumulated attention weight
 ``rope_table``   cosines and sines by position, for the rotation
+``pair_axes``   which axis of a position each pair of a head turns by
 
 Argument marshalling only: every step runs in the HIP kernels of
 ``libsvfsim.so``, on torch's current stream of the tensors' device.  All tensors are
@@ -20,7 +21,7 @@ from __future__ import annotations
 
 import math
 import struct
-from typing import NamedTuple, Optional, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -28,6 +29,7 @@ from . import svfsim
 
 DTYPE = {torch.bfloat16: 0, torch.float16: 1}
 LAYOUT = {"half": 0, "interleaved": 1}
+MOST_AXES = 4
 
 # the structs of svfkv.h
 _CACHE = struct.Struct("@4P6q5i4x")
@@ -35,6 +37,7 @@ _BATCH = struct.Struct("@3Pq4i")
 _APPEND = struct.Struct("@6P8q4i")
 _ATTEND = struct.Struct("@4P5qf4i4x")
 _EVICT = struct.Struct("@3Pq3i4x")
+_AXES = struct.Struct("@P2qi128s4x")
 
 
 class Cache(NamedTuple):
@@ -73,9 +76,9 @@ def last_error() -> str:
     return svfsim.load().svf_kv_last_error().decode(errors="replace")
 
 
-def _check(rc: int):
+def _check(rc: int, error=last_error):
     if rc != 0:
-        raise svfsim.SvfError(rc, last_error())
+        raise svfsim.SvfError(rc, error())
 
 
 # A step is some microseconds on the GPU, so the checks are one expression each
@@ -165,14 +168,14 @@ def _kind(cache: Cache):
     return (k.dtype, k.get_device(), shape[3]), shape[1]
 
 
-def _call(fn, dev: int, *packed: bytes):
+def _call(fn, dev: int, *packed, error=last_error):
     if dev == torch.cuda.current_device():
         rc = fn(*packed, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
             rc = fn(*packed, _raw_stream(dev))
     if rc != 0:
-        _check(rc)
+        _check(rc, error)
 
 
 def _gradient():
@@ -196,13 +199,18 @@ def _workspace(n: int, like: torch.Tensor) -> Optional[torch.Tensor]:
 
 
 def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, rope: Optional[torch.Tensor],
-           batch: Batch, cache: Cache, layout: str = "half", q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+           batch: Batch, cache: Cache, layout: str = "half", q_out: Optional[torch.Tensor] = None,
+           axes: Optional[bytes] = None, kept: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotate new queries ``q`` [tokens, heads, head_dim] and keys ``k`` [tokens,
     kv_heads, head_dim] by their ``positions`` (int32 [tokens]) and write keys and values
     ``v`` into their slots; returns the rotated queries (``q_out``, which may be
     ``q``).  ``rope`` is a table of ``rope_table`` (None: nothing is rotated);
     its width is the rotated part of a head.  Views with any strides of
-    tokens and heads are taken, such as the parts of one projection's output."""
+    tokens and heads are taken, such as the parts of one projection's output.
+
+    For positions with several axes ``axes`` names the axis of every pair (``pair_axes``); ``positions`` are then
+    [tokens, axes], with any strides, and ``kept`` (int32 [tokens]) is what ``cache.position`` is set to in
+    place of axis 0's position: the token's place in the text, which ``evict`` goes by."""
     if (q.requires_grad or k.requires_grad or v.requires_grad or cache.k.requires_grad or cache.v.requires_grad
             or (rope is not None and rope.requires_grad) or (q_out is not None and q_out.requires_grad)):
         _gradient()
@@ -214,9 +222,18 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     tokens, heads = q.shape[:2]
     if not (k.shape[0] == tokens and v.shape[0] == tokens):
         _need(False, "q, k and v must have as many tokens")
-    if not (positions.dtype == torch.int32 and positions.dim() == 1 and positions.shape[0] == tokens
-            and positions.is_contiguous() and positions.get_device() == dev):
+    if axes is not None:
+        if not (positions.dtype == torch.int32 and positions.dim() == 2 and positions.shape[0] == tokens
+                and positions.get_device() == dev):
+            _need(False, "positions must be int32 [tokens, axes]")
+        if not (kept is None or (kept.dtype == torch.int32 and kept.dim() == 1 and kept.shape[0] == tokens
+                                 and kept.is_contiguous() and kept.get_device() == dev)):
+            _need(False, "kept must be contiguous int32 [tokens]")
+    elif not (positions.dtype == torch.int32 and positions.dim() == 1 and positions.shape[0] == tokens
+              and positions.is_contiguous() and positions.get_device() == dev):
         _need(False, "positions must be contiguous int32 [tokens]")
+    elif kept is not None:
+        _need(False, "kept goes with axes")
     if batch.q_offsets is None or layout not in LAYOUT:
         _need(batch.q_offsets is not None, "q_offsets must not be None")
         _need(False, f"layout must be one of {tuple(LAYOUT)}")
@@ -233,17 +250,25 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     ot, oh = _rows(q_out, "q_out", *kind)
     a = _APPEND.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), positions.data_ptr(), table,
                      qt, qh, kt, kh, vt, vh, ot, oh, heads, rot, LAYOUT[layout], rows)
-    _call(svfsim.load().svf_kv_append, dev, *_pack(cache, batch, tokens), a)
+    if axes is None:
+        _call(svfsim.load().svf_kv_append, dev, *_pack(cache, batch, tokens), a)
+        return q_out
+    if not (isinstance(axes, bytes) and len(axes) * 2 == rot and rot <= 256):
+        _need(False, "axes must be bytes, one for each pair of the table (pair_axes)")
+    pt, pa = positions.stride()
+    x = _AXES.pack(0 if kept is None else kept.data_ptr(), pt, pa, positions.shape[1], axes)
+    _call(svfsim.load().svf_kv_append_axes, dev, *_pack(cache, batch, tokens), a, x)
     return q_out
 
 
 def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, window: int = 0,
            scale: Optional[float] = None, add_weight: bool = False,
-           out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+           out: Optional[torch.Tensor] = None, first: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
     """Attention of the new tokens' queries ``q`` [tokens, heads, head_dim] over
     their sequences' slots: (``out`` like q, ``lse`` float32 [tokens, heads]).
     ``scale`` is 1/sqrt(head_dim) by default; ``window`` > 0 lets a token see that many
-    slots up to its own.  ``add_weight`` adds every slot's softmax, summed
+    slots up to its own, and the sequence's ``first`` slots besides; pages of slots that no token sees any more may be
+    given back (-1 in the page table).    ``add_weight`` adds every slot's softmax, summed
     over the tokens and the query heads that share its key head, to
     ``cache.weight``.  A token that sees no slot has out = 0, lse = -inf."""
     if (q.requires_grad or cache.k.requires_grad or cache.v.requires_grad
@@ -275,7 +300,11 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     if need:
         ws = _workspace(need, q)
         a = _ATTEND.pack(*at, ws.data_ptr(), need, *fixed)
-    _call(lib.svf_kv_attend, kind[1], kv, seqs, a)
+    if first == 0:
+        _call(lib.svf_kv_attend, kind[1], kv, seqs, a)
+    else:
+        _need(0 < first < 1 << 31, "first must be >= 0, a 32-bit integer")
+        _call(lib.svf_kv_attend_first, kind[1], kv, seqs, a, int(first))
     return out, lse
 
 
@@ -308,8 +337,21 @@ def evict(batch: Batch, cache: Cache, budget: int, recent: int, next_position: t
     return new_len
 
 
+def pair_axes(pairs: Sequence[int], order: str = "blocks") -> bytes:
+    """The axis of each pair of a head, for ``append``: axis a has ``pairs[a]`` of them, in ``blocks`` one behind the
+    other or in ``turns``, a pair of each axis at a time until it has all of its pairs."""
+    pairs = [int(n) for n in pairs]
+    _need(1 <= len(pairs) <= MOST_AXES and min(pairs) >= 0 and sum(pairs) <= 128,
+          f"pairs must be 1 .. {MOST_AXES} numbers >= 0, 128 together at most")
+    _need(order in ("blocks", "turns"), "order must be 'blocks' or 'turns'")
+    if order == "blocks":
+        return bytes(a for a, n in enumerate(pairs) for _ in range(n))
+    return bytes(a for i in range(max(pairs)) for a, n in enumerate(pairs) if i < n)
+
+
 def rope_table(positions: int, rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
-               original: int = 0, fast: float = 32.0, slow: float = 1.0, device="cuda") -> torch.Tensor:
+               original: int = 0, fast: float = 32.0, slow: float = 1.0, device="cuda",
+               axes: Optional[bytes] = None) -> torch.Tensor:
     """Cosines and sines of ``positions`` positions for ``append``: float32 [positions,
     rot], rot/2 cosines, then rot/2 sines.  Pair i turns by position * base^(-2i/rot),
     computed in 64 bits.  For contexts ``factor`` times longer than the
@@ -321,7 +363,18 @@ def rope_table(positions: int, rot: int, base: float = 10000.0, scaling: str = "
     ``by-parts``  pairs that turn more than ``fast`` times within the original context stay, those
                   that turn less than ``slow`` times are divided by factor, a ramp in the
                   turns' order between them; cosines and sines times 0.1 ln(factor) + 1
+
+    With ``axes`` (``pair_axes``) every axis has the whole range of frequencies for itself: its n pairs turn as a head
+    with rot = 2n would.  Without, a pair's frequency goes by its place in the head, whichever axis it turns by.
     """
+    if axes is not None:
+        _need(isinstance(axes, bytes) and 2 * len(axes) == rot, "axes must be bytes, one for each pair")
+        table = torch.empty((positions, rot), dtype=torch.float32, device=device)
+        for a in set(axes):
+            mine = [i for i, x in enumerate(axes) if x == a]
+            part = rope_table(positions, 2 * len(mine), base, scaling, factor, original, fast, slow, device)
+            table[:, mine + [i + len(axes) for i in mine]] = part
+        return table
     _need(rot >= 2 and rot % 2 == 0 and positions >= 1, "positions must be >= 1 and rot even, >= 2")
     _need(scaling in ("none", "linear", "base", "by-parts"), f"unknown scaling {scaling!r}")
     _need(factor >= 1.0 and base > 1.0, "factor must be >= 1 and base > 1")

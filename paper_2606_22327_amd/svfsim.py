@@ -39,7 +39,9 @@ EXPORTS = ("svf_create", "svf_reset", "svf_step", "svf_run", "svf_read", "svf_st
            "svf_set_profiling", "svf_timings", "svf_shape", "svf_destroy",
            "svf_last_error", "svf_abi_version", "svf_opt_burst", "svf_opt_burst_batch",
            "svf_run_noalloc", "svf_kv_append", "svf_kv_attend", "svf_kv_attend_workspace",
-           "svf_kv_evict", "svf_kv_evict_workspace", "svf_kv_last_error")
+           "svf_kv_evict", "svf_kv_evict_workspace", "svf_kv_last_error",
+           "svf_kv_append_axes", "svf_kv_attend_first", "svf_logprob", "svf_logprob_workspace",
+           "svf_logprob_last_error")
 
 
 class SvfError(RuntimeError):
@@ -123,14 +125,20 @@ def load(path: str = LIB_PATH):
     lib.svf_run_noalloc.argtypes = [ctypes.POINTER(BatchDesc), V, V, V, V, V, V]
     for name in ("svf_kv_append", "svf_kv_attend", "svf_kv_evict"):
         getattr(lib, name).argtypes = [V, V, V, V]
-    lib.svf_kv_last_error.argtypes = []
-    lib.svf_kv_last_error.restype = ctypes.c_char_p
+    lib.svf_kv_append_axes.argtypes = [V, V, V, V, V]
+    lib.svf_kv_attend_first.argtypes = [V, V, V, I32, V]
+    lib.svf_logprob.argtypes = [V, V]
+    for name in ("svf_kv_last_error", "svf_logprob_last_error"):
+        getattr(lib, name).argtypes = []
+        getattr(lib, name).restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("svf_last_error", "svf_kv_last_error"):
+        if not name.endswith("last_error"):
             getattr(lib, name).restype = ctypes.c_int
     for name in ("svf_kv_attend_workspace", "svf_kv_evict_workspace"):
         getattr(lib, name).argtypes = [V, V, V]
         getattr(lib, name).restype = I64
+    lib.svf_logprob_workspace.argtypes = [V]
+    lib.svf_logprob_workspace.restype = I64
     _lib = lib
     return lib
 

@@ -1,0 +1,327 @@
+"""Attention with a window and first tokens that stay visible: against its definition in 64 bits, and its refusals."""
+
+import math
+
+import pytest
+import torch
+
+import kv_plain as P
+from paper_2606_22327_amd import kvcache as C
+from paper_2606_22327_amd import svfsim as S
+from test_kvcache import BF, HEADS, HF, batch_of, make
+from test_kvcache_refusals import A, attend, batch, cache
+
+NAN, INF = float("nan"), float("inf")
+
+
+def plain(s, causal, window, first, scale):
+    """(out, lse, weight, tol) as kv_plain.attend has them, with the first tokens visible."""
+    q, k, v = s["q"].double(), s["k"], s["v"]
+    T, H, D = q.shape
+    pages, hk, page = k.shape[:3]
+    G = H // hk
+    out, absv = torch.zeros_like(q), torch.zeros_like(q)
+    lse = torch.full((T, H), -math.inf, dtype=torch.float64)
+    big = torch.zeros((T, H), dtype=torch.float64)
+    weight = torch.zeros((pages, hk, page), dtype=torch.float64)
+    for i in range(len(s["kv_len"])):
+        a, b = int(s["offsets"][i]), int(s["offsets"][i + 1])
+        pg, row = P.slots_of(s["table"], i, s["kv_len"][i], page, pages)
+        n, m = b - a, len(pg)
+        if n == 0 or m == 0:
+            continue
+        r, j = m - n + torch.arange(n)[:, None], torch.arange(m)
+        seen = (pg >= 0) & (j < m)
+        seen = seen & (j <= r) if causal else seen.expand(n, m)
+        if window:
+            seen = seen & ((j > r - window) | (j < first))
+        any_ = seen.any(0)
+        pg, row, seen = pg[any_], row[any_], seen[:, any_]
+        for h in range(hk):
+            kk, vv = k[pg, h, row].double(), v[pg, h, row].double()
+            odd = ~vv.isfinite()
+            for g in range(h * G, (h + 1) * G):
+                sc = torch.where(seen, scale * (q[a:b, g] @ kk.T), -math.inf)
+                top = sc.amax(1, keepdim=True) if sc.shape[1] else torch.full((n, 1), -math.inf, dtype=torch.float64)
+                e = torch.where(seen, torch.exp(sc - torch.where(top == -math.inf, 0.0, top)), 0.0)
+                total = e.sum(1, keepdim=True)
+                p = torch.where(total != 0, e / total, 0.0)
+                out[a:b, g] = p @ torch.where(odd, 0.0, vv)
+                absv[a:b, g] = p @ torch.where(odd, 0.0, vv).abs()
+                if odd.any():                       # what a row sees decides its output
+                    for x in range(n):
+                        w = seen[x][:, None] & odd
+                        hit = w.any(0)
+                        total_odd = torch.where(w, vv, 0.0).sum(0)
+                        out[a + x, g] = torch.where(hit, total_odd, out[a + x, g])
+                size = torch.where(seen, q[a:b, g].abs() @ kk.abs().T, 0.0) * abs(scale)
+                big[a:b, g] = size.amax(1) if size.shape[1] else 0.0
+                lse[a:b, g] = (top + total.log()).squeeze(1)
+                weight[pg, h, row] += p.sum(0)
+    return out, lse, weight, {"absv": absv, "big": big}
+
+
+def check(s, window, first, causal=True, scale=None, add_weight=False, **given):
+    T, H, D = s["q"].shape
+    sc = 1 / math.sqrt(D) if scale is None else scale
+    out, lse, weight, tol = plain(s, causal, window, first, sc)
+    w = s["weight"].cuda() if add_weight else None
+    c = C.Cache(given.get("k", s["k"].cuda()), given.get("v", s["v"].cuda()), w)
+    got, got_lse = C.attend(given.get("q", s["q"].cuda()), batch_of(s), c, causal=causal, window=window, scale=scale,
+                            add_weight=add_weight, first=first)
+    slots = int(s["kv_len"].max()) if len(s["kv_len"]) else 0
+    x, e = got.cpu().double(), P.out_tolerance(s["q"].dtype, D, out, tol, slots)
+    bad = ~torch.where(out.isfinite(), (x - out).abs() <= e, (x == out) | (x.isnan() & out.isnan()))
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[0].tolist(), x[bad][0], out[bad][0], e[bad][0])
+    y = got_lse.cpu().double()
+    empty = lse == -math.inf
+    assert torch.equal(y == -math.inf, empty)
+    assert (empty | ((y - lse).abs() <= P.lse_tolerance(D, lse, tol))).all()
+    if add_weight:
+        z = w.cpu().double() - s["weight"].double()
+        rows = s["max_q"] * H // s["k"].shape[1]
+        assert ((z - weight).abs() <= P.weight_tolerance(D, s["weight"].double(), weight, tol, rows)).all()
+    return got, got_lse, w
+
+
+def give_back(s, window, first, what=-1):
+    """The pages that no row sees go out of the table."""
+    page = s["k"].shape[2]
+    n = s["offsets"][1:] - s["offsets"][:-1]
+    for i in range(len(s["kv_len"])):
+        oldest = int(s["kv_len"][i] - n[i]) - window + 1
+        for x in range(s["table"].shape[1]):
+            if x * page >= first and (x + 1) * page <= oldest:
+                s["table"][i, x] = what
+
+
+# -- on the CPU ------------------------------------------------------------------
+
+def test_attend_first_refuses():
+    lib = S.load()
+    assert lib.svf_kv_attend_first(cache(), batch(), attend(window=8), -1, None) == -1 and "first" in C.last_error()
+    for kw, text in ((dict(heads=7), "multiple of kv_heads"), (dict(window=-1), "window"), (dict(scale=NAN), "scale"),
+                     (dict(out=A + 8), "aligned"), (dict(lse=0), "NULL"), (dict(q=0), "NULL")):
+        assert lib.svf_kv_attend_first(cache(), batch(), attend(**kw), 4, None) == -1
+        assert text in C.last_error()
+    need = lib.svf_kv_attend_workspace(cache(), batch(), attend(add_weight=1, window=8))
+    assert lib.svf_kv_attend_first(cache(), batch(), attend(add_weight=1, window=8, workspace_bytes=need - 1), 4, None) == -1
+    assert "workspace" in C.last_error()
+    assert lib.svf_kv_attend_first(cache(), batch(num_tokens=0), attend(window=8), 4, None) == 0
+    assert lib.svf_kv_attend_first(None, batch(), attend(), 4, None) == -1 and "NULL" in C.last_error()
+
+
+# -- on the GPU ------------------------------------------------------------------
+
+gpu = pytest.mark.gpu
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+@pytest.mark.parametrize("page", [1, 16, 256])
+def test_single_tokens(dtype, heads, kv_heads, dim, page):
+    s = make(1, [1, 17, 0, 64, 65, 300, 2, 528, 129], [1, 1, 1, 1, 1, 1, 0, 1, 1], heads, kv_heads, dim, page, dtype, stats=True)
+    check(s, 64, 4)
+    check(s, 64, 4, add_weight=True)
+    give_back(s, 20, 33)
+    check(s, 20, 33, add_weight=True)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+@pytest.mark.parametrize("causal,window,first", [(True, 37, 4), (False, 5, 65), (True, 20, 200), (True, 1, 1)])
+def test_chunks(dtype, heads, kv_heads, dim, causal, window, first):
+    s = make(2, [350, 3, 1, 177, 40, 0, 200], [100, 3, 1, 2, 33, 5, 0], heads, kv_heads, dim, 16, dtype, stats=True)
+    check(s, window, first, causal=causal)
+    check(s, window, first, causal=causal, add_weight=True)
+
+
+@gpu
+@pytest.mark.parametrize("length", [1, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 191, 255, 257, 321, 513, 1025])
+@pytest.mark.parametrize("window", [1, 32, 100])
+@pytest.mark.parametrize("first", [1, 16, 17, 64, 130])
+def test_lengths_windows_and_first_tokens(length, window, first):
+    s = make(length, [length] * 3, [1, 2, 40], 8, 2, 128, 16, BF, stats=True)
+    check(s, window, first, add_weight=True)
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 2, 3, 5, 8, 9, 16, 17, 33, 64, 65, 129])
+@pytest.mark.parametrize("heads,kv_heads,dim,page", [(4, 1, 128, 16), (2, 2, 64, 32), (6, 2, 128, 1), (4, 2, 256, 64)])
+def test_every_number_of_new_tokens(new, heads, kv_heads, dim, page):
+    s = make(new, [new, new + 1, new + 330, max(new - 1, 0)], [new] * 4, heads, kv_heads, dim, page, BF, stats=True)
+    check(s, 70, 5, add_weight=True)
+    check(s, 130, 90, add_weight=True)
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 2, 24, 90])
+@pytest.mark.parametrize("what", [NAN, INF, -INF])
+@pytest.mark.parametrize("page", [8, 16, 128])
+def test_pages_given_back_and_what_the_others_hold(new, what, page):
+    """Neither a page that is not there nor what lies in slots that nobody sees matters."""
+    s = make(4, [1000, 700, 333], [new, 1, new], 8, 2, 128, page, BF, garbage=what, stats=True)
+    want = check(s, 100, 12, add_weight=True)
+    hidden = dict(s, k=s["k"].clone(), v=s["v"].clone())
+    n = s["offsets"][1:] - s["offsets"][:-1]
+    for i, length in enumerate(s["kv_len"].tolist()):
+        pg, row = P.slots_of(s["table"], i, length, page, s["k"].shape[0])
+        j = torch.arange(length)
+        out = (j >= 12) & (j < length - int(n[i]) - 100 + 1)
+        hidden["k"][pg[out], :, row[out]] = what
+        hidden["v"][pg[out], :, row[out]] = what
+    got = check(hidden, 100, 12, add_weight=True)
+    for x, y in zip(want, got):
+        assert torch.equal(x, y)
+    for gone in (-1, s["k"].shape[0], 2 ** 31 - 1):
+        give_back(s, 100, 12, gone)
+        got = check(s, 100, 12, add_weight=True)
+        for x, y in zip(want[:2], got[:2]):
+            assert torch.equal(x, y)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new,heads", [(1, 4), (2, 4), (8, 2), (40, 4), (100, 8)])
+@pytest.mark.parametrize("what", [NAN, INF, -INF])
+def test_values_that_are_not_numbers(dtype, new, heads, what):
+    """Seen in the first tokens by all, in the window by some, in between by none."""
+    s = make(8, [900, 450], [new, new], heads, 2, 128, 16, dtype)
+    for i, length in enumerate((900, 450)):
+        pg, row = P.slots_of(s["table"], i, length, 16, s["k"].shape[0])
+        s["v"][pg[100], :, row[100], ::5] = what            # nobody sees it
+        s["v"][pg[5], 0, row[5], 3] = what                  # everybody does
+        at = length - new - 150 + 2
+        s["v"][pg[at], 1, row[at], 7] = what                # some of the rows
+        s["v"][pg[length - 1], 1, row[length - 1], 100] = what
+    check(s, 150, 20)
+    check(s, 150, 70)
+    check(s, 150, 70, causal=False)
+    s["v"][:, 0, :, 64] = what
+    check(s, 150, 70)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,heads,kv_heads,dim", [(BF, 8, 1, 128), (HF, 4, 2, 64), (BF, 4, 1, 256)])
+@pytest.mark.parametrize("causal,window,first", [(True, 700, 300), (True, 2500, 64), (True, 300, 1000), (False, 700, 10)])
+def test_few_row_tiles_are_split(dtype, heads, kv_heads, dim, causal, window, first):
+    s = make(16, [6000, 3500, 700], [40, 61, 30], heads, kv_heads, dim, 16, dtype, stats=True)
+    check(s, window, first, causal=causal)
+    give_back(s, window, first)
+    check(s, window, first, causal=causal, add_weight=True)
+
+
+@gpu
+@pytest.mark.parametrize("what", [NAN, INF])
+@pytest.mark.parametrize("at", [0, 63, 64, 299, 5000, 5998])
+def test_split_tiles_and_values_that_are_not_numbers(what, at):
+    s = make(17, [6000], [40], 4, 1, 128, 16, BF)
+    pg, row = P.slots_of(s["table"], 0, 6000, 16, s["k"].shape[0])
+    s["v"][pg[at], 0, row[at], 9] = what
+    check(s, 2000, 300)
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 50])
+def test_no_window_every_token_or_none(new):
+    s = make(9, [500, 64, 700], [new, 1, new], 8, 2, 128, 16, BF, stats=True)
+
+    def run(window, first):
+        c = C.Cache(s["k"].cuda(), s["v"].cuda(), s["weight"].cuda())
+        return (*C.attend(s["q"].cuda(), batch_of(s), c, window=window, first=first, add_weight=True), c.weight)
+
+    same = lambda a, b: all(torch.equal(x, y) for x, y in zip(a, b))  # noqa: E731
+    assert same(run(0, 5), run(0, 0)) and same(run(0, 2 ** 31 - 1), run(0, 0))
+    assert same(run(2 ** 31 - 1, 7), run(0, 0))
+    for first in (699, 700, 2 ** 31 - 1):           # everything is visible, window or not
+        check(s, 64, first, add_weight=True)
+        a, b = run(64, first), run(0, 0)
+        assert all((x.double() - y.double()).abs().max() < 0.05 for x, y in zip(a, b))
+
+
+@gpu
+def test_first_tokens_in_one_page_with_the_window_and_pages_larger_than_both():
+    for page in (256, 1024):
+        for first, window in ((3, 10), (255, 1), (256, 256), (257, 100)):
+            s = make(10, [1, 300, 511, 512, 513, 900], [1, 2, 1, 1, 3, 60], 4, 2, 64, page, HF, stats=True)
+            check(s, window, first, add_weight=True)
+
+
+@gpu
+def test_too_many_new_tokens_is_nan_and_rows_without_a_slot():
+    s = make(11, [300, 400, 2], [1, 9, 30], 4, 2, 128, 16, BF)
+    b = batch_of(s)._replace(max_q=8)
+    out, lse = C.attend(s["q"].cuda(), b, C.Cache(s["k"].cuda(), s["v"].cuda()), window=50, first=6)
+    assert out[1:].isnan().all() and lse[1:].isnan().all() and not out[0].isnan().any()
+    out, lse, _ = check(s, 50, 6)
+    assert (out[10:38] == 0).all() and (lse[10:38] == -INF).all()
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 4, 70])
+def test_strides(new):
+    s = make(12, [800, 333], [new, new], 4, 2, 128, 16, BF, stats=True)
+    flat = lambda x: x.transpose(1, 2).contiguous().cuda().transpose(1, 2)  # noqa: E731
+    wide = torch.zeros((2 * new, 9, 128), dtype=BF, device="cuda")
+    wide[:, 3:7] = s["q"].cuda()
+    check(s, 90, 40, add_weight=True, k=flat(s["k"]), v=flat(s["v"]), q=wide[:, 3:7])
+
+
+@gpu
+def test_a_long_cache():
+    """Slots past 65,536 of two sequences, the pages between given back."""
+    lens, page = [70001, 66000], 64
+    s = {"kv_len": torch.tensor(lens, dtype=torch.int32), "offsets": torch.tensor([0, 1, 34], dtype=torch.int32), "max_q": 33}
+    g = torch.Generator().manual_seed(3)
+    width = -(-lens[0] // page)
+    s["table"] = torch.full((2, width), -1, dtype=torch.int32)
+    held = [[p for p in range(width) if p * page < 200 or (p * page < n and (p + 1) * page > n - 33 - 2000)] for n in lens]
+    perm = torch.randperm(sum(map(len, held)), generator=g).int()
+    s["table"][0, held[0]], s["table"][1, held[1]] = perm[:len(held[0])], perm[len(held[0]):]
+    pool = len(perm)
+    s["k"], s["v"] = (torch.randn((pool, 2, page, 128), generator=g).to(BF) for _ in range(2))
+    s["q"] = torch.randn((34, 8, 128), generator=g).to(BF)
+    s["weight"] = torch.rand((pool, 2, page), generator=g)
+    check(s, 2000, 200, add_weight=True)
+
+
+@gpu
+def test_the_same_every_time_on_another_stream_and_in_a_graph():
+    s = make(13, [1000, 750, 6000], [1, 9, 40], 8, 2, 128, 16, BF, stats=True)
+    b, q, k, v = batch_of(s), s["q"].cuda(), s["k"].cuda(), s["v"].cuda()
+
+    def step(q, w):
+        out, lse = C.attend(q, b, C.Cache(k, v, w), window=500, first=20, add_weight=True)
+        return out, lse
+
+    w = s["weight"].cuda()
+    want = (*step(q, w), w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        w = s["weight"].cuda()
+        got = (*step(q, w), w)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
+    held, start, qg = s["weight"].cuda(), s["weight"].cuda(), q.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held.copy_(start)
+        got = (*step(qg, held), held)
+    for seed in range(3):
+        qg.copy_(q.roll(seed, 0))
+        w = s["weight"].cuda()
+        want = (*step(q.roll(seed, 0), w), w)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+@gpu
+def test_first_is_refused_where_it_is_no_number_of_tokens():
+    s = make(14, [10], [1], 4, 2, 64, 16, BF)
+    for bad in (-1, 2 ** 31):
+        with pytest.raises(S.SvfError, match="first"):
+            C.attend(s["q"].cuda(), batch_of(s), C.Cache(s["k"].cuda(), s["v"].cuda()), window=4, first=bad)
