@@ -39,17 +39,17 @@ enum {
     SVF_LOGITS_F32 = 2
 };
 
-enum { SVF_LOGPROB_MOST_TOP = 64 };
+enum { SVF_LOGPROB_MOST_TOP = 64, SVF_LOGPROB_MOST_VOCAB = 1 << 21 };
 
 /*
  *   logits       [rows][vocab], row_stride elements from row to row (0 and up), vocab contiguous; any
  *                alignment that the type has
  *   token        [rows], int32 or int64 as token_bytes says (4 or 8)
- *   top          0 .. 64, no more than vocab;  scale > 0, finite (1 / temperature)
+ *   vocab        1 .. 2^21;  top 0 .. 64, no more than vocab;  scale (1 / temperature) > 0, below 2^126
  *   logprob, entropy   float [rows];  rank int32 [rows]
  *   top_logprob, top_index   float and int32 [rows][top]
  *   workspace    svf_logprob_workspace bytes, 256-byte aligned, nothing kept in it
- * rows * top and rows + vocab below 2^31.
+ * rows * top below 2^31, rows (some 2^24) such that a launch has fewer than 2^32 threads.
  */
 typedef struct svf_logprob_args {
     const void *logits;

@@ -2,97 +2,501 @@
 #include "svf_kv_device.h"
 #include "svf_logprob.h"
 
+#pragma clang fp contract(off)  // a reference and a distance from it are rounded as they are written
+
 namespace svfp {
 namespace {
 
 constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kEntries = 4096;   // pieces of a row whose largest logits are kept in LDS
+constexpr int kListed = 512;    // of them that may hold one of the best
+constexpr int kCand = kEntries / 2;  // logits that may be one of the best, in the pieces' place
+constexpr int kMostParts = 64;
+
+// What a part of a row found: its largest logit, the sum of 2^y and of y 2^y over its logits, y their distance from that in log2 terms, and how
+// many come before the token.
+struct Part {
+    float m, s, sy;
+    int32_t before;
+};
+
+// How a row is dealt out.
+struct Plan {
+    int32_t parts;   // workgroups of a row
+    int32_t per;     // whole 16-byte vectors of a part, a multiple of 64
+    int32_t group;   // log2 of the vectors of a piece: 0, or 3 where there would be more than kEntries
+    Part* part;      // [rows][parts] (parts > 1)
+    uint64_t* keys;  // [rows][parts][top]
+};
 
 // A logit's place in the order as a whole number, larger first: -0 as 0, NaN below all.
 __device__ inline uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return x != x ? 0u : u >> 31 ? ~u : u | 0x80000000u;
 }
-// With the index behind it, so that no two are equal.
+__device__ inline float logit_of(uint32_t order) {
+    return order == 0 ? __builtin_nanf("") : __uint_as_float(order >> 31 ? order & 0x7fffffffu : ~order);
+}
+// With the index behind it, so that no two are equal; 0 is none.
 __device__ inline uint64_t key_of(float x, int i) { return (uint64_t)order_of(x) << 32 | (uint32_t)~i; }
 
-__device__ inline int64_t token_of(const Args& p, int row) {
-    return p.token_wide ? ((const int64_t*)p.token)[row] : ((const int32_t*)p.token)[row];
+// The next number above (NaN above +infinity).
+__device__ inline float above(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return __uint_as_float(u >> 31 ? u - 1 : u + 1);
 }
 
-template <class V, class Op>
+template <class T>
+struct Logits {
+    static constexpr int W = 16 / sizeof(T);  // of a vector
+    static __device__ inline float at(const uint4& w, int i) {
+        const uint32_t x = (&w.x)[i * (int)sizeof(T) / 4];
+        if constexpr (sizeof(T) == 4) return __uint_as_float(x);
+        if constexpr (__is_same(T, __bf16)) return __uint_as_float(i & 1 ? x & 0xffff0000u : x << 16);
+        if constexpr (__is_same(T, _Float16)) return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? x >> 16 : x));
+    }
+    static __device__ inline float largest(const uint4& w) {
+        if constexpr (__is_same(T, _Float16)) {  // two at a time
+            typedef _Float16 V2 __attribute__((ext_vector_type(2)));
+            const V2 x = __builtin_elementwise_max(
+                __builtin_elementwise_max(__builtin_bit_cast(V2, w.x), __builtin_bit_cast(V2, w.y)),
+                __builtin_elementwise_max(__builtin_bit_cast(V2, w.z), __builtin_bit_cast(V2, w.w)));
+            return fmaxf((float)x.x, (float)x.y);
+        }
+        float x = fmaxf(at(w, 0), at(w, 1));
+#pragma unroll
+        for (int i = 2; i < W; i += 2) x = fmaxf(x, fmaxf(at(w, i), at(w, i + 1)));
+        return x;
+    }
+};
+
+template <int NT, class V, class Op>
 __device__ inline V over_group(V x, Op op) {
-    __shared__ V part[4];
+    __shared__ V part[NT / 64];
     for (int d = 32; d; d >>= 1) x = op(x, __shfl_xor(x, d));
     __syncthreads();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    return op(op(part[0], part[1]), op(part[2], part[3]));
+    x = part[0];
+    for (int i = 1; i < NT / 64; i++) x = op(x, part[i]);
+    return x;
 }
 
-// A row by a workgroup, one sum after another.
+// The larger of eight lanes in each of them.
+__device__ inline float max_of_8(float x) {
+    auto with = [](float x, auto ctrl) {
+        const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true);
+        return fmaxf(x, __int_as_float(y));
+    };
+    x = with(x, std::integral_constant<int, 0xb1>{});   // quad_perm 1 0 3 2
+    x = with(x, std::integral_constant<int, 0x4e>{});   // quad_perm 2 3 0 1
+    return with(x, std::integral_constant<int, 0x141>{});  // the eight lanes the other way round
+}
+
+// The distance of a logit from the largest of all in log2 terms (by halves, so that it does not pass what 32 bits hold on the way).
+__device__ inline float distance(float x, float m, float scale2) { return (0.5f * x - 0.5f * m) * (2.f * scale2); }
+
+// What a row's scalars come to.
+__device__ inline void write_row(const Args& p, int row, const Part& x, bool known, float mine) {
+    const bool none = x.m == -INFINITY && x.s == 0.f, bad = !(x.s * 0.f == 0.f) || x.m == INFINITY;
+    const float total = __builtin_amdgcn_logf(x.s) * kLn2, nan = __builtin_nanf("");
+    p.logprob[row] = !known || bad ? nan : none ? -INFINITY : distance(mine, x.m, p.scale) - total;
+    p.entropy[row] = bad ? nan : none ? 0.f : total - x.sy / x.s * kLn2;
+    p.rank[row] = known ? x.before : -1;
+}
+__device__ inline void write_top(const Args& p, int row, int at, const Part& x, uint64_t key) {
+    const bool none = x.m == -INFINITY && x.s == 0.f, bad = !(x.s * 0.f == 0.f) || x.m == INFINITY;
+    const float total = __builtin_amdgcn_logf(x.s) * kLn2;
+    p.top_index[(int64_t)row * p.top + at] = (int)~(uint32_t)key;
+    p.top_logprob[(int64_t)row * p.top + at] =
+        bad ? __builtin_nanf("") : none ? -INFINITY : distance(logit_of((uint32_t)(key >> 32)), x.m, p.scale) - total;
+}
+
+// The logits of one part: vectors [v0, v1) of the row's aligned grid, and with the first part the up to 2 (W - 1) logits before the
+// first and behind the last whole vector.  Vector v holds the logits v * W - off and following.
 template <class T>
-__global__ __launch_bounds__(256) void k_logprob(Args p) {
-    const int row = blockIdx.x, tid = threadIdx.x, V = p.vocab;
-    const T* x = (const T*)(p.logits + row * p.row_stride);
+struct Span {
+    const T* x;
+    int off, lead, tail, vocab;  // logits [0, lead) and [tail, vocab) lie outside whole vectors
+    int v0, v1;
+    bool edges;
+    __device__ inline int edge_count() const { return edges ? lead + vocab - tail : 0; }
+    __device__ inline int edge(int i) const { return i < lead ? i : tail + i - lead; }
+    // all of the part, in rising order
+    __device__ inline int body() const { return v0 * Logits<T>::W - off; }
+    __device__ inline int count() const { return edge_count() + (v1 - v0) * Logits<T>::W; }
+    __device__ inline int nth(int i) const {
+        const int first = edges ? lead : 0, in = (v1 - v0) * Logits<T>::W;
+        return i < first ? i : i - first < in ? body() + i - first : tail + i - first - in;
+    }
+};
+
+template <class T>
+__device__ inline Span<T> span_of(const Args& p, const Plan& plan, int row, int part) {
+    constexpr int W = Logits<T>::W;
+    Span<T> s;
+    s.x = (const T*)(p.logits + row * p.row_stride);
+    s.vocab = p.vocab;
+    s.off = (int)((uint64_t)s.x & 15) / (int)sizeof(T);
+    s.lead = min(s.vocab, s.off ? W - s.off : 0);
+    const int first = s.off ? 1 : 0, end = max(first, (s.vocab + s.off) / W);
+    s.tail = min(s.vocab, max(s.lead, end * W - s.off));
+    s.v0 = (int)min((int64_t)end, first + (int64_t)part * plan.per);
+    s.v1 = min(end, s.v0 + plan.per);
+    s.edges = part == 0;
+    return s;
+}
+
+// One pass over a row's logits, or a part of them, in 16-byte loads, 64 bytes a lane on their way while as many are worked on. Each lane
+// keeps sums of 2^y and y 2^y, y the distance from a reference of its own that follows the largest logit it has met where that has
+// grown by more than 2^8.  Logits that may come before the token are counted only where a vector has one: with likely tokens hardly anywhere.
+//
+// The best alternatives: the largest logit of every piece of the row (128 bytes, the vectors of eight lanes, or one
+// vector where the row is short) goes to LDS.  Pieces in 64 (or all threads') bins: the top-th largest of the bins' best is a bound that at
+// least ``top`` logits reach, so only pieces whose largest reaches it are read again, some more than ``top``, and of their logits those that reach it
+// are put in order by counting.  Where too many reach it (long runs of large logits), ``top`` rounds over the row find them one
+// by one; where too few are larger than -infinity, the lowest indices follow.
+template <class T, int NT, bool TOP>
+__global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan plan) {
+    using L = Logits<T>;
+    constexpr int W = L::W, U = 4;
+    constexpr float kSlack = 8.f;
+    __shared__ float largest[TOP ? kEntries : 1];
+    __shared__ uint16_t listed[TOP ? kListed : 1];
+    __shared__ uint64_t bins[TOP ? NT : 1];
+    __shared__ uint64_t sh_bound;
+    __shared__ int sh_listed, sh_cand;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = blockIdx.x / plan.parts, part = blockIdx.x - row * plan.parts;
+    const Span<T> s = span_of<T>(p, plan, row, part);
     auto add = [](auto a, auto b) { return a + b; };
-    const int64_t token = token_of(p, row);
-    const bool known = token >= 0 && token < V;
-    const uint64_t mine = known ? key_of((float)x[token], (int)token) : 0;
-    float m = -INFINITY, bad = 0.f;
+    const int64_t token = p.token_wide ? ((const int64_t*)p.token)[row] : ((const int32_t*)p.token)[row];
+    const bool known = token >= 0 && token < p.vocab;
+    const float mine = known ? (float)s.x[token] : __builtin_nanf("");
+    const float over = mine == mine ? above(mine) : mine;
+    const int vt = known ? ((int)token + s.off) / W : 0, vb = min(vt, s.v1);  // its vector, and the last one before it
+
+    float m = -INFINITY, b = 3e38f, sum = 0.f, sumy = 0.f;
     int before = 0;
-    for (int i = tid; i < V; i += 256) {
-        const float y = (float)x[i];
-        m = fmaxf(m, y);
-        bad += y == INFINITY || y != y ? 1.f : 0.f;
-        before += key_of(y, i) > mine;
+    const float c = p.scale2;
+    const uint4* at = (const uint4*)((uint64_t)s.x & ~(uint64_t)15);
+    auto work = [&](const uint4(&w)[U], int v, bool all) {
+        float top[U];
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            top[u] = L::largest(w[u]);
+            most = fmaxf(most, top[u]);
+            if constexpr (TOP) {
+                const int e = v - s.v0 + u * NT;
+                if (plan.group) {
+                    const float x = max_of_8(top[u]);
+                    if ((lane & 7) == 0 && (all || v + u * NT < s.v1)) largest[e >> 3] = x;
+                } else if (all || v + u * NT < s.v1) {
+                    largest[e] = top[u];
+                }
+            }
+        }
+        m = fmaxf(m, most);
+        const float far = fmaf(most, c, b);
+        if (__any(far > kSlack)) {
+            const float now = far > kSlack ? -most * c : b, step = now - b, keep = __builtin_amdgcn_exp2f(step);
+            sumy = keep * fmaf(sum, step, sumy);
+            sum *= keep;
+            b = now;
+        }
+        if (__any(most >= mine)) {
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const float least = v + u * NT < vb ? mine : over;
+#pragma unroll
+                for (int i = 0; i < W; i++) before += L::at(w[u], i) >= least;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < W; i++) {
+                const float y = fmaf(L::at(w[u], i), c, b), e = __builtin_amdgcn_exp2f(y);
+                sum += e;
+                sumy = fmaf(e, fmaxf(y, -200.f), sumy);  // 0 times -infinity is 0
+            }
+    };
+    int v = s.v0 + tid;
+    // (the last vectors of a part by themselves: logits of -infinity in the place of those that are not there)
+    constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;
+    const int whole = (s.v1 - s.v0) / (U * NT);
+    uint4 next[U];
+    if (whole > 0) {
+#pragma unroll
+        for (int u = 0; u < U; u++) next[u] = at[v + u * NT];
     }
-    m = over_group(m, [](float a, float b) { return fmaxf(a, b); });
-    bad = over_group(bad, add);
-    before = over_group(before, add);
-    const bool none = m == -INFINITY;
-    float s = 0.f, sx = 0.f;
-    for (int i = tid; i < V && !none; i += 256) {
-        const float y = (0.5f * (float)x[i] - 0.5f * m) * (2.f * p.scale2), e = __builtin_amdgcn_exp2f(y);
-        s += e;
-        sx += e * fmaxf(y, -200.f);  // 0 times -infinity is 0
+    for (int it = 0; it < whole; it++, v += U * NT) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) w[u] = next[u];
+        if (it + 1 < whole) {
+#pragma unroll
+            for (int u = 0; u < U; u++) next[u] = at[v + (U + u) * NT];
+        }
+        work(w, v, true);
     }
-    s = over_group(s, add);
-    sx = over_group(sx, add);
-    // (halves, and in natural terms: no difference of two numbers passes what 32 bits hold on the way)
-    const float total = __builtin_amdgcn_logf(s) * kLn2, nan = __builtin_nanf("");
-    auto lp = [&](float y) { return bad != 0.f ? nan : none ? -INFINITY : (0.5f * y - 0.5f * m) * (2.f * p.scale) - total; };
+    if (__any(v < s.v1)) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            w[u] = make_uint4(kNone, kNone, kNone, kNone);
+            if (v + u * NT < s.v1) w[u] = at[v + u * NT];
+        }
+        work(w, v, false);
+    }
+    const int edges = s.edge_count();
+    const uint64_t mine_key = known ? key_of(mine, (int)token) : ~0ull;
+    if (tid < edges) {
+        const int i = s.edge(tid);
+        const float x = (float)s.x[i];
+        m = fmaxf(m, x);
+        const float far = fmaf(x, c, b);
+        if (far > kSlack) {
+            const float step = -x * c - b, keep = __builtin_amdgcn_exp2f(step);
+            sumy = keep * fmaf(sum, step, sumy);
+            sum *= keep;
+            b = -x * c;
+        }
+        const float y = fmaf(x, c, b), e = __builtin_amdgcn_exp2f(y);
+        sum += e;
+        sumy = fmaf(e, fmaxf(y, -200.f), sumy);
+        before += mine == mine && key_of(x, i) > mine_key;
+    }
+    if (known && tid == 0 && vt >= s.v0 && vt < s.v1)  // equal logits before the token in its own vector
+        for (int i = vt * W - s.off; i < (int)token; i++) before += (float)s.x[i] == mine;
+
+    Part x;
+    x.m = over_group<NT>(m, [](float a, float b) { return fmaxf(a, b); });
+    {
+        const float d = fmaf(x.m, c, b), f = x.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-d), dc = fminf(d, 1000.f);
+        x.s = over_group<NT>(sum * f, add);
+        x.sy = over_group<NT>(f * fmaf(sum, -dc, sumy), add);
+    }
+    x.before = over_group<NT>(before, add);
+    // Logits so large that a reference in log2 terms is rounded by more than 2^-4, or none in 32 bits: once more, each distance by itself.
+    if (x.m != -INFINITY && !(fabsf(x.m * c) < 1048576.f) && x.m != INFINITY) {
+        sum = sumy = 0.f;
+        for (int i = tid; i < s.count(); i += NT) {
+            const float y = distance((float)s.x[s.nth(i)], x.m, c), e = __builtin_amdgcn_exp2f(y);
+            sum += e;
+            sumy = fmaf(e, fmaxf(y, -200.f), sumy);
+        }
+        x.s = over_group<NT>(sum, add);
+        x.sy = over_group<NT>(sumy, add);
+    }
+    if (known && mine != mine) {  // a token that is no number comes behind all that are
+        before = 0;
+        for (int i = tid; i < s.count(); i += NT) before += key_of((float)s.x[s.nth(i)], s.nth(i)) > mine_key;
+        x.before = over_group<NT>(before, add);
+    }
     if (tid == 0) {
-        p.logprob[row] = known ? lp((float)x[token]) : nan;
-        p.entropy[row] = bad != 0.f ? nan : none ? 0.f : total - sx / s * kLn2;
-        p.rank[row] = known ? before : -1;
+        if (plan.parts == 1)
+            write_row(p, row, x, known, mine);
+        else
+            plan.part[blockIdx.x] = x;
     }
-    uint64_t last = ~0ull;
-    for (int k = 0; k < p.top; k++) {
+    if constexpr (TOP) {
+        auto emit = [&](int at, uint64_t key) {
+            if (plan.parts == 1)
+                write_top(p, row, at, x, key);
+            else
+                plan.keys[(int64_t)blockIdx.x * p.top + at] = key;
+        };
+        // the bound
+        const int shift = plan.group, entries = (s.v1 - s.v0 + (1 << shift) - 1) >> shift;
+        auto entry_key = [&](int e) { return largest[e] > -INFINITY ? key_of(largest[e], e) : 0; };
         uint64_t best = 0;
-        for (int i = tid; i < V; i += 256) {
-            const uint64_t key = key_of((float)x[i], i);
-            if (key < last && key > best) best = key;
+        for (int e = tid; e < entries; e += NT) best = max(best, entry_key(e));
+        bins[tid] = best;
+        if (tid == 0) sh_bound = 0, sh_listed = 0, sh_cand = 0;
+        __syncthreads();
+        if (p.top <= 32) {
+            if (wave == 0) {
+#pragma unroll
+                for (int i = 1; i < NT / 64; i++) best = max(best, bins[i * 64 + lane]);
+                int larger = 0;
+                const int lo = (int)(uint32_t)best, hi = (int)(best >> 32);
+#pragma unroll
+                for (int i = 0; i < 64; i++) {
+                    const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, i);
+                    larger += y > best;
+                }
+                if (larger == p.top - 1 && best != 0) sh_bound = best;
+            }
+        } else {
+            int larger = 0;
+#pragma unroll 8
+            for (int i = 0; i < NT; i++) larger += bins[i] > best;
+            if (larger == p.top - 1 && best != 0) sh_bound = best;
         }
-        last = over_group(best, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-        if (tid == 0) {
-            const int at = (int)~(uint32_t)last;
-            p.top_index[row * p.top + k] = at;
-            p.top_logprob[row * p.top + k] = lp((float)x[at]);
+        __syncthreads();
+        const uint64_t bound = sh_bound;
+        for (int e = tid; e < entries; e += NT) {
+            const uint64_t key = entry_key(e);
+            if (key == 0 || key < bound) continue;
+            const int to = atomicAdd(&sh_listed, 1);
+            if (to < kListed) listed[to] = (uint16_t)e;
+        }
+        __syncthreads();
+        // the logits that reach it, in the pieces' place
+        uint64_t* cand = (uint64_t*)largest;
+        const int pieces = min(sh_listed, kListed);
+        for (int i = tid; i < pieces << shift; i += NT) {
+            const int e = listed[i >> shift], v = s.v0 + (e << shift) + (i & ((1 << shift) - 1));
+            if (v >= s.v1) continue;
+            const uint4 w = at[v];
+#pragma unroll
+            for (int j = 0; j < W; j++) {
+                const float y = L::at(w, j);
+                if (!(y > -INFINITY) || key_of(y, e) < bound) continue;
+                const int to = atomicAdd(&sh_cand, 1);
+                if (to < kCand) cand[to] = key_of(y, v * W - s.off + j);
+            }
+        }
+        if (tid < edges) {
+            const float y = (float)s.x[s.edge(tid)];
+            if (y > -INFINITY) {
+                const int to = atomicAdd(&sh_cand, 1);
+                if (to < kCand) cand[to] = key_of(y, s.edge(tid));
+            }
+        }
+        __syncthreads();
+        int n = sh_cand;
+        if (n <= kCand && sh_listed <= kListed) {
+            // too few: the lowest indices of -infinity, then of NaN
+            for (int kind = 0; kind < 2 && n < p.top; kind++)
+                for (int i0 = 0; i0 < s.count() && n < p.top; i0 += NT) {
+                    const int i = i0 + tid, j = i < s.count() ? s.nth(i) : 0;
+                    const float y = i < s.count() ? (float)s.x[j] : 0.f;
+                    const bool hit = kind ? y != y : y == -INFINITY;
+                    const uint64_t mask = __ballot(hit);
+                    __syncthreads();
+                    if (lane == 0) bins[wave] = __popcll(mask);
+                    __syncthreads();
+                    int to = n + __popcll(mask & ((1ull << lane) - 1));
+                    for (int w = 0; w < NT / 64; w++) {
+                        if (w < wave) to += (int)bins[w];
+                        n += (int)bins[w];
+                    }
+                    if (hit && to < kCand) cand[to] = key_of(y, j);
+                }
+            n = min(n, kCand);
+            __syncthreads();
+            for (int i = tid; i < n; i += NT) {
+                const uint64_t key = cand[i];
+                int larger = 0;
+#pragma unroll 8
+                for (int j = 0; j < n; j++) larger += cand[j] > key;
+                if (larger < p.top) emit(larger, key);
+            }
+            for (int i = n + tid; i < p.top; i += NT) emit(i, 0);  // a part with fewer logits
+        } else {
+            uint64_t last = ~0ull;
+            for (int k = 0; k < p.top; k++) {
+                best = 0;
+                for (int i = tid; i < s.count() && last; i += NT) {
+                    const uint64_t key = key_of((float)s.x[s.nth(i)], s.nth(i));
+                    if (key < last) best = max(best, key);
+                }
+                last = over_group<NT>(best, [](uint64_t a, uint64_t b) { return max(a, b); });
+                if (tid == 0) emit(k, last);
+            }
         }
     }
+}
+
+// The parts of a row: its scalars, and of the parts' best the best.
+template <class T>
+__global__ __launch_bounds__(256) void k_join(Args p, Plan plan) {
+    __shared__ uint64_t cand[kCand];
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const int64_t token = p.token_wide ? ((const int64_t*)p.token)[row] : ((const int32_t*)p.token)[row];
+    const bool known = token >= 0 && token < p.vocab;
+    Part x = lane < plan.parts ? plan.part[(int64_t)row * plan.parts + lane] : Part{-INFINITY, 0.f, 0.f, 0};
+    float m = x.m;
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    const float d = m == -INFINITY ? 0.f : x.m == -INFINITY ? -INFINITY : distance(x.m, m, p.scale2), f = __builtin_amdgcn_exp2f(d);
+    x.sy = f * fmaf(x.s, fmaxf(d, -1000.f), x.sy);
+    x.s *= f;
+    for (int k = 32; k; k >>= 1) {
+        x.s += __shfl_xor(x.s, k);
+        x.sy += __shfl_xor(x.sy, k);
+        x.before += __shfl_xor(x.before, k);
+    }
+    x.m = m;
+    if (tid == 0) write_row(p, row, x, known, known ? (float)((const T*)(p.logits + row * p.row_stride))[token] : 0.f);
+    const int n = plan.parts * p.top;
+    for (int i = tid; i < n; i += 256) cand[i] = plan.keys[(int64_t)row * n + i];
+    __syncthreads();
+    for (int i = tid; i < n; i += 256) {
+        const uint64_t key = cand[i];
+        int larger = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; j++) larger += cand[j] > key;
+        if (key != 0 && larger < p.top) write_top(p, row, larger, x, key);
+    }
+}
+
+struct Layout {
+    int32_t parts, per, group, threads;
+    int64_t keys, bytes;
+};
+
+Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
+    Layout y;
+    const int64_t vectors = (int64_t)vocab / (dtype == SVF_LOGITS_F32 ? 4 : 8) + 1;
+    y.threads = rows >= 1024 ? 256 : 1024;
+    // as many parts as the GPU has room for and as many candidates as a join can order, none of fewer vectors than threads
+    int64_t parts = y.threads == 256 ? 1 : 512 / (rows < 1 ? 1 : rows);
+    if (parts > vectors / (4 * y.threads)) parts = vectors / (4 * y.threads);
+    if (top > 0 && parts > kCand / 4 / top) parts = kCand / 4 / top;
+    // a part's pieces have to fit
+    const int64_t least = (vectors + kEntries * 8 - 1 - 64) / (kEntries * 8 - 64);
+    if (parts < least) parts = least;
+    if (parts > kMostParts) parts = kMostParts;
+    if (parts < 1) parts = 1;
+    y.parts = (int32_t)parts;
+    y.per = (int32_t)(((vectors + parts - 1) / parts + 63) & ~int64_t(63));
+    y.group = y.per <= kEntries ? 0 : 3;
+    y.keys = ((int64_t)rows * parts * (int64_t)sizeof(Part) + 255) & ~int64_t(255);
+    y.bytes = parts == 1 ? 0 : y.keys + (int64_t)rows * parts * top * 8;
+    return y;
+}
+
+template <class T>
+hipError_t launch_type(const Args& a, const Layout& y, hipStream_t s) {
+    const Plan plan{y.parts, y.per, y.group, (Part*)a.ws, (uint64_t*)(a.ws + y.keys)};
+    const dim3 grid((unsigned)(a.rows * y.parts));
+    hipError_t e;
+    if (y.threads == 256)
+        e = a.top ? svfk::run(k_score<T, 256, true>, grid, 256, s, a, plan) : svfk::run(k_score<T, 256, false>, grid, 256, s, a, plan);
+    else
+        e = a.top ? svfk::run(k_score<T, 1024, true>, grid, 1024, s, a, plan) : svfk::run(k_score<T, 1024, false>, grid, 1024, s, a, plan);
+    if (e != hipSuccess || y.parts == 1) return e;
+    return svfk::run(k_join<T>, dim3(a.rows), 256, s, a, plan);
 }
 
 }  // namespace
 
-int64_t workspace(int32_t, int32_t, int32_t, int32_t) { return 0; }
+int64_t workspace(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) { return layout(rows, vocab, top, dtype).bytes; }
 
-int64_t threads(int32_t rows, int32_t, int32_t, int32_t) { return (int64_t)rows * 256; }
+int64_t threads(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
+    const Layout y = layout(rows, vocab, top, dtype);
+    return (int64_t)rows * y.parts * y.threads;
+}
 
 hipError_t launch(const Args& a, int32_t dtype, hipStream_t s) {
-    const dim3 grid(a.rows);
-    return dtype == SVF_LOGITS_BF16  ? svfk::run(k_logprob<__bf16>, grid, 256, s, a)
-           : dtype == SVF_LOGITS_F16 ? svfk::run(k_logprob<_Float16>, grid, 256, s, a)
-                                     : svfk::run(k_logprob<float>, grid, 256, s, a);
+    const Layout y = layout(a.rows, a.vocab, a.top, dtype);
+    return dtype == SVF_LOGITS_BF16  ? launch_type<__bf16>(a, y, s)
+           : dtype == SVF_LOGITS_F16 ? launch_type<_Float16>(a, y, s)
+                                     : launch_type<float>(a, y, s);
 }
 
 }  // namespace svfp

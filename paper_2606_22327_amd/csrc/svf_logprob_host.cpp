@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 
@@ -32,13 +33,13 @@ int64_t item(const svf_logprob_args* a) { return a->dtype == SVF_LOGITS_F32 ? 4 
 
 int check(const svf_logprob_args* a) {
     if (!a) return fail(SVF_EINVAL, "args must not be NULL");
-    if (a->rows < 0 || a->vocab < 1) return fail(SVF_EINVAL, "rows must be >= 0 and vocab >= 1 (%d, %d)", a->rows, a->vocab);
+    if (a->rows < 0 || a->vocab < 1 || a->vocab > SVF_LOGPROB_MOST_VOCAB)
+        return fail(SVF_EINVAL, "rows must be >= 0 and vocab in 1 .. %d (%d, %d)", SVF_LOGPROB_MOST_VOCAB, a->rows, a->vocab);
     if (a->top < 0 || a->top > SVF_LOGPROB_MOST_TOP || a->top > a->vocab)
         return fail(SVF_EINVAL, "top must be in 0 .. %d and no more than vocab (%d, %d)", SVF_LOGPROB_MOST_TOP, a->top, a->vocab);
     if (a->dtype != SVF_LOGITS_BF16 && a->dtype != SVF_LOGITS_F16 && a->dtype != SVF_LOGITS_F32)
         return fail(SVF_EINVAL, "unknown dtype %d", a->dtype);
-    if ((int64_t)a->rows + a->vocab >= kLimit31 || (int64_t)a->rows * a->top >= kLimit31)
-        return fail(SVF_EINVAL, "rows + vocab and rows * top must be below 2^31");
+    if ((int64_t)a->rows * a->top >= kLimit31) return fail(SVF_EINVAL, "rows * top must be below 2^31");
     if (svfp::threads(a->rows, a->vocab, a->top, a->dtype) >= kThreadLimit) return fail(SVF_EINVAL, "rows is too large (%d)", a->rows);
     return SVF_OK;
 }
@@ -59,7 +60,7 @@ int svf_logprob(const svf_logprob_args* a, void* hip_stream) {
     if (a->row_stride < 0 || a->row_stride >= kStrideLimit) return fail(SVF_EINVAL, "row_stride must be in 0 .. 2^40");
     if (a->token_bytes != 4 && a->token_bytes != 8) return fail(SVF_EINVAL, "token_bytes must be 4 or 8 (%d)", a->token_bytes);
     const float scale = a->scale * 1.4426950408889634f;  // for powers of two
-    if (!(scale > 0.f) || !(scale - scale == 0.f)) return fail(SVF_EINVAL, "scale must be above 0 and below 2^127");
+    if (!(scale > 0.f) || !(2.f * scale < INFINITY)) return fail(SVF_EINVAL, "scale must be above 0 and below 2^126");
     if (a->rows == 0) return SVF_OK;
     if (!a->logits || !a->token || !a->logprob || !a->entropy || !a->rank || (a->top > 0 && (!a->top_logprob || !a->top_index)))
         return fail(SVF_EINVAL, "logits, token and outputs must not be NULL");

@@ -28,7 +28,7 @@ def args(**kw):
     (dict(scale=3e38), "scale"), (dict(scale=1e-45), "scale"),
     (dict(logits=0), "NULL"), (dict(token=0), "NULL"), (dict(rank=0), "NULL"), (dict(top_index=0), "NULL"),
     (dict(logits=A + 1), "aligned"), (dict(logits=A + 2, dtype=2), "aligned"), (dict(token=A + 4), "aligned"),
-    (dict(vocab=(1 << 31) - 4), "2^31"), (dict(rows=1 << 26, top=32), "2^31"),
+    (dict(vocab=(1 << 21) + 1), "vocab"), (dict(rows=1 << 26, top=32), "2^31"), (dict(rows=1 << 24, top=0), "rows"),
 ])
 def test_score_refuses(kw, text):
     if kw.get("scale") == 1e-45:
