@@ -169,6 +169,127 @@ __global__ __launch_bounds__(64) void k_append_any(AppendArgs p) {
 
 // Positions with several axes: a pair turns by its axis' position.  The row of the table that it takes its cosine and sine
 // from is another for each axis; an axis whose position is outside the table makes NaN of its own pairs alone.
+__device__ inline int axis_of(const AxesArgs& x, int pair) { return x.of_pair[pair >> 4] >> 2 * (pair & 15) & 3; }
+
+// As in k_append_wide, for rotated parts of any size from 16 on and rows at any address: the pairs are taken eight at a time, the last eight
+// again from the end, so that two lanes may turn the same pair (both have read it before either writes: they are lanes of one
+// wave), and a 16-byte access may lie across two lines.  The rest of a head is copied 16 elements at a time in the same way.
+struct Units {
+    int turned, all;  // of a head: units of eight pairs, and with those that are copied
+};
+template <class E>
+__global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Units units, int groups, int per) {
+    using T = typename E::T;
+    typedef T V8 __attribute__((ext_vector_type(8), aligned(2)));
+    typedef T V2 __attribute__((ext_vector_type(2), aligned(2)));
+    typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int wave = __builtin_amdgcn_readfirstlane((int)((blockIdx.x * 256 + threadIdx.x) >> 6));
+    const int t = wave / groups, group = wave - t * groups;
+    if (t >= p.kv.tokens) return;
+    const int lane = threadIdx.x & 63;
+    const int seq = find_seq(p.kv, t);
+    const Seq s = seq_of(p.kv, seq);
+    const int slot = s.len - s.n + (t - s.q0);
+    const bool ours = t >= s.q0 && t < s.q0 + s.n;
+    const int row = ours && slot >= 0 ? pool_row(p.kv, seq, slot) : -1;
+
+    const int lanes = 64 / units.all;  // heads that the wave takes at a time
+    const int sub = lane / units.all, unit = lane - sub * units.all;
+    const bool turned = unit < units.turned;
+    const int half = p.rot >> 1, u0 = min(unit * 8, half - 8);
+    // elements [ea, ea + 8) and [eb, eb + 8)
+    const int rest = p.rot + (unit - units.turned) * 16;
+    const int ea = !turned ? min(rest, p.dim - 8) : p.half_layout ? u0 : 2 * u0;
+    const int eb = !turned ? min(rest + 8, p.dim - 8) : p.half_layout ? half + u0 : 2 * u0 + 8;
+    const int few = p.dim - p.rot < 8 ? p.dim - p.rot : 0;  // elements behind the pairs, where no eight are
+    float c[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) c[i] = 1.f, sn[i] = 0.f;
+    if (turned) {
+        auto table = [&](int axis) {
+            const int pos = p.positions[t * x.token + axis * x.axis];
+            return (unsigned)pos < (unsigned)p.rope_rows ? p.rope + (int64_t)pos * p.rot + u0 : nullptr;
+        };
+        const uint64_t words = (uint64_t)x.of_pair[min(7, (u0 >> 4) + 1)] << 32 | x.of_pair[u0 >> 4];
+        const uint32_t mine = (uint32_t)(words >> 2 * (u0 & 15)) & 0xffff;
+        if (mine == (mine & 3) * 0x5555u) {  // one axis for all eight
+            const float* tab = table(mine & 3);
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                const F4 a = tab ? *(const F4*)(tab + i) : F4(__builtin_nanf("")), b = tab ? *(const F4*)(tab + half + i) : F4(__builtin_nanf(""));
+#pragma unroll
+                for (int j = 0; j < 4; j++) c[i + j] = a[j], sn[i + j] = b[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float* tab = table(mine >> 2 * i & 3);
+                c[i] = tab ? tab[i] : __builtin_nanf("");
+                sn[i] = tab ? tab[half + i] : __builtin_nanf("");
+            }
+        }
+    }
+    const int hk = p.kv.kv_heads;
+    const int total = p.heads + 2 * hk;
+    const int h0 = group * lanes * per + sub;
+    for (int i = 0; i < per && sub < lanes; i++) {
+        const int h = h0 + i * lanes;
+        if (h >= total) break;
+        const char* src;
+        char* dst;
+        bool rotate = turned;
+        if (h < p.heads) {
+            src = p.q + t * p.q_tok + h * p.q_head;
+            dst = p.q_out + t * p.o_tok + h * p.o_head;
+        } else {
+            if (row < 0) continue;
+            const int g = h - p.heads;
+            if (g < hk) {
+                src = p.kn + t * p.k_tok + g * p.k_head;
+                dst = const_cast<char*>(p.kv.k) + row_offset(row, p.kv.shift, p.kv.k_page, p.kv.k_row) + g * p.kv.k_head;
+            } else {
+                src = p.vn + t * p.v_tok + (g - hk) * p.v_head;
+                dst = const_cast<char*>(p.kv.v) + row_offset(row, p.kv.shift, p.kv.v_page, p.kv.v_row) + (g - hk) * p.kv.v_head;
+                rotate = false;
+            }
+        }
+        if (few && !turned) {
+            for (int j = p.rot; j < p.dim; j += 2) *(V2*)(dst + 2 * j) = *(const V2*)(src + 2 * j);
+            continue;
+        }
+        V8 a = *(const V8*)(src + 2 * ea), b = *(const V8*)(src + 2 * eb);
+        if (rotate) {
+            if (p.half_layout) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const float y = a[j], z = b[j];
+                    a[j] = (T)(y * c[j] - z * sn[j]);
+                    b[j] = (T)(z * c[j] + y * sn[j]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    V8& v = j < 4 ? a : b;
+                    const float y = v[2 * (j & 3)], z = v[2 * (j & 3) + 1];
+                    v[2 * (j & 3)] = (T)(y * c[j] - z * sn[j]);
+                    v[2 * (j & 3) + 1] = (T)(z * c[j] + y * sn[j]);
+                }
+            }
+        }
+        *(V8*)(dst + 2 * ea) = a;
+        *(V8*)(dst + 2 * eb) = b;
+    }
+    if (group == 0 && row >= 0) {
+        const int kept = x.kept ? x.kept[t] : p.positions[t * x.token];
+        for (int g = lane; g < hk; g += 64) {
+            const int64_t at = stat_index(p.kv, row, g);
+            if (p.kv.weight) p.kv.weight[at] = 0.f;
+            if (p.kv.position) p.kv.position[at] = kept;
+        }
+    }
+}
+
+// The same pair by pair, for rotated parts of fewer than eight pairs.
 template <class E>
 __global__ __launch_bounds__(64) void k_axes_any(AppendArgs p, AxesArgs x) {
     using T = typename E::T;
@@ -205,8 +326,7 @@ __global__ __launch_bounds__(64) void k_axes_any(AppendArgs p, AxesArgs x) {
         const int ea = half_pair ? u : 2 * u, eb = half_pair ? u + half : 2 * u + 1;
         const T a = src[ea], b = src[eb];
         if (rotate) {
-            const int axis = x.of_pair[u >> 4] >> 2 * (u & 15) & 3;
-            const int pos = p.positions[t * x.token + axis * x.axis];
+            const int pos = p.positions[t * x.token + axis_of(x, u) * x.axis];
             const bool known = (unsigned)pos < (unsigned)p.rope_rows;
             const float* tab = p.rope + (int64_t)(known ? pos : 0) * p.rot + u;
             const float c = known ? tab[0] : __builtin_nanf(""), sn = known ? tab[half] : __builtin_nanf("");
@@ -233,9 +353,9 @@ struct Wide {
     int64_t blocks;
 };
 
-Wide wide_grid(const AppendArgs& a) {
+Wide wide_grid(const AppendArgs& a, int units) {
     Wide w;
-    w.units = a.dim / 16;
+    w.units = units;
     const int lanes = 64 / w.units, steps = (a.heads + 2 * a.kv.kv_heads + lanes - 1) / lanes;
     // Heads that a lane walks over: all of a token's once 8,192 waves are there
     // without splitting a token, fewer for fewer tokens.
@@ -248,20 +368,38 @@ Wide wide_grid(const AppendArgs& a) {
 
 }  // namespace
 
-int64_t append_threads(const AppendArgs& a, bool wide) { return wide ? wide_grid(a).blocks * 256 : (int64_t)a.kv.tokens * 64; }
+int64_t append_threads(const AppendArgs& a, bool wide) { return wide ? wide_grid(a, a.dim / 16).blocks * 256 : (int64_t)a.kv.tokens * 64; }
 
 hipError_t launch_append(const AppendArgs& a, int32_t dtype, bool wide, hipStream_t s) {
     if (wide) {
-        const Wide w = wide_grid(a);
+        const Wide w = wide_grid(a, a.dim / 16);
         const dim3 grid((unsigned)w.blocks);
         return run(dtype == SVF_KV_BF16 ? k_append_wide<BF16> : k_append_wide<F16>, grid, 256, s, a, w.units, w.groups, w.per);
     }
     return run(dtype == SVF_KV_BF16 ? k_append_any<BF16> : k_append_any<F16>, dim3(a.kv.tokens), 64, s, a);
 }
 
-int64_t append_axes_threads(const AppendArgs& a) { return (int64_t)a.kv.tokens * 64; }
+namespace {
+
+bool axes_wide(const AppendArgs& a) { return a.rot >= 16; }
+
+Units axes_units(const AppendArgs& a) {
+    const int turned = (a.rot / 2 + 7) / 8;
+    return {turned, turned + (a.dim - a.rot + 15) / 16};
+}
+
+}  // namespace
+
+int64_t append_axes_threads(const AppendArgs& a) {
+    return axes_wide(a) ? wide_grid(a, axes_units(a).all).blocks * 256 : (int64_t)a.kv.tokens * 64;
+}
 
 hipError_t launch_append_axes(const AppendArgs& a, const AxesArgs& x, int32_t dtype, hipStream_t s) {
+    if (axes_wide(a)) {
+        const Units units = axes_units(a);
+        const Wide w = wide_grid(a, units.all);
+        return run(dtype == SVF_KV_BF16 ? k_axes_wide<BF16> : k_axes_wide<F16>, dim3((unsigned)w.blocks), 256, s, a, x, units, w.groups, w.per);
+    }
     return run(dtype == SVF_KV_BF16 ? k_axes_any<BF16> : k_axes_any<F16>, dim3(a.kv.tokens), 64, s, a, x);
 }
 
