@@ -194,10 +194,14 @@ int svf_kv_attend(const svf_kv_cache *cache, const svf_kv_batch *batch,
  * The same with first tokens that stay visible: row r also sees the slots j < first that its window
  * hides (0 <= j < kv_len, j <= r when causal).  Slots that no row sees are not read, and the pages that hold nothing
  * else may have been given back (no page there, a page number outside the pool).  Without a window, or where first is 0, it is
- * svf_kv_attend; the workspace is that of svf_kv_attend.
+ * svf_kv_attend.
+ *   workspace   (of svf_kv_attend_args) svf_kv_attend_first_workspace bytes
  */
 int svf_kv_attend_first(const svf_kv_cache *cache, const svf_kv_batch *batch,
                         const svf_kv_attend_args *args, int32_t first, void *hip_stream);
+
+int64_t svf_kv_attend_first_workspace(const svf_kv_cache *cache, const svf_kv_batch *batch,
+                                      const svf_kv_attend_args *args, int32_t first);
 
 /* Bytes of workspace that svf_kv_attend needs for these sizes (only sizes
  * and add_weight are read); negative: the code of an error. */

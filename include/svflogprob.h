@@ -49,7 +49,7 @@ enum { SVF_LOGPROB_MOST_TOP = 64, SVF_LOGPROB_MOST_VOCAB = 1 << 21 };
  *   logprob, entropy   float [rows];  rank int32 [rows]
  *   top_logprob, top_index   float and int32 [rows][top]
  *   workspace    svf_logprob_workspace bytes, 256-byte aligned, nothing kept in it
- * rows * top below 2^31, rows (some 2^24) such that a launch has fewer than 2^32 threads.
+ * rows * top below 2^31, rows (some 2^23) such that a launch has fewer than 2^32 threads.
  */
 typedef struct svf_logprob_args {
     const void *logits;

@@ -245,7 +245,7 @@ int attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_arg
     if (b->num_tokens == 0 || b->num_seqs == 0) return SVF_OK;
     if (!b->q_offsets || !a->q || !a->out || !a->lse) return fail(SVF_EINVAL, "q_offsets, q, out and lse must not be NULL");
     if (!aligned(a->out, 16)) return fail(SVF_EINVAL, "out must be aligned to 16 bytes");
-    const int64_t need = attend_workspace(sizes(c, b, a));
+    const int64_t need = attend_workspace(sizes(c, b, a, first));
     if (a->workspace_bytes < need || (need > 0 && !a->workspace) || !aligned(a->workspace, 256))
         return fail(SVF_EINVAL, "workspace must have %lld bytes, aligned to 256", (long long)need);
     const Rows q = {a->q, a->q_token_stride, a->q_head_stride}, out = {a->out, a->out_token_stride, a->out_head_stride};
@@ -293,6 +293,11 @@ int64_t svf_kv_attend_workspace(const svf_kv_cache* c, const svf_kv_batch* b, co
 
 int svf_kv_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, void* hip_stream) {
     return attend(c, b, a, 0, static_cast<hipStream_t>(hip_stream));
+}
+
+int64_t svf_kv_attend_first_workspace(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first) {
+    if (int rc = check_attend(c, b, a, first)) return rc;
+    return attend_workspace(sizes(c, b, a, first));
 }
 
 int svf_kv_attend_first(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first, void* hip_stream) {

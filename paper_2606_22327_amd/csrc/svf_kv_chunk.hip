@@ -551,7 +551,21 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // are added at the end, so nothing is added atomically.  2,048 tokens over 14,049 slots of 8 key heads (32 query heads, 218
 // GFLOP, 8.5e8 exponentials) take 326 us; nothing bounds it alone: the matrix units are busy for 0.27 of the cycles, other vector
 // instructions take 0.33, exponentials 0.2 more, and products and exponentials of a tile follow each other.
+//
+// With first tokens (FIRST) a window leaves few slot tiles, so the rows are split over as many parts as there is room
+// for, whose sums k_weight_join adds up in their order.
 constexpr int kWSlots = 256, kWRows = 64;
+constexpr int kMostWeightParts = 16;
+
+struct WeightPlan {
+    int32_t groups;  // workgroups to fill (FIRST)
+    int32_t items;   // slot tiles over all key heads that k_weight_chunk takes at most
+    float* part;     // [groups][kWSlots]
+};
+
+// The slot tiles that k_weight_chunk takes, and the parts of each, of ``total`` tiles of a key head.
+__device__ inline int weight_items(const WeightPlan& plan, int64_t total, int hk) { return (int)min((int64_t)plan.items, total * hk); }
+__device__ inline int weight_parts(const WeightPlan& plan, int items) { return max(1, min(kMostWeightParts, plan.groups / max(items, 1))); }
 
 template <bool FIRST>
 __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
@@ -560,7 +574,7 @@ __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
 }
 
 template <class E, int D, bool FIRST>
-__device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, int tile, int head) {
+__device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, int tile, int head, int part = 0, int parts = 1, float* to = nullptr) {
     using T = typename E::T;
     using V8 = typename E::V8;
     constexpr int KS = D / 16, CH = D / 8, PER = kWRows * CH / 256;
@@ -573,7 +587,15 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
     // rows that see one of the slots: tokens t0 .. t1 - 1
     const int t0 = p.causal ? max(0, j0 - r0) : 0;
     const int t1 = p.window > 0 && !(FIRST && j0 < p.first) ? (int)max((int64_t)0, min((int64_t)s.n, (int64_t)j1 - 1 + p.window - r0)) : s.n;
-    const int row0 = t0 * G, row1 = t1 * G;
+    int row0 = t0 * G, row1 = t1 * G;
+    if constexpr (FIRST) {
+        if (parts > 1) {
+            const int64_t tiles = max(0, (row1 - row0 + kWRows - 1) / kWRows);
+            const int end = (int)(row0 + tiles * (part + 1) / parts * kWRows);
+            row0 += (int)(tiles * part / parts) * kWRows;
+            row1 = min(row1, end);
+        }
+    }
 
     // this wave's slots and their keys
     const int base = j0 + wave * 64;
@@ -710,20 +732,58 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
             for (int d = 16; d; d >>= 1) x += __shfl_xor(x, d);
             // the lane that looked this slot up has its row
             const int off = (i >> 2) * 8 + h * 4 + (i & 3);
-            if (c == off && pool[st] >= 0) p.kv.weight[stat_index(p.kv, pool[st], head)] += x;
+            if (FIRST && to) {
+                if (c == off) to[wave * 64 + st * 32 + off] = x;
+            } else if (c == off && pool[st] >= 0) p.kv.weight[stat_index(p.kv, pool[st], head)] += x;
         }
 }
 
 // One tile a workgroup, of as many as the pool has slots for.
 template <class E, int D, bool FIRST>
-__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(AttendArgs p) {
+__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(AttendArgs p, WeightPlan plan) {
     __shared__ int64_t scan[4];
     const int hk = p.kv.kv_heads;
     int seq, tile;
+    if constexpr (FIRST) {
+        int item = 0, part = 0, parts = 1, items = 0;
+        const auto place = [&](int64_t total) {
+            items = weight_items(plan, total, hk);
+            parts = weight_parts(plan, items);
+            if (blockIdx.x >= (int64_t)items * parts) return total;
+            part = blockIdx.x / items;
+            item = blockIdx.x - part * items;
+            return (int64_t)(item / hk);
+        };
+        if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan, seq, tile)) return;
+        float* to = parts > 1 ? plan.part + (int64_t)blockIdx.x * kWSlots : nullptr;
+        weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, item % hk, part, parts, to);
+        return;
+    }
     if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan,
                    seq, tile))
         return;
     weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
+}
+
+// The parts' sums of a tile's slots, a slot a thread.
+__global__ __launch_bounds__(256) void k_weight_join(AttendArgs p, WeightPlan plan) {
+    __shared__ int64_t scan[4];
+    const int hk = p.kv.kv_heads, tid = threadIdx.x;
+    int seq, tile, items = 0, parts = 1;
+    const auto place = [&](int64_t total) {
+        items = weight_items(plan, total, hk);
+        parts = weight_parts(plan, items);
+        return parts > 1 && blockIdx.x < items ? (int64_t)(blockIdx.x / hk) : total;
+    };
+    if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles<true>(p, s); }, scan, seq, tile)) return;
+    const Seq s = seq_of(p.kv, seq);
+    const int j = slot_of<true>(line_of<true>(p, s, kWSlots), tile * kWSlots) + tid;
+    const int row = j < s.len ? pool_row(p.kv, seq, j) : -1;
+    if (row < 0) return;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < parts; i++) sum += plan.part[((int64_t)i * items + blockIdx.x) * kWSlots + tid];
+    p.kv.weight[stat_index(p.kv, row, blockIdx.x % hk)] += sum;
 }
 
 // Sequences with slots that have no page can have more tiles than that: those from ``first`` on, in a loop (a kernel of its own,
@@ -753,10 +813,16 @@ int32_t split_groups(const AttendSizes& z, int32_t few) {
     return least * z.kv_heads > groups / 2 ? 0 : groups;
 }
 
-int64_t chunk_workspace(const AttendSizes& z, int32_t few) {
+// Workgroups that the weights' parts fill: four times what the GPU holds, so that the last ones to come are short.  (2,048 tokens behind
+// 12,001 in a window of 4,096, 200 slot tiles: not split 346 us, filled once 191, twice 174, four times 168.)
+int32_t weight_groups(const AttendSizes& z) { return z.first > 0 && z.add_weight ? (z.dim <= 128 ? 2048 : 1024) : 0; }
+
+int64_t split_bytes(const AttendSizes& z, int32_t few) {
     const int32_t groups = split_groups(z, few);
     return groups ? 256 + groups / 2 * (int64_t)sizeof(Item) + (int64_t)groups * kRows * (z.dim + 4) * 4 : 0;
 }
+
+int64_t chunk_workspace(const AttendSizes& z, int32_t few) { return split_bytes(z, few) + (int64_t)weight_groups(z) * kWSlots * 4; }
 
 // Workgroups of the launches for these sizes.
 struct ChunkGrids {
@@ -802,8 +868,13 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         if (e != hipSuccess) return e;
     }
     if (g.tiles > 0) {
-        e = run(k_weight_chunk<E, D, FIRST>, dim3((unsigned)g.tiles), 256, s, a);
+        const WeightPlan w{weight_groups(z), (int32_t)g.tiles, (float*)(ws + split_bytes(z, a.few))};
+        e = run(k_weight_chunk<E, D, FIRST>, dim3((unsigned)(g.tiles > w.groups ? g.tiles : w.groups)), 256, s, a, w);
         if (e != hipSuccess) return e;
+        if (w.groups) {  // tiles in two parts or more are at most half as many as that
+            e = run(k_weight_join, dim3((unsigned)(g.tiles < w.groups / 2 ? g.tiles : w.groups / 2)), 256, s, a, w);
+            if (e != hipSuccess) return e;
+        }
     }
     return g.more > 0 ? run(k_weight_chunk_more<E, D, FIRST>, dim3((unsigned)g.more), 256, s, a, g.tiles / z.kv_heads) : hipSuccess;
 }

@@ -12,6 +12,7 @@ constexpr int kEntries = 4096;   // pieces of a row whose largest logits are kep
 constexpr int kListed = 512;    // of them that may hold one of the best
 constexpr int kCand = kEntries / 2;  // logits that may be one of the best, in the pieces' place
 constexpr int kMostParts = 64;
+constexpr int NT = 512;  // threads of a workgroup
 
 // What a part of a row found: its largest logit, the sum of 2^y and of y 2^y over its logits, y their distance from that in log2 terms, and how
 // many come before the token.
@@ -70,10 +71,16 @@ struct Logits {
     }
 };
 
-template <int NT, class V, class Op>
+template <class V, class Op>
+__device__ inline V over_wave(V x, Op op) {
+    for (int d = 32; d; d >>= 1) x = op(x, __shfl_xor(x, d));
+    return x;
+}
+
+template <class V, class Op>
 __device__ inline V over_group(V x, Op op) {
     __shared__ V part[NT / 64];
-    for (int d = 32; d; d >>= 1) x = op(x, __shfl_xor(x, d));
+    x = over_wave(x, op);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -156,8 +163,8 @@ __device__ inline Span<T> span_of(const Args& p, const Plan& plan, int row, int 
 // least ``top`` logits reach, so only pieces whose largest reaches it are read again, some more than ``top``, and of their logits those that reach it
 // are put in order by counting.  Where too many reach it (long runs of large logits), ``top`` rounds over the row find them one
 // by one; where too few are larger than -infinity, the lowest indices follow.
-template <class T, int NT, bool TOP>
-__global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan plan) {
+template <class T, bool TOP>
+__global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     using L = Logits<T>;
     constexpr int W = L::W, U = 4;
     constexpr float kSlack = 8.f;
@@ -170,7 +177,19 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x / plan.parts, part = blockIdx.x - row * plan.parts;
     const Span<T> s = span_of<T>(p, plan, row, part);
-    auto add = [](auto a, auto b) { return a + b; };
+    const uint4* at = (const uint4*)((uint64_t)s.x & ~(uint64_t)15);
+    // (the last vectors of a part by themselves: logits of -infinity in the place of those that are not there)
+    constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;
+    const int whole = (s.v1 - s.v0) / (U * NT);
+    int v = s.v0 + tid;
+    uint4 next[U];
+    auto load = [&](int v) {
+        if (s.v0 == s.v1) return;
+#pragma unroll
+        for (int u = 0; u < U; u++) next[u] = at[min(v + u * NT, s.v1 - 1)];
+    };
+    load(v);
+    __builtin_amdgcn_sched_barrier(0);  // on their way before the token's
     const int64_t token = p.token_wide ? ((const int64_t*)p.token)[row] : ((const int32_t*)p.token)[row];
     const bool known = token >= 0 && token < p.vocab;
     const float mine = known ? (float)s.x[token] : __builtin_nanf("");
@@ -180,7 +199,6 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
     float m = -INFINITY, b = 3e38f, sum = 0.f, sumy = 0.f;
     int before = 0;
     const float c = p.scale2;
-    const uint4* at = (const uint4*)((uint64_t)s.x & ~(uint64_t)15);
     auto work = [&](const uint4(&w)[U], int v, bool all) {
         float top[U];
         float most = -INFINITY;
@@ -223,33 +241,18 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
                 sumy = fmaf(e, fmaxf(y, -200.f), sumy);  // 0 times -infinity is 0
             }
     };
-    int v = s.v0 + tid;
-    // (the last vectors of a part by themselves: logits of -infinity in the place of those that are not there)
-    constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;
-    const int whole = (s.v1 - s.v0) / (U * NT);
-    uint4 next[U];
-    if (whole > 0) {
-#pragma unroll
-        for (int u = 0; u < U; u++) next[u] = at[v + u * NT];
-    }
     for (int it = 0; it < whole; it++, v += U * NT) {
         uint4 w[U];
 #pragma unroll
         for (int u = 0; u < U; u++) w[u] = next[u];
-        if (it + 1 < whole) {
-#pragma unroll
-            for (int u = 0; u < U; u++) next[u] = at[v + (U + u) * NT];
-        }
+        load(v + U * NT);
         work(w, v, true);
     }
-    if (__any(v < s.v1)) {
-        uint4 w[U];
+    if (whole * U * NT < s.v1 - s.v0) {
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            w[u] = make_uint4(kNone, kNone, kNone, kNone);
-            if (v + u * NT < s.v1) w[u] = at[v + u * NT];
-        }
-        work(w, v, false);
+        for (int u = 0; u < U; u++)
+            if (v + u * NT >= s.v1) next[u] = make_uint4(kNone, kNone, kNone, kNone);
+        work(next, v, false);
     }
     const int edges = s.edge_count();
     const uint64_t mine_key = known ? key_of(mine, (int)token) : ~0ull;
@@ -272,14 +275,35 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
     if (known && tid == 0 && vt >= s.v0 && vt < s.v1)  // equal logits before the token in its own vector
         for (int i = vt * W - s.off; i < (int)token; i++) before += (float)s.x[i] == mine;
 
+    // The row's scalars: the largest logit, then the sums relative to it.
+    auto add = [](auto a, auto b) { return a + b; };
+    __shared__ float group_m[NT / 64];
+    __shared__ Part group[NT / 64];
     Part x;
-    x.m = over_group<NT>(m, [](float a, float b) { return fmaxf(a, b); });
+    x.m = over_wave(m, [](float a, float b) { return fmaxf(a, b); });
+    if (lane == 0) group_m[wave] = x.m;
+    __syncthreads();
+    for (int i = 0; i < NT / 64; i++) x.m = fmaxf(x.m, group_m[i]);
     {
         const float d = fmaf(x.m, c, b), f = x.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-d), dc = fminf(d, 1000.f);
-        x.s = over_group<NT>(sum * f, add);
-        x.sy = over_group<NT>(f * fmaf(sum, -dc, sumy), add);
+        sumy = f * fmaf(sum, -dc, sumy);
+        sum *= f;
     }
-    x.before = over_group<NT>(before, add);
+#pragma unroll
+    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k), sumy += __shfl_xor(sumy, k), before += __shfl_xor(before, k);
+    if (lane == 0) group[wave] = Part{0.f, sum, sumy, before};
+    // a thread's best piece
+    const int shift = plan.group, entries = (s.v1 - s.v0 + (1 << shift) - 1) >> shift;
+    auto entry_key = [&](int e) { return largest[e] > -INFINITY ? key_of(largest[e], e) : 0; };
+    uint64_t best = 0;
+    if constexpr (TOP) {
+        for (int e = tid; e < entries; e += NT) best = max(best, entry_key(e));
+        bins[tid] = best;
+        if (tid == 0) sh_bound = 0, sh_listed = 0, sh_cand = 0;
+    }
+    __syncthreads();
+    x.s = x.sy = 0.f, x.before = 0;
+    for (int i = 0; i < NT / 64; i++) x.s += group[i].s, x.sy += group[i].sy, x.before += group[i].before;
     // Logits so large that a reference in log2 terms is rounded by more than 2^-4, or none in 32 bits: once more, each distance by itself.
     if (x.m != -INFINITY && !(fabsf(x.m * c) < 1048576.f) && x.m != INFINITY) {
         sum = sumy = 0.f;
@@ -288,13 +312,13 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
             sum += e;
             sumy = fmaf(e, fmaxf(y, -200.f), sumy);
         }
-        x.s = over_group<NT>(sum, add);
-        x.sy = over_group<NT>(sumy, add);
+        x.s = over_group(sum, add);
+        x.sy = over_group(sumy, add);
     }
     if (known && mine != mine) {  // a token that is no number comes behind all that are
         before = 0;
         for (int i = tid; i < s.count(); i += NT) before += key_of((float)s.x[s.nth(i)], s.nth(i)) > mine_key;
-        x.before = over_group<NT>(before, add);
+        x.before = over_group(before, add);
     }
     if (tid == 0) {
         if (plan.parts == 1)
@@ -310,13 +334,6 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
                 plan.keys[(int64_t)blockIdx.x * p.top + at] = key;
         };
         // the bound
-        const int shift = plan.group, entries = (s.v1 - s.v0 + (1 << shift) - 1) >> shift;
-        auto entry_key = [&](int e) { return largest[e] > -INFINITY ? key_of(largest[e], e) : 0; };
-        uint64_t best = 0;
-        for (int e = tid; e < entries; e += NT) best = max(best, entry_key(e));
-        bins[tid] = best;
-        if (tid == 0) sh_bound = 0, sh_listed = 0, sh_cand = 0;
-        __syncthreads();
         if (p.top <= 32) {
             if (wave == 0) {
 #pragma unroll
@@ -405,7 +422,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? 8 : 4) void k_score(Args p, Plan pl
                     const uint64_t key = key_of((float)s.x[s.nth(i)], s.nth(i));
                     if (key < last) best = max(best, key);
                 }
-                last = over_group<NT>(best, [](uint64_t a, uint64_t b) { return max(a, b); });
+                last = over_group(best, [](uint64_t a, uint64_t b) { return max(a, b); });
                 if (tid == 0) emit(k, last);
             }
         }
@@ -445,17 +462,16 @@ __global__ __launch_bounds__(256) void k_join(Args p, Plan plan) {
 }
 
 struct Layout {
-    int32_t parts, per, group, threads;
+    int32_t parts, per, group;
     int64_t keys, bytes;
 };
 
 Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     Layout y;
     const int64_t vectors = (int64_t)vocab / (dtype == SVF_LOGITS_F32 ? 4 : 8) + 1;
-    y.threads = rows >= 1024 ? 256 : 1024;
-    // as many parts as the GPU has room for and as many candidates as a join can order, none of fewer vectors than threads
-    int64_t parts = y.threads == 256 ? 1 : 512 / (rows < 1 ? 1 : rows);
-    if (parts > vectors / (4 * y.threads)) parts = vectors / (4 * y.threads);
+    // as many parts as the GPU has CUs for and as a join can order candidates of, none of fewer vectors than eight a thread
+    int64_t parts = 256 / (rows < 1 ? 1 : rows);
+    if (parts > vectors / (8 * NT)) parts = vectors / (8 * NT);
     if (top > 0 && parts > kCand / 4 / top) parts = kCand / 4 / top;
     // a part's pieces have to fit
     const int64_t least = (vectors + kEntries * 8 - 1 - 64) / (kEntries * 8 - 64);
@@ -474,11 +490,7 @@ template <class T>
 hipError_t launch_type(const Args& a, const Layout& y, hipStream_t s) {
     const Plan plan{y.parts, y.per, y.group, (Part*)a.ws, (uint64_t*)(a.ws + y.keys)};
     const dim3 grid((unsigned)(a.rows * y.parts));
-    hipError_t e;
-    if (y.threads == 256)
-        e = a.top ? svfk::run(k_score<T, 256, true>, grid, 256, s, a, plan) : svfk::run(k_score<T, 256, false>, grid, 256, s, a, plan);
-    else
-        e = a.top ? svfk::run(k_score<T, 1024, true>, grid, 1024, s, a, plan) : svfk::run(k_score<T, 1024, false>, grid, 1024, s, a, plan);
+    const hipError_t e = a.top ? svfk::run(k_score<T, true>, grid, NT, s, a, plan) : svfk::run(k_score<T, false>, grid, NT, s, a, plan);
     if (e != hipSuccess || y.parts == 1) return e;
     return svfk::run(k_join<T>, dim3(a.rows), 256, s, a, plan);
 }
@@ -489,7 +501,7 @@ int64_t workspace(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) { ret
 
 int64_t threads(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     const Layout y = layout(rows, vocab, top, dtype);
-    return (int64_t)rows * y.parts * y.threads;
+    return (int64_t)rows * y.parts * NT;
 }
 
 hipError_t launch(const Args& a, int32_t dtype, hipStream_t s) {

@@ -286,6 +286,7 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
         _need(False, "out must have the shape of q")
     ot, oh = _rows(out, "out", *kind)
     kv, seqs = _pack(cache, batch, tokens)
+    first = int(first)
     lse = q.new_empty((tokens, heads), dtype=torch.float32)
     scale = dim ** -0.5 if scale is None else float(scale)
     fixed = (qt, qh, ot, oh, scale, heads, bool(causal), int(window), bool(add_weight))
@@ -295,16 +296,19 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
         a = _ATTEND.pack(*at, 0, 0, *fixed)
     except struct.error as e:
         raise _no_fit(e, "window and heads") from None
-    need = lib.svf_kv_attend_workspace(kv, seqs, a)
+    if first:
+        _need(0 < first < 1 << 31, "first must be >= 0, a 32-bit integer")
+        need = lib.svf_kv_attend_first_workspace(kv, seqs, a, first)
+    else:
+        need = lib.svf_kv_attend_workspace(kv, seqs, a)
     ws = None
     if need:
         ws = _workspace(need, q)
         a = _ATTEND.pack(*at, ws.data_ptr(), need, *fixed)
-    if first == 0:
-        _call(lib.svf_kv_attend, kind[1], kv, seqs, a)
+    if first:
+        _call(lib.svf_kv_attend_first, kind[1], kv, seqs, a, first)
     else:
-        _need(0 < first < 1 << 31, "first must be >= 0, a 32-bit integer")
-        _call(lib.svf_kv_attend_first, kind[1], kv, seqs, a, int(first))
+        _call(lib.svf_kv_attend, kind[1], kv, seqs, a)
     return out, lse
 
 

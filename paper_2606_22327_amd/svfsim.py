@@ -40,7 +40,7 @@ EXPORTS = ("svf_create", "svf_reset", "svf_step", "svf_run", "svf_read", "svf_st
            "svf_last_error", "svf_abi_version", "svf_opt_burst", "svf_opt_burst_batch",
            "svf_run_noalloc", "svf_kv_append", "svf_kv_attend", "svf_kv_attend_workspace",
            "svf_kv_evict", "svf_kv_evict_workspace", "svf_kv_last_error",
-           "svf_kv_append_axes", "svf_kv_attend_first", "svf_logprob", "svf_logprob_workspace",
+           "svf_kv_append_axes", "svf_kv_attend_first", "svf_kv_attend_first_workspace", "svf_logprob", "svf_logprob_workspace",
            "svf_logprob_last_error")
 
 
@@ -137,8 +137,10 @@ def load(path: str = LIB_PATH):
     for name in ("svf_kv_attend_workspace", "svf_kv_evict_workspace"):
         getattr(lib, name).argtypes = [V, V, V]
         getattr(lib, name).restype = I64
+    lib.svf_kv_attend_first_workspace.argtypes = [V, V, V, I32]
     lib.svf_logprob_workspace.argtypes = [V]
-    lib.svf_logprob_workspace.restype = I64
+    for name in ("svf_kv_attend_first_workspace", "svf_logprob_workspace"):
+        getattr(lib, name).restype = I64
     _lib = lib
     return lib
 

@@ -104,7 +104,8 @@ def test_attend_first_refuses():
                      (dict(out=A + 8), "aligned"), (dict(lse=0), "NULL"), (dict(q=0), "NULL")):
         assert lib.svf_kv_attend_first(cache(), batch(), attend(**kw), 4, None) == -1
         assert text in C.last_error()
-    need = lib.svf_kv_attend_workspace(cache(), batch(), attend(add_weight=1, window=8))
+    need = lib.svf_kv_attend_first_workspace(cache(), batch(), attend(add_weight=1, window=8), 4)
+    assert lib.svf_kv_attend_first_workspace(cache(), batch(), attend(), -1) == -1 and "first" in C.last_error()
     assert lib.svf_kv_attend_first(cache(), batch(), attend(add_weight=1, window=8, workspace_bytes=need - 1), 4, None) == -1
     assert "workspace" in C.last_error()
     assert lib.svf_kv_attend_first(cache(), batch(num_tokens=0), attend(window=8), 4, None) == 0
