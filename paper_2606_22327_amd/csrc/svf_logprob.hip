@@ -1,4 +1,6 @@
 // svf_logprob.hip -- log probabilities of given tokens, entropies and the best alternatives of rows of logits.
+#include <type_traits>
+
 #include "svf_kv_device.h"
 #include "svf_logprob.h"
 
@@ -24,8 +26,8 @@ struct Part {
 // How a row is dealt out.
 struct Plan {
     int32_t parts;   // workgroups of a row
-    int32_t per;     // whole 16-byte vectors of a part, a multiple of 64
-    int32_t group;   // log2 of the vectors of a piece: 0, or 3 where there would be more than kEntries
+    int32_t per;     // whole 16-byte vectors of a part, a multiple of 32
+    int32_t group;   // log2 of the vectors of a piece: 0, 3 or 5, by the length of a part
     Part* part;      // [rows][parts] (parts > 1)
     uint64_t* keys;  // [rows][parts][top]
 };
@@ -69,12 +71,46 @@ struct Logits {
         for (int i = 2; i < W; i += 2) x = fmaxf(x, fmaxf(at(w, i), at(w, i + 1)));
         return x;
     }
+    // Of U vectors.  In bfloat16 a word as a 32-bit number is its upper logit with some bits behind it, or, if that is infinite, no number:
+    // +infinity may be missed, which the row's sum then shows.
+    template <int U>
+    static __device__ inline float largest(const uint4 (&w)[U]) {
+        float x = -INFINITY, upper = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if constexpr (__is_same(T, __bf16)) {
+                upper = fmaxf(fmaxf(upper, fmaxf(__uint_as_float(w[u].x), __uint_as_float(w[u].y))),
+                              fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
+                x = fmaxf(fmaxf(x, fmaxf(at(w[u], 0), at(w[u], 2))), fmaxf(at(w[u], 4), at(w[u], 6)));
+            } else {
+                x = fmaxf(x, largest(w[u]));
+            }
+        }
+        return fmaxf(x, __uint_as_float(__float_as_uint(upper) & 0xffff0000u));
+    }
 };
 
+// What another lane of the same sixteen has.
+template <int Ctrl, class V>
+__device__ inline V from_near(V x) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), Ctrl, 0xf, 0xf, true));
+}
+template <class V, class Op>
+__device__ inline V over_8(V x, Op op) {
+    x = op(x, from_near<0xb1>(x));         // quad_perm 1 0 3 2
+    x = op(x, from_near<0x4e>(x));         // quad_perm 2 3 0 1
+    return op(x, from_near<0x141>(x));     // the eight lanes the other way round
+}
 template <class V, class Op>
 __device__ inline V over_wave(V x, Op op) {
-    for (int d = 32; d; d >>= 1) x = op(x, __shfl_xor(x, d));
-    return x;
+    if constexpr (sizeof(V) == 4) {
+        x = over_8(x, op);
+        x = op(x, from_near<0x140>(x));    // the sixteen the other way round
+    } else {
+        for (int d = 1; d < 16; d <<= 1) x = op(x, __shfl_xor(x, d));
+    }
+    x = op(x, __shfl_xor(x, 16));
+    return op(x, __shfl_xor(x, 32));
 }
 
 template <class V, class Op>
@@ -87,17 +123,6 @@ __device__ inline V over_group(V x, Op op) {
     x = part[0];
     for (int i = 1; i < NT / 64; i++) x = op(x, part[i]);
     return x;
-}
-
-// The larger of eight lanes in each of them.
-__device__ inline float max_of_8(float x) {
-    auto with = [](float x, auto ctrl) {
-        const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true);
-        return fmaxf(x, __int_as_float(y));
-    };
-    x = with(x, std::integral_constant<int, 0xb1>{});   // quad_perm 1 0 3 2
-    x = with(x, std::integral_constant<int, 0x4e>{});   // quad_perm 2 3 0 1
-    return with(x, std::integral_constant<int, 0x141>{});  // the eight lanes the other way round
 }
 
 // The distance of a logit from the largest of all in log2 terms (by halves, so that it does not pass what 32 bits hold on the way).
@@ -158,8 +183,8 @@ __device__ inline Span<T> span_of(const Args& p, const Plan& plan, int row, int 
 // keeps sums of 2^y and y 2^y, y the distance from a reference of its own that follows the largest logit it has met where that has
 // grown by more than 2^8.  Logits that may come before the token are counted only where a vector has one: with likely tokens hardly anywhere.
 //
-// The best alternatives: the largest logit of every piece of the row (128 bytes, the vectors of eight lanes, or one
-// vector where the row is short) goes to LDS.  Pieces in 64 (or all threads') bins: the top-th largest of the bins' best is a bound that at
+// The best alternatives: the largest logit of every piece of the row (512 bytes, four vectors of eight lanes; 128 or 16 bytes
+// where the row is short) goes to LDS.  Pieces in 64 (or 128) bins: the top-th largest of the bins' best is a bound that at
 // least ``top`` logits reach, so only pieces whose largest reaches it are read again, some more than ``top``, and of their logits those that reach it
 // are put in order by counting.  Where too many reach it (long runs of large logits), ``top`` rounds over the row find them one
 // by one; where too few are larger than -infinity, the lowest indices follow.
@@ -170,7 +195,7 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     constexpr float kSlack = 8.f;
     __shared__ float largest[TOP ? kEntries : 1];
     __shared__ uint16_t listed[TOP ? kListed : 1];
-    __shared__ uint64_t bins[TOP ? NT : 1];
+    __shared__ int hits[NT / 64];
     __shared__ uint64_t sh_bound;
     __shared__ int sh_listed, sh_cand;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -181,12 +206,12 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     // (the last vectors of a part by themselves: logits of -infinity in the place of those that are not there)
     constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;
     const int whole = (s.v1 - s.v0) / (U * NT);
-    int v = s.v0 + tid;
+    int v = s.v0 + (tid >> 3) * (8 * U) + (tid & 7);  // eight lanes have U lines that follow each other
     uint4 next[U];
     auto load = [&](int v) {
         if (s.v0 == s.v1) return;
 #pragma unroll
-        for (int u = 0; u < U; u++) next[u] = at[min(v + u * NT, s.v1 - 1)];
+        for (int u = 0; u < U; u++) next[u] = at[min(v + u * 8, s.v1 - 1)];
     };
     load(v);
     __builtin_amdgcn_sched_barrier(0);  // on their way before the token's
@@ -197,23 +222,31 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     const int vt = known ? ((int)token + s.off) / W : 0, vb = min(vt, s.v1);  // its vector, and the last one before it
 
     float m = -INFINITY, b = 3e38f, sum = 0.f, sumy = 0.f;
-    int before = 0;
+    int before = 0;  // of the whole wave
+    bool masked = false;
     const float c = p.scale2;
+    // the same vector, whose logits are taken out of it again: kept from one use to the next they would need more registers than there are
+    auto again = [](uint4 w) {
+        asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w));
+        return w;
+    };
     auto work = [&](const uint4(&w)[U], int v, bool all) {
-        float top[U];
-        float most = -INFINITY;
+        const float most = L::largest(w);
+        if constexpr (TOP) {
+            const auto more = [](float a, float b) { return fmaxf(a, b); };
+            if (plan.group == 5) {
+                const float x = over_8(most, more);
+                if ((lane & 7) == 0 && (all || v < s.v1)) largest[(v - s.v0) >> 5] = x;
+            } else if (plan.group == 3) {
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            top[u] = L::largest(w[u]);
-            most = fmaxf(most, top[u]);
-            if constexpr (TOP) {
-                const int e = v - s.v0 + u * NT;
-                if (plan.group) {
-                    const float x = max_of_8(top[u]);
-                    if ((lane & 7) == 0 && (all || v + u * NT < s.v1)) largest[e >> 3] = x;
-                } else if (all || v + u * NT < s.v1) {
-                    largest[e] = top[u];
+                for (int u = 0; u < U; u++) {
+                    const float x = over_8(L::largest(again(w[u])), more);
+                    if ((lane & 7) == 0 && (all || v + u * 8 < s.v1)) largest[(v - s.v0 + u * 8) >> 3] = x;
                 }
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; u++)
+                    if (all || v + u * 8 < s.v1) largest[v - s.v0 + u * 8] = L::largest(again(w[u]));
             }
         }
         m = fmaxf(m, most);
@@ -227,19 +260,39 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
         if (__any(most >= mine)) {
 #pragma unroll
             for (int u = 0; u < U; u++) {
-                const float least = v + u * NT < vb ? mine : over;
+                const float least = v + u * 8 < vb ? mine : over;
 #pragma unroll
-                for (int i = 0; i < W; i++) before += L::at(w[u], i) >= least;
+                for (int i = 0; i < W; i++) before += __popcll(__ballot(L::at(w[u], i) >= least));
             }
         }
+        // 0 times -infinity is 0: from the first such logit of a wave on, distances are kept above what gives 0
+        const float had = sumy;
+        if (!masked) {
 #pragma unroll
-        for (int u = 0; u < U; u++)
+            for (int u = 0; u < U; u++) {
+                const uint4 x = __is_same(T, _Float16) ? again(w[u]) : w[u];
+#pragma unroll
+                for (int i = 0; i < W; i++) {
+                    const float y = fmaf(L::at(x, i), c, b), e = __builtin_amdgcn_exp2f(y);
+                    sum += e;
+                    sumy = fmaf(e, y, sumy);
+                }
+            }
+            if (!__any(sumy != sumy)) return;
+            sumy = had;
+        }
+        const float once = masked ? 1.f : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const uint4 x = again(w[u]);
 #pragma unroll
             for (int i = 0; i < W; i++) {
-                const float y = fmaf(L::at(w[u], i), c, b), e = __builtin_amdgcn_exp2f(y);
-                sum += e;
-                sumy = fmaf(e, fmaxf(y, -200.f), sumy);  // 0 times -infinity is 0
+                const float y = fmaf(L::at(x, i), c, b), e = __builtin_amdgcn_exp2f(y);
+                sum = fmaf(e, once, sum);
+                sumy = fmaf(e, fmaxf(y, -200.f), sumy);
             }
+        }
+        masked = true;
     };
     for (int it = 0; it < whole; it++, v += U * NT) {
         uint4 w[U];
@@ -251,11 +304,12 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     if (whole * U * NT < s.v1 - s.v0) {
 #pragma unroll
         for (int u = 0; u < U; u++)
-            if (v + u * NT >= s.v1) next[u] = make_uint4(kNone, kNone, kNone, kNone);
+            if (v + u * 8 >= s.v1) next[u] = make_uint4(kNone, kNone, kNone, kNone);
         work(next, v, false);
     }
     const int edges = s.edge_count();
     const uint64_t mine_key = known ? key_of(mine, (int)token) : ~0ull;
+    bool edge_before = false;
     if (tid < edges) {
         const int i = s.edge(tid);
         const float x = (float)s.x[i];
@@ -270,10 +324,12 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
         const float y = fmaf(x, c, b), e = __builtin_amdgcn_exp2f(y);
         sum += e;
         sumy = fmaf(e, fmaxf(y, -200.f), sumy);
-        before += mine == mine && key_of(x, i) > mine_key;
+        edge_before = mine == mine && key_of(x, i) > mine_key;
     }
+    int equal = 0;
     if (known && tid == 0 && vt >= s.v0 && vt < s.v1)  // equal logits before the token in its own vector
-        for (int i = vt * W - s.off; i < (int)token; i++) before += (float)s.x[i] == mine;
+        for (int i = vt * W - s.off; i < (int)token; i++) equal += (float)s.x[i] == mine;
+    before += __popcll(__ballot(edge_before)) + __builtin_amdgcn_readfirstlane(equal);
 
     // The row's scalars: the largest logit, then the sums relative to it.
     auto add = [](auto a, auto b) { return a + b; };
@@ -282,25 +338,56 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     Part x;
     x.m = over_wave(m, [](float a, float b) { return fmaxf(a, b); });
     if (lane == 0) group_m[wave] = x.m;
+    if (TOP && tid == 0) sh_listed = 0, sh_cand = 0;
     __syncthreads();
+    const int shift = plan.group, entries = (s.v1 - s.v0 + (1 << shift) - 1) >> shift;
+    if (TOP && wave == 0) {
+        // The bound, by the first wave while the others add up: the top-th largest of 64 bins' best pieces, or of 128.
+        const bool two = p.top > 32;
+        float most[2] = {-INFINITY, -INFINITY};
+        int at[2] = {0, 0};
+        auto take = [&](int e, int i) {
+            const float y = e < entries ? largest[e] : -INFINITY;
+            if (y > most[i]) most[i] = y, at[i] = e;
+        };
+        for (int e = lane; e < entries; e += 256) {
+            take(e, 0), take(e + 128, 0);
+            if (two)
+                take(e + 64, 1), take(e + 192, 1);
+            else
+                take(e + 64, 0), take(e + 192, 0);
+        }
+        uint64_t best[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) best[i] = most[i] > -INFINITY ? key_of(most[i], at[i]) : 0;
+        int larger[2] = {0, 0};
+        auto count = [&](uint64_t x, auto both) {
+#pragma unroll
+            for (int i = 0; i < 64; i++) {
+                const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 |
+                                   (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, i);
+                larger[0] += y > best[0];
+                if (both) larger[1] += y > best[1];
+            }
+        };
+        if (two) {
+            count(best[0], std::true_type());
+            count(best[1], std::true_type());
+        } else {
+            count(best[0], std::false_type());
+        }
+        if (lane == 0) sh_bound = 0;
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            if (larger[i] == p.top - 1 && best[i] != 0) sh_bound = best[i];
+    }
     for (int i = 0; i < NT / 64; i++) x.m = fmaxf(x.m, group_m[i]);
     {
         const float d = fmaf(x.m, c, b), f = x.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-d), dc = fminf(d, 1000.f);
-        sumy = f * fmaf(sum, -dc, sumy);
-        sum *= f;
+        sumy = over_wave(f * fmaf(sum, -dc, sumy), add);
+        sum = over_wave(sum * f, add);
     }
-#pragma unroll
-    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k), sumy += __shfl_xor(sumy, k), before += __shfl_xor(before, k);
     if (lane == 0) group[wave] = Part{0.f, sum, sumy, before};
-    // a thread's best piece
-    const int shift = plan.group, entries = (s.v1 - s.v0 + (1 << shift) - 1) >> shift;
-    auto entry_key = [&](int e) { return largest[e] > -INFINITY ? key_of(largest[e], e) : 0; };
-    uint64_t best = 0;
-    if constexpr (TOP) {
-        for (int e = tid; e < entries; e += NT) best = max(best, entry_key(e));
-        bins[tid] = best;
-        if (tid == 0) sh_bound = 0, sh_listed = 0, sh_cand = 0;
-    }
     __syncthreads();
     x.s = x.sy = 0.f, x.before = 0;
     for (int i = 0; i < NT / 64; i++) x.s += group[i].s, x.sy += group[i].sy, x.before += group[i].before;
@@ -315,7 +402,8 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
         x.s = over_group(sum, add);
         x.sy = over_group(sumy, add);
     }
-    if (known && mine != mine) {  // a token that is no number comes behind all that are
+    const bool bad = !(x.s * 0.f == 0.f);  // a logit that is no number, or +infinity
+    if (known && (mine != mine || bad)) {  // a token that is no number comes behind all that are
         before = 0;
         for (int i = tid; i < s.count(); i += NT) before += key_of((float)s.x[s.nth(i)], s.nth(i)) > mine_key;
         x.before = over_group(before, add);
@@ -333,31 +421,11 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
             else
                 plan.keys[(int64_t)blockIdx.x * p.top + at] = key;
         };
-        // the bound
-        if (p.top <= 32) {
-            if (wave == 0) {
-#pragma unroll
-                for (int i = 1; i < NT / 64; i++) best = max(best, bins[i * 64 + lane]);
-                int larger = 0;
-                const int lo = (int)(uint32_t)best, hi = (int)(best >> 32);
-#pragma unroll
-                for (int i = 0; i < 64; i++) {
-                    const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, i);
-                    larger += y > best;
-                }
-                if (larger == p.top - 1 && best != 0) sh_bound = best;
-            }
-        } else {
-            int larger = 0;
-#pragma unroll 8
-            for (int i = 0; i < NT; i++) larger += bins[i] > best;
-            if (larger == p.top - 1 && best != 0) sh_bound = best;
-        }
-        __syncthreads();
+        // the pieces that reach the bound
         const uint64_t bound = sh_bound;
+        const float bound_logit = bound ? logit_of((uint32_t)(bound >> 32)) : -INFINITY;
         for (int e = tid; e < entries; e += NT) {
-            const uint64_t key = entry_key(e);
-            if (key == 0 || key < bound) continue;
+            if (!(largest[e] >= bound_logit) || largest[e] == -INFINITY || key_of(largest[e], e) < bound) continue;
             const int to = atomicAdd(&sh_listed, 1);
             if (to < kListed) listed[to] = (uint16_t)e;
         }
@@ -365,16 +433,26 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
         // the logits that reach it, in the pieces' place
         uint64_t* cand = (uint64_t*)largest;
         const int pieces = min(sh_listed, kListed);
-        for (int i = tid; i < pieces << shift; i += NT) {
-            const int e = listed[i >> shift], v = s.v0 + (e << shift) + (i & ((1 << shift) - 1));
-            if (v >= s.v1) continue;
-            const uint4 w = at[v];
+        for (int i0 = tid; i0 < pieces << shift; i0 += 2 * NT) {
+            uint4 w[2];
+            int e[2], v[2];
 #pragma unroll
-            for (int j = 0; j < W; j++) {
-                const float y = L::at(w, j);
-                if (!(y > -INFINITY) || key_of(y, e) < bound) continue;
-                const int to = atomicAdd(&sh_cand, 1);
-                if (to < kCand) cand[to] = key_of(y, v * W - s.off + j);
+            for (int k = 0; k < 2; k++) {
+                const int i = i0 + k * NT;
+                e[k] = listed[min(i >> shift, pieces - 1)];
+                v[k] = i < pieces << shift ? s.v0 + (e[k] << shift) + (i & ((1 << shift) - 1)) : s.v1;
+                if (v[k] < s.v1) w[k] = at[v[k]];
+            }
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                if (v[k] >= s.v1 || !(L::largest(w[k]) >= bound_logit)) continue;
+#pragma unroll
+                for (int j = 0; j < W; j++) {
+                    const float y = L::at(w[k], j);
+                    if (!(y >= bound_logit) || y == -INFINITY || key_of(y, e[k]) < bound) continue;
+                    const int to = atomicAdd(&sh_cand, 1);
+                    if (to < kCand) cand[to] = key_of(y, v[k] * W - s.off + j);
+                }
             }
         }
         if (tid < edges) {
@@ -386,7 +464,7 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
         }
         __syncthreads();
         int n = sh_cand;
-        if (n <= kCand && sh_listed <= kListed) {
+        if (n <= kCand && sh_listed <= kListed && !bad) {
             // too few: the lowest indices of -infinity, then of NaN
             for (int kind = 0; kind < 2 && n < p.top; kind++)
                 for (int i0 = 0; i0 < s.count() && n < p.top; i0 += NT) {
@@ -395,12 +473,12 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
                     const bool hit = kind ? y != y : y == -INFINITY;
                     const uint64_t mask = __ballot(hit);
                     __syncthreads();
-                    if (lane == 0) bins[wave] = __popcll(mask);
+                    if (lane == 0) hits[wave] = __popcll(mask);
                     __syncthreads();
                     int to = n + __popcll(mask & ((1ull << lane) - 1));
                     for (int w = 0; w < NT / 64; w++) {
-                        if (w < wave) to += (int)bins[w];
-                        n += (int)bins[w];
+                        if (w < wave) to += hits[w];
+                        n += hits[w];
                     }
                     if (hit && to < kCand) cand[to] = key_of(y, j);
                 }
@@ -417,7 +495,7 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
         } else {
             uint64_t last = ~0ull;
             for (int k = 0; k < p.top; k++) {
-                best = 0;
+                uint64_t best = 0;
                 for (int i = tid; i < s.count() && last; i += NT) {
                     const uint64_t key = key_of((float)s.x[s.nth(i)], s.nth(i));
                     if (key < last) best = max(best, key);
@@ -474,13 +552,14 @@ Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     if (parts > vectors / (8 * NT)) parts = vectors / (8 * NT);
     if (top > 0 && parts > kCand / 4 / top) parts = kCand / 4 / top;
     // a part's pieces have to fit
-    const int64_t least = (vectors + kEntries * 8 - 1 - 64) / (kEntries * 8 - 64);
+    const int64_t least = (vectors + kEntries * 32 - 33) / (kEntries * 32 - 32);
     if (parts < least) parts = least;
     if (parts > kMostParts) parts = kMostParts;
     if (parts < 1) parts = 1;
     y.parts = (int32_t)parts;
-    y.per = (int32_t)(((vectors + parts - 1) / parts + 63) & ~int64_t(63));
-    y.group = y.per <= kEntries ? 0 : 3;
+    y.per = (int32_t)(((vectors + parts - 1) / parts + 31) & ~int64_t(31));
+    // some hundred pieces: few for the bound, many for 64 of them to be a small part
+    y.group = y.per <= 1024 ? 0 : y.per <= 8192 ? 3 : 5;
     y.keys = ((int64_t)rows * parts * (int64_t)sizeof(Part) + 255) & ~int64_t(255);
     y.bytes = parts == 1 ? 0 : y.keys + (int64_t)rows * parts * top * 8;
     return y;
