@@ -1,7 +1,8 @@
 """Replays a simulated schedule on one layer's paged key-value cache.
 
     python -m paper_2606_22327_amd.replay [--config 1] [--instance 0] [--requests N] [--policy svf]
-                                          [--keep SLOTS] [--heads 32] [--kv-heads 8] [--dim 128] [--page 16]
+                                          [--keep SLOTS | --window SLOTS [--first SLOTS]] [--grid H W]
+                                          [--vocab V [--top K]] [--heads 32] [--kv-heads 8] [--dim 128] [--page 16]
 
 The simulator plans with a budget of M cache slots and steps of one token for
 every running request.  Here each simulated step is carried out: the running
@@ -14,16 +15,20 @@ after a step never exceed M.
 
 ``--keep`` is the other way to live with little memory than evicting whole requests:
 each request is held to that many slots, those of the largest attention weight, the
-first 4 tokens and the newest quarter.
+first 4 tokens and the newest quarter.  ``--window`` is a third: a token sees so many slots up to its own and the request's
+``--first`` slots, and the pages that no token will see again go back.
 
-Queries, keys and values are random numbers in place of a model's projections.
+``--grid`` makes prompts of texts and images of H x W tokens, whose positions have three axes.  ``--vocab`` ends
+a step with the log probability of each request's token among so many, and the ``--top`` best.
+
+Queries, keys, values and logits are random numbers in place of a model's projections.
 """
 
 from __future__ import annotations
 
 import argparse
 import json
-from typing import Dict, Iterator, List, NamedTuple, Optional
+from typing import Dict, Iterator, List, NamedTuple, Optional, Tuple
 
 import numpy as np
 
@@ -57,8 +62,28 @@ def timeline(prompt, output, start) -> Iterator[Step]:
         running = [i for i in running if t - start[i] < output[i]]
 
 
+#: Tokens of text before each image of a prompt with a grid.
+TEXT = 32
+
+
+def grid_positions(token, prompt, grid: Tuple[int, int]) -> np.ndarray:
+    """Time, row and column of tokens (their numbers in requests of ``prompt`` tokens): in a prompt ``TEXT`` tokens of
+    text and an image of grid[0] x grid[1] tokens follow each other.  Text counts on every axis; in an image time
+    stands still, rows and columns count from there, and what follows goes on behind the larger of the two.  Answers are text."""
+    token, prompt = np.asarray(token, dtype=np.int64), np.asarray(prompt, dtype=np.int64)
+    h, w = grid
+    at = np.minimum(token, prompt)                       # an answer counts on from the prompt's end
+    turn, i = at // (TEXT + h * w), at % (TEXT + h * w)
+    start = turn * (TEXT + max(h, w)) + np.minimum(i, TEXT)
+    inside = np.maximum(i - TEXT, 0)
+    answer = token >= prompt
+    start = start + np.where(answer, token - prompt + np.where(i > TEXT, max(h, w), 0), 0)
+    inside = np.where(answer, 0, inside)
+    return np.stack((start, start + inside // w, start + inside % w), -1)
+
+
 class Pages:
-    """Page lists of the running requests out of one pool."""
+    """Page lists of the running requests out of one pool; -1 where a page was given back."""
 
     def __init__(self, num_pages: int, page: int):
         self.page = page
@@ -72,9 +97,19 @@ class Pages:
         while len(pages) < need:
             pages.append(self.free.pop())
         while len(pages) > need:
-            self.free.append(pages.pop())
+            last = pages.pop()
+            if last >= 0:
+                self.free.append(last)
         if not pages:
             del self.held[request]
+
+    def give_back(self, request: int, begin: int, end: int):
+        """The request holds none of the slots [begin, end) any more: pages that hold nothing else go back."""
+        pages = self.held[request]
+        for i in range(-(-begin // self.page), min(end // self.page, len(pages))):
+            if pages[i] >= 0:
+                self.free.append(pages[i])
+                pages[i] = -1
 
     def table(self, requests) -> np.ndarray:
         lists = [self.held[int(i)] for i in requests]
@@ -91,11 +126,15 @@ class Replay:
     a page more, which is what pages that are not full can cost."""
 
     def __init__(self, prompt, output, start, M: int, heads: int = 32, kv_heads: int = 8, dim: int = 128,
-                 page: int = 16, keep: Optional[int] = None, seed: int = 0):
+                 page: int = 16, keep: Optional[int] = None, seed: int = 0, window: int = 0, first: int = 0,
+                 grid: Optional[Tuple[int, int]] = None, vocab: int = 0, top: int = 0):
         import torch
-        from . import kvcache
+        from . import kvcache, logprobs
 
-        self.torch, self.C = torch, kvcache
+        if keep and window:
+            raise ValueError("a window counts slots, which eviction moves: keep or window, not both")
+        self.torch, self.C, self.L = torch, kvcache, logprobs
+        self.window, self.first, self.grid, self.vocab, self.top = window, first, grid, vocab, top
         self.steps = timeline(prompt, output, start)
         self.prompt, self.output = np.asarray(prompt, dtype=np.int64), np.asarray(output, dtype=np.int64)
         self.M, self.heads, self.kv_heads, self.dim, self.keep = int(M), heads, kv_heads, dim, keep
@@ -109,7 +148,10 @@ class Replay:
                                    torch.empty((*pool, dim), dtype=torch.bfloat16, **gpu),
                                    torch.zeros(pool, **gpu) if keep else None,
                                    torch.zeros(pool, dtype=torch.int32, **gpu) if keep else None)
-        self.rope = kvcache.rope_table(int((self.prompt + self.output).max(initial=0)) + 1, dim)
+        # an image of one row or column is the largest step of a position
+        far = int((self.prompt + self.output).max(initial=0)) + 1 + (max(grid) if grid else 0)
+        self.rope = kvcache.rope_table(far, dim)
+        self.axes = kvcache.pair_axes((dim // 2 - 2 * (dim // 6), dim // 6, dim // 6)) if grid else None
         self.random = torch.Generator(device="cuda").manual_seed(seed)
 
     def step(self):
@@ -130,9 +172,25 @@ class Replay:
         qkv = torch.randn((tokens, self.heads + 2 * self.kv_heads, self.dim), dtype=torch.bfloat16, device="cuda",
                           generator=self.random)
         q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)
-        q = C.append(q, k, v, gpu(position), self.rope, batch, self.cache)
-        out, lse = C.attend(q, batch, self.cache, add_weight=bool(self.keep))
-        read = int(length.sum())
+        if self.grid:
+            places = grid_positions(position, self.prompt[s.request][owner], self.grid)
+            q = C.append(q, k, v, gpu(places), self.rope, batch, self.cache, axes=self.axes, kept=gpu(position))
+        else:
+            q = C.append(q, k, v, gpu(position), self.rope, batch, self.cache)
+        if self.window:
+            out, lse = C.attend(q, batch, self.cache, window=self.window, first=self.first)
+        else:
+            out, lse = C.attend(q, batch, self.cache, add_weight=bool(self.keep))
+        read = length
+        if self.window:                     # what the oldest new token's window hides from all, but for the first tokens
+            hidden = np.maximum(length - s.new - self.window + 1, 0)
+            read = length - hidden + np.minimum(self.first, hidden)
+        score = None
+        if self.vocab:
+            requests = len(s.request)
+            logits = 3 * torch.randn((requests, self.vocab), dtype=torch.bfloat16, device="cuda", generator=self.random)
+            token = torch.randint(self.vocab, (requests,), device="cuda", generator=self.random)
+            score = self.L.score(logits, token, top=self.top)
         if self.keep:
             C.evict(batch, self.cache, self.keep, recent=self.keep // 4, first=min(4, self.keep // 2),
                     next_position=gpu(s.age + s.new))
@@ -141,8 +199,17 @@ class Replay:
         self.length[s.request] = np.where(done, 0, length)
         for i, n in zip(s.request, self.length[s.request]):
             self.pages.resize(int(i), int(n))
-        return {"time": s.time, "request": s.request, "batch": batch, "q": q, "out": out, "lse": lse,
-                "read": read, "tokens": tokens, "held": int(length.sum())}
+            if self.window and n:       # the next token's window begins at slot n + 1 - window
+                self.pages.give_back(int(i), self.first, int(n) + 1 - self.window)
+        held = length
+        if self.window:
+            hidden = np.maximum(length + 1 - self.window, 0)
+            held = length - hidden + np.minimum(self.first, hidden)
+        result = {"time": s.time, "request": s.request, "batch": batch, "q": q, "out": out, "lse": lse,
+                  "read": int(read.sum()), "tokens": tokens, "held": int(held.sum())}
+        if score is not None:
+            result.update(logits=logits, token=token, score=score)
+        return result
 
     def _start(self, s: Step) -> np.ndarray:
         age = s.age - self.prompt[s.request]                 # tokens generated before the step
@@ -162,6 +229,7 @@ def run(batch, policy: str = "svf", instance: int = 0, **kw) -> Dict[str, float]
         raise ValueError("only schedules that finish without evictions are replayed")
     r = Replay(one.prompt, one.output, got["start"], one.M, **kw)
     sums = {"steps": 0, "tokens": 0, "slots_read": 0, "most_slots": 0}
+    nats = torch.zeros((), dtype=torch.float64, device="cuda")
     a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     a.record()
     while True:
@@ -172,8 +240,12 @@ def run(batch, policy: str = "svf", instance: int = 0, **kw) -> Dict[str, float]
         sums["tokens"] += s["tokens"]
         sums["slots_read"] += s["read"]
         sums["most_slots"] = max(sums["most_slots"], s["held"])
+        if r.vocab:
+            nats -= s["score"].logprob.sum()
     b.record()
     torch.cuda.synchronize()
+    if r.vocab:
+        sums["nats"] = round(float(nats), 1)
     o, p = one.output.astype(np.int64), one.prompt.astype(np.int64)
     sums.update(requests=len(o), M=int(one.M), volume=int((p * o + (o * o + o) // 2).sum()),
                 us_per_step=round(a.elapsed_time(b) * 1e3 / max(sums["steps"], 1), 1))
@@ -189,6 +261,11 @@ def main(argv=None):
     ap.add_argument("--requests", type=int, default=None)
     ap.add_argument("--policy", default="svf", choices=("svf", "sjf", "fcfs"))
     ap.add_argument("--keep", type=int, default=None)
+    ap.add_argument("--window", type=int, default=0)
+    ap.add_argument("--first", type=int, default=4)
+    ap.add_argument("--grid", type=int, nargs=2, default=None, metavar=("H", "W"))
+    ap.add_argument("--vocab", type=int, default=0)
+    ap.add_argument("--top", type=int, default=0)
     ap.add_argument("--heads", type=int, default=32)
     ap.add_argument("--kv-heads", type=int, default=8)
     ap.add_argument("--dim", type=int, default=128)
@@ -196,7 +273,8 @@ def main(argv=None):
     a = ap.parse_args(argv)
     batch = workloads.config(a.config, instances=a.instance + 1, n=a.requests)
     print(json.dumps(run(batch, a.policy, a.instance, heads=a.heads, kv_heads=a.kv_heads, dim=a.dim, page=a.page,
-                         keep=a.keep)))
+                         keep=a.keep, window=a.window, first=a.first, grid=a.grid and tuple(a.grid), vocab=a.vocab,
+                         top=a.top)))
 
 
 if __name__ == "__main__":
