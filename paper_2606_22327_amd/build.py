@@ -4,7 +4,8 @@ The library holds every kernel of the simulator and the host runtime behind
 the C ABI of ``include/svfsim.h``, the paged cache's operators
 (``include/svfkv.h``), the scores of answers (``include/svflogprob.h``) and the host-side exact optimum of tiny burst instances
 (``include/svfopt.h``).  It is built in-tree so that the same file
-is loaded by the tests, the smoke check and the benchmark.
+is loaded by the tests, the smoke check and the benchmark.  ``_svfbinding.so`` beside it
+is the cache's binding to torch.
 """
 
 import os
@@ -61,9 +62,31 @@ def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
     _run(["hipcc", f"--offload-arch={ARCH}", "-shared", "-fPIC", *objects, "-pthread", "-o", tmp])
     os.replace(tmp, LIB)
+    build_binding()
     if verbose:
         print(LIB)
     return LIB
+
+
+# What looks at torch's tensors for the cache's calls, against the headers and libraries of the torch that is installed.
+BINDING = os.path.join(PKG, "_svfbinding.so")
+
+
+def build_binding() -> str:
+    import sysconfig
+
+    import torch
+
+    at = os.path.dirname(torch.__file__)
+    include = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_path("include")]
+    tmp = BINDING + ".tmp"
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          "-I", INCLUDE, *[x for i in include for x in ("-isystem", i)], os.path.join(CSRC, "svf_binding.cpp"), "-o", tmp,
+          "-L", PKG, "-l:libsvfsim.so", "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+          "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, BINDING)
+    return BINDING
 
 
 # The runtime's host code under the address and undefined-behaviour

@@ -305,6 +305,7 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (v + u * 8 >= s.v1) next[u] = make_uint4(kNone, kNone, kNone, kNone);
+        masked = masked || __any(v + (U - 1) * 8 >= s.v1);
         work(next, v, false);
     }
     const int edges = s.edge_count();

@@ -9,8 +9,8 @@ steps does to a layer's cache on the GPU:
 ``rope_table``   cosines and sines by position, for the rotation
 ``pair_axes``   which axis of a position each pair of a head turns by
 
-Argument marshalling only: every step runs in the HIP kernels of
-``libsvfsim.so``, on torch's current stream of the tensors' device.  All tensors are
+Argument marshalling only, in ``csrc/svf_binding.cpp`` for ordinary arguments and here for all others: every step runs in
+the HIP kernels of ``libsvfsim.so``, on torch's current stream of the tensors' device.  All tensors are
 on one GPU.  There are no backward passes: where gradients are recorded, tensors that
 require one are refused.  Arguments that can be checked on the host are, and raise
 ``svfsim.SvfError`` (``SVF_EINVAL``); what lengths, offsets and page numbers in
@@ -81,8 +81,8 @@ def _check(rc: int, error=last_error):
         raise svfsim.SvfError(rc, error())
 
 
-# A step is some microseconds on the GPU, so the checks are one expression each
-# where all is well; which of them failed is found out afterwards.
+# What follows is the long way, for whatever the binding has not taken: another device than the current one, tensors of
+# gradients, arguments to be refused.  The checks are one expression each where all is well; which of them failed is found out afterwards.
 
 def _pack(cache: Cache, batch: Batch, tokens: int) -> Tuple[bytes, bytes]:
     k, v, weight, position = cache
@@ -192,6 +192,23 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream"):      # the same handle withou
     _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)     # the current one
+_bound = None
+
+
+def _binding():
+    """The compiled binding (raises if it is not built)."""
+    global _bound
+    if _bound is None:
+        svfsim.load()       # torch's runtime, then the library, then what links both
+        try:
+            from . import _svfbinding
+        except ImportError as e:
+            raise RuntimeError(f"_svfbinding.so is not built ({e}); run __graft_entry__.build()") from None
+        _bound = _svfbinding
+    return _bound
+
+
 def _workspace(n: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     if n < 0:
         _check(int(n))
@@ -211,6 +228,12 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
     For positions with several axes ``axes`` names the axis of every pair (``pair_axes``); ``positions`` are then
     [tokens, axes], with any strides, and ``kept`` (int32 [tokens]) is what ``cache.position`` is set to in
     place of axis 0's position: the token's place in the text, which ``evict`` goes by."""
+    if q.is_cuda:
+        dev = _device()
+        r = (_bound or _binding()).append(q, k, v, positions, rope, batch, cache, LAYOUT.get(layout), q_out, axes, kept, dev,
+                                          _raw_stream(dev))
+        if r is not None:
+            return _check(r) if r.__class__ is int else r
     if (q.requires_grad or k.requires_grad or v.requires_grad or cache.k.requires_grad or cache.v.requires_grad
             or (rope is not None and rope.requires_grad) or (q_out is not None and q_out.requires_grad)):
         _gradient()
@@ -271,6 +294,11 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     given back (-1 in the page table).    ``add_weight`` adds every slot's softmax, summed
     over the tokens and the query heads that share its key head, to
     ``cache.weight``.  A token that sees no slot has out = 0, lse = -inf."""
+    if out is None and q.is_cuda:
+        dev = _device()
+        r = (_bound or _binding()).attend(q, batch, cache, causal, window, scale, add_weight, first, dev, _raw_stream(dev))
+        if r is not None:
+            return _check(r) if r.__class__ is int else r
     if (q.requires_grad or cache.k.requires_grad or cache.v.requires_grad
             or (add_weight and cache.weight is not None and cache.weight.requires_grad)
             or (out is not None and out.requires_grad)):

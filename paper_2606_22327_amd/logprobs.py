@@ -3,7 +3,7 @@ tokens, their ranks, entropies and the best alternatives, from logits.
 
 ``score``   one row of logits and one token for each request of a step, or for each token of a prompt
 
-Argument marshalling only: every step runs in the HIP kernels of ``libsvfsim.so``, on
+Argument marshalling only, in ``csrc/svf_binding.cpp`` for ordinary arguments and here for all others: every step runs in the HIP kernels of ``libsvfsim.so``, on
 torch's current stream of the tensors' device.  There is no backward pass: where gradients are recorded, logits that
 require one are refused.  What can be checked on the host raises ``svfsim.SvfError`` (``SVF_EINVAL``).
 """
@@ -15,7 +15,7 @@ from typing import NamedTuple
 
 import torch
 
-from . import svfsim
+from . import kvcache, svfsim
 from .kvcache import _call, _gradient, _need
 
 DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
@@ -49,6 +49,11 @@ def score(logits: torch.Tensor, token: torch.Tensor, top: int = 0, scale: float 
     indices; ``top_index`` are the first ``top`` (at most 64) of that order.  ``scale`` is the inverse temperature.
     A row with a NaN or +infinity has NaN for its logarithms and its entropy, one of -infinity alone
     -infinity and 0; a token outside the vocabulary has logprob NaN and rank -1."""
+    if logits.is_cuda:
+        dev = kvcache._device()
+        r = (kvcache._bound or kvcache._binding()).score(logits, token, top, float(scale), dev, kvcache._raw_stream(dev))
+        if r is not None:
+            return Scores._make(r) if r.__class__ is tuple else kvcache._check(r, last_error)
     if logits.requires_grad:
         _gradient()
     shape, dev = logits.shape, logits.get_device()

@@ -1,0 +1,97 @@
+"""The compiled binding and the long way in Python: the same results, the same refusals."""
+
+import pytest
+import torch
+
+from paper_2606_22327_amd import kvcache as C
+from paper_2606_22327_amd import logprobs as L
+from paper_2606_22327_amd import svfsim as S
+from test_kvcache import BF, HF, batch_of, make
+
+
+class Never:
+    """A binding that takes nothing."""
+
+    append = attend = score = staticmethod(lambda *a: None)
+
+
+@pytest.fixture
+def long_way(monkeypatch):
+    return lambda: monkeypatch.setattr(C, "_bound", Never)
+
+
+def test_it_takes_nothing_that_it_does_not_know():
+    b = C._binding()
+    x = torch.zeros((2, 2, 64))
+    cache, batch = C.Cache(x, x), C.Batch(None, x, x, 1)
+    for f, n in ((b.append, 13), (b.attend, 10), (b.score, 6)):
+        for k in range(n + 2):
+            assert f(*([None] * k)) is None and f(*([x] * k)) is None and f(*([0] * k)) is None
+    assert b.append(x, x, x, x, None, batch, cache, 0, None, None, None, 0, 0) is None          # host tensors
+    assert b.attend(x, batch, cache, True, 0, None, False, 0, 0, 0) is None
+    assert b.score(x[0], x[0], 1, 1.0, 0, 0) is None
+
+
+def same(a, b):
+    return all(torch.equal(torch.nan_to_num(x, 7.0), torch.nan_to_num(y, 7.0)) for x, y in zip(a, b))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new", [[1, 1, 1], [3, 40, 1]])
+def test_both_ways_are_alike(dtype, new, long_way):
+    s = make(1, [300, 50, 1], new, 8, 2, 128, 16, dtype, garbage=0.0, stats=True)
+    g = torch.Generator().manual_seed(1)
+    T = sum(new)
+    k, v = (torch.randn((T, 2, 128), generator=g).to(dtype).cuda() for _ in range(2))
+    pos = torch.randint(0, 99, (T, 3), generator=g).int().cuda()
+    rope, ax = C.rope_table(100, 128), C.pair_axes((16, 24, 24))
+    x, token = torch.randn((7, 3001), generator=g).to(dtype).cuda(), torch.arange(7).cuda()
+
+    def run():
+        c = C.Cache(*(s[n].cuda() for n in ("k", "v", "weight", "position")))
+        b, q = batch_of(s), s["q"].cuda()
+        out = [C.append(q, k, v, pos[:, 0].contiguous(), rope, b, c), C.append(q, k, v, pos, rope, b, c, axes=ax),
+               C.append(q, k, v, pos, rope, b, c, layout="interleaved", axes=ax, kept=pos[:, 2].contiguous()),
+               C.append(q.clone(), k, v, pos[:, 1].contiguous(), None, b, c, q_out=torch.empty_like(q))]
+        out += C.attend(q, b, c, add_weight=True)
+        out += C.attend(q, b, c, window=20, first=5, scale=0.1, add_weight=True)
+        out += C.attend(q, b, c, causal=False)
+        out += L.score(x, token, top=4, scale=0.5)
+        out += L.score(x, token.int())
+        return [*out, *c]
+
+    a = run()
+    long_way()
+    b = run()
+    assert same(a, b) and [(t.shape, t.dtype, t.stride()) for t in a] == [(t.shape, t.dtype, t.stride()) for t in b]
+
+
+@pytest.mark.gpu
+def test_what_the_short_way_leaves_is_done_or_refused():
+    s = make(2, [40, 9], [1, 1], 4, 2, 64, 16, BF, garbage=0.0, stats=True)
+    c = C.Cache(*(s[n].cuda() for n in ("k", "v", "weight", "position")))
+    b, q = batch_of(s), s["q"].cuda()
+    want = C.attend(q, b, c, window=7, scale=1.0)
+    import numpy as np
+    assert same(C.attend(q, b, c, causal=1, window=np.int64(7), scale=1), want)             # other kinds of numbers
+    out = torch.empty_like(q)
+    assert C.attend(q, b, c, window=7, scale=1.0, out=out)[0] is out and torch.equal(out, want[0])
+    grad = q.clone().requires_grad_()
+    for f in (lambda: C.attend(grad, b, c), lambda: C.append(grad, q[:, :2], q[:, :2], b.kv_len, None, b, c),
+              lambda: C.append(q, grad[:, :2], q[:, :2], b.kv_len, None, b, c)):
+        with pytest.raises(S.SvfError, match="backward"):
+            f()
+    with torch.no_grad():
+        assert same(C.attend(grad, b, c, window=7, scale=1.0), want)
+    for f, text in ((lambda: C.attend(q, b, c._replace(weight=None), add_weight=True), "weight"),
+                    (lambda: C.attend(q, b, c, scale=float("nan")), "scale"), (lambda: C.attend(q, b, c, window=-1), "window"),
+                    (lambda: C.attend(q[:, :3], b, c), "multiple of kv_heads"),
+                    (lambda: C.attend(q, b._replace(max_q=2 ** 31), c), "32-bit"),
+                    (lambda: C.attend(q.float(), b, c), "dtype"), (lambda: C.attend(q, b._replace(q_offsets=None), c), "q_offsets"),
+                    (lambda: C.append(q, q[:, :2], q[:, :2], b.kv_len, None, b, c, layout="other"), "layout"),
+                    (lambda: C.append(q, q[:, :2], q[:, :2], b.kv_len.long(), None, b, c), "positions"),
+                    (lambda: L.score(q[:, 0], b.kv_len, top=65), "top"), (lambda: L.score(q[:, 0], b.kv_len, scale=0.0), "scale"),
+                    (lambda: L.score(q[:, 0], b.kv_len[:1]), "token")):
+        with pytest.raises(S.SvfError, match=text):
+            f()
