@@ -610,41 +610,50 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
 #pragma unroll
         for (int x = 0; x < KS; x++) k[st][x] = load_global<V8>(at + x * 32 + h * 16);
     }
-    // The rows whose pieces this thread brings to LDS, as token and query head: a tile on is ``step_t`` tokens
-    // and ``step_g`` heads on.
-    int qt[PER], qg[PER];
+    // The rows whose pieces this thread brings to LDS, one statistic with them: where they lie, and which query head each is. A tile on is
+    // ``step_t`` tokens and ``step_g`` heads on, and with the last head one token more; nothing is divided in the loop.
+    const int step_t = kWRows / G, step_g = kWRows - step_t * G, x16 = tid % CH * 16;
+    const int64_t q_step = step_t * p.q_tok + step_g * p.q_head, q_wrap = p.q_tok - G * p.q_head;
+    auto query = [&](int row) {
+        const int t = row / G;
+        return (uint64_t)(p.q + (s.q0 + t) * p.q_tok + (head * G + row - t * G) * p.q_head + x16);
+    };
+    uint64_t qat[PER];
+    int qg[PER];
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         const int row = row0 + (i * 256 + tid) / CH;
-        qt[i] = row / G;
-        qg[i] = row - qt[i] * G;
+        qat[i] = query(row);
+        qg[i] = row % G;
     }
-    const int step_t = kWRows / G, step_g = kWRows - step_t * G;
+    const uint64_t q_last = row0 < row1 ? query(row1 - 1) : 0;
+    int64_t stat_at = (int64_t)(s.q0 + (row0 + (tid & 63)) / G) * p.heads + head * G + (row0 + (tid & 63)) % G;
+    int stat_g = (row0 + (tid & 63)) % G;
     V8 staged[PER];
     float staged_stat = 0.f;
     auto take = [&](int at) {  // rows at .. at + 63 into registers
 #pragma unroll
         for (int i = 0; i < PER; i++) {
-            const int piece = i * 256 + tid, x = piece % CH;
             // a row behind the last has the last one's query: its statistic takes it out
-            const int t = min(qt[i], t1 - 1);
-            const char* from = p.q + (s.q0 + t) * p.q_tok + (head * G + qg[i]) * p.q_head + x * 16;
+            const uint64_t from = at + (i * 256 + tid) / CH < row1 ? qat[i] : q_last;
             if (p.q_wide) {
-                staged[i] = load_global<V8>((uint64_t)from);
+                staged[i] = load_global<V8>(from);
             } else {
 #pragma unroll
-                for (int y = 0; y < 8; y++) staged[i][y] = load_global<T>((uint64_t)(from + y * 2));
+                for (int y = 0; y < 8; y++) staged[i][y] = load_global<T>(from + y * 2);
             }
-            qt[i] += step_t;
             qg[i] += step_g;
-            if (qg[i] >= G) qg[i] -= G, qt[i]++;
+            qat[i] += q_step;
+            if (qg[i] >= G) qg[i] -= G, qat[i] += q_wrap;
         }
         if (tid < kWRows) {
-            const int row = at + tid, t = row / G;
             // a row that saw nothing, or is none, adds exp2(-inf)
             float x = -INFINITY;
-            if (row < row1) x = p.lse[(int64_t)(s.q0 + t) * p.heads + head * G + row - t * G];
+            if (at + tid < row1) x = p.lse[stat_at];
             staged_stat = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
+            stat_g += step_g;
+            stat_at += (int64_t)step_t * p.heads + step_g;
+            if (stat_g >= G) stat_g -= G, stat_at += p.heads - G;
         }
     };
     auto put = [&](int buf) {
@@ -667,10 +676,14 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
     __builtin_amdgcn_s_waitcnt(0x0f70);  // the keys are there: no wait for them in the loop
     __syncthreads();
     int buf = 0;
+    // the tile's first row as token and query head, what its last is on from there, and the lane's two
+    int ta = row0 / G, ga = row0 - ta * G;
+    const int last_t = (kWRows - 1) / G, last_g = (kWRows - 1) % G, end_t = (row1 - 1) / G;
+    const int own_t[2] = {c / G, (c + 32) / G}, own_g[2] = {c % G, (c + 32) % G};
     for (int at = row0; at < row1; at += kWRows, buf ^= 1) {
         if (at + kWRows < row1) take(at + kWRows);
-        // tokens of the first and the last row
-        const int ta = at / G, tb = min(at + kWRows - 1, row1 - 1) / G;
+        // token of the last row
+        const int tb = min(ta + last_t + (ga + last_g >= G), end_t);
         const bool whole = (!p.causal || base + 63 <= r0 + ta) && (p.window == 0 || base > r0 + tb - p.window || (FIRST && base + 63 < p.first)) &&
                            base + 63 < j1;
         const bool none = (p.causal && base > r0 + tb) || (p.window > 0 && base + 63 <= r0 + ta - p.window && !(FIRST && base < p.first)) ||
@@ -705,7 +718,7 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
 #pragma unroll
                         for (int i = 0; i < 16; i++) sum[st][i] += exp2_fast(fmaf(sc[st][i], p.scale, -lse));
                 } else {
-                    const int r = r0 + (at + rt * 32 + c) / G;
+                    const int r = r0 + ta + own_t[rt] + (ga + own_g[rt] >= G);
                     uint64_t sees = bits_between(p.window > 0 ? r - p.window + 1 - base : 0, p.causal ? r - base : 63);
                     if constexpr (FIRST) sees |= bits_between(0, (p.causal ? min(r, p.first - 1) : p.first - 1) - base);
                     const uint64_t seen = sees >> (h * 4);
@@ -721,6 +734,8 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
                 }
             }
         }
+        ta += step_t, ga += step_g;
+        if (ga >= G) ga -= G, ta++;
         if (at + kWRows < row1) put(buf ^ 1);
         __syncthreads();
     }
