@@ -171,13 +171,17 @@ __global__ __launch_bounds__(64) void k_append_any(AppendArgs p) {
 // from is another for each axis; an axis whose position is outside the table makes NaN of its own pairs alone.
 __device__ inline int axis_of(const AxesArgs& x, int pair) { return x.of_pair[pair >> 4] >> 2 * (pair & 15) & 3; }
 
-// As in k_append_wide, for rotated parts of any size from 16 on and rows at any address: the pairs are taken eight at a time, the last eight
+// As in k_append_wide, for rotated parts of any size from 16 on and rows at any address: a lane has eight elements of the part's first half
+// and eight of its second (eight pairs, or twice four where pairs are neighbours), the last ones
 // again from the end, so that two lanes may turn the same pair (both have read it before either writes: they are lanes of one
-// wave), and a 16-byte access may lie across two lines.  The rest of a head is copied 16 elements at a time in the same way.
+// wave), and a 16-byte access may lie across two lines.  The rest of a head is copied in the same way.
+// PAST: where a load of the lanes of a head covers whole lines it goes past the caches.  20,376 tokens of images (489 MB) take 79 us so and
+// 96 through them, more than a copy reaches; where it does not (three quarters of a head turned, 32,001 tokens of a video, 801 MB) 180
+// and 167.
 struct Units {
     int turned, all;  // of a head: units of eight pairs, and with those that are copied
 };
-template <class E>
+template <class E, bool PAST>
 __global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Units units, int groups, int per) {
     using T = typename E::T;
     typedef T V8 __attribute__((ext_vector_type(8), aligned(2)));
@@ -196,11 +200,13 @@ __global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Uni
     const int lanes = 64 / units.all;  // heads that the wave takes at a time
     const int sub = lane / units.all, unit = lane - sub * units.all;
     const bool turned = unit < units.turned;
-    const int half = p.rot >> 1, u0 = min(unit * 8, half - 8);
-    // elements [ea, ea + 8) and [eb, eb + 8)
-    const int rest = p.rot + (unit - units.turned) * 16;
-    const int ea = !turned ? min(rest, p.dim - 8) : p.half_layout ? u0 : 2 * u0;
-    const int eb = !turned ? min(rest + 8, p.dim - 8) : p.half_layout ? half + u0 : 2 * u0 + 8;
+    // elements [ea, ea + 8) and [eb, eb + 8): of the two halves of the rotated part (neighbours are not torn apart), or of the rest
+    const int half = p.rot >> 1, cut = p.half_layout ? half : (half + 1) & ~1;
+    const int copied = unit - units.turned, rest_half = (units.all - units.turned) * 8;
+    const int ea = turned ? min(unit * 8, cut - 8) : min(p.rot + copied * 8, p.dim - 8);
+    const int eb = turned ? min(cut + unit * 8, p.rot - 8) : min(p.rot + rest_half + copied * 8, p.dim - 8);
+    // and their pairs: eight from pa on, or four from pa and four from pb
+    const int pa = p.half_layout ? ea : ea >> 1, pb = p.half_layout ? ea + 4 : eb >> 1;
     const int few = p.dim - p.rot < 8 ? p.dim - p.rot : 0;  // elements behind the pairs, where no eight are
     float c[8], sn[8];
 #pragma unroll
@@ -208,24 +214,25 @@ __global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Uni
     if (turned) {
         auto table = [&](int axis) {
             const int pos = p.positions[t * x.token + axis * x.axis];
-            return (unsigned)pos < (unsigned)p.rope_rows ? p.rope + (int64_t)pos * p.rot + u0 : nullptr;
+            return (unsigned)pos < (unsigned)p.rope_rows ? p.rope + (int64_t)pos * p.rot : nullptr;
         };
-        const uint64_t words = (uint64_t)x.of_pair[min(7, (u0 >> 4) + 1)] << 32 | x.of_pair[u0 >> 4];
-        const uint32_t mine = (uint32_t)(words >> 2 * (u0 & 15)) & 0xffff;
-        if (mine == (mine & 3) * 0x5555u) {  // one axis for all eight
-            const float* tab = table(mine & 3);
 #pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-                const F4 a = tab ? *(const F4*)(tab + i) : F4(__builtin_nanf("")), b = tab ? *(const F4*)(tab + half + i) : F4(__builtin_nanf(""));
+        for (int i = 0; i < 8; i += 4) {
+            const int p0 = i ? pb : pa;
+            const uint64_t words = (uint64_t)x.of_pair[min(7, (p0 >> 4) + 1)] << 32 | x.of_pair[p0 >> 4];
+            const uint32_t mine = (uint32_t)(words >> 2 * (p0 & 15)) & 0xff;
+            if (mine == (mine & 3) * 0x55u) {  // one axis for all four
+                const float* tab = table(mine & 3);
+                const F4 a = tab ? *(const F4*)(tab + p0) : F4(__builtin_nanf("")), b = tab ? *(const F4*)(tab + half + p0) : F4(__builtin_nanf(""));
 #pragma unroll
                 for (int j = 0; j < 4; j++) c[i + j] = a[j], sn[i + j] = b[j];
-            }
-        } else {
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float* tab = table(mine >> 2 * i & 3);
-                c[i] = tab ? tab[i] : __builtin_nanf("");
-                sn[i] = tab ? tab[half + i] : __builtin_nanf("");
+                for (int j = 0; j < 4; j++) {
+                    const float* tab = table(mine >> 2 * j & 3);
+                    c[i + j] = tab ? tab[p0 + j] : __builtin_nanf("");
+                    sn[i + j] = tab ? tab[half + p0 + j] : __builtin_nanf("");
+                }
             }
         }
     }
@@ -257,7 +264,12 @@ __global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Uni
             for (int j = p.rot; j < p.dim; j += 2) *(V2*)(dst + 2 * j) = *(const V2*)(src + 2 * j);
             continue;
         }
-        V8 a = *(const V8*)(src + 2 * ea), b = *(const V8*)(src + 2 * eb);
+        V8 a, b;
+        if constexpr (PAST) {
+            a = __builtin_nontemporal_load((const V8*)(src + 2 * ea)), b = __builtin_nontemporal_load((const V8*)(src + 2 * eb));
+        } else {
+            a = *(const V8*)(src + 2 * ea), b = *(const V8*)(src + 2 * eb);
+        }
         if (rotate) {
             if (p.half_layout) {
 #pragma unroll
@@ -384,7 +396,7 @@ namespace {
 bool axes_wide(const AppendArgs& a) { return a.rot >= 16; }
 
 Units axes_units(const AppendArgs& a) {
-    const int turned = (a.rot / 2 + 7) / 8;
+    const int half = a.rot / 2, turned = ((a.half_layout ? half : (half + 1) & ~1) + 7) / 8;
     return {turned, turned + (a.dim - a.rot + 15) / 16};
 }
 
@@ -398,7 +410,11 @@ hipError_t launch_append_axes(const AppendArgs& a, const AxesArgs& x, int32_t dt
     if (axes_wide(a)) {
         const Units units = axes_units(a);
         const Wide w = wide_grid(a, units.all);
-        return run(dtype == SVF_KV_BF16 ? k_axes_wide<BF16> : k_axes_wide<F16>, dim3((unsigned)w.blocks), 256, s, a, x, units, w.groups, w.per);
+        // a load of a half covers whole lines
+        const bool past = a.rot % 128 == 0;
+        auto kernel = dtype == SVF_KV_BF16 ? past ? k_axes_wide<BF16, true> : k_axes_wide<BF16, false>
+                                           : past ? k_axes_wide<F16, true> : k_axes_wide<F16, false>;
+        return run(kernel, dim3((unsigned)w.blocks), 256, s, a, x, units, w.groups, w.per);
     }
     return run(dtype == SVF_KV_BF16 ? k_axes_any<BF16> : k_axes_any<F16>, dim3(a.kv.tokens), 64, s, a, x);
 }
