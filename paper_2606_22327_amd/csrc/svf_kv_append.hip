@@ -175,7 +175,7 @@ __device__ inline int axis_of(const AxesArgs& x, int pair) { return x.of_pair[pa
 // and eight of its second (eight pairs, or twice four where pairs are neighbours), the last ones
 // again from the end, so that two lanes may turn the same pair (both have read it before either writes: they are lanes of one
 // wave), and a 16-byte access may lie across two lines.  The rest of a head is copied in the same way.
-// PAST: where a load of the lanes of a head covers whole lines it goes past the caches.  20,376 tokens of images (489 MB) take 79 us so and
+// PAST: where a load of the lanes of a head covers whole lines it goes past the caches.  19,432 tokens of prompts with images (489 MB) take 79 us so and
 // 96 through them, more than a copy reaches; where it does not (three quarters of a head turned, 32,001 tokens of a video, 801 MB) 180
 // and 167.
 struct Units {
