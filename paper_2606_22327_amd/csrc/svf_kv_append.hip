@@ -175,13 +175,12 @@ __device__ inline int axis_of(const AxesArgs& x, int pair) { return x.of_pair[pa
 // and eight of its second (eight pairs, or twice four where pairs are neighbours), the last ones
 // again from the end, so that two lanes may turn the same pair (both have read it before either writes: they are lanes of one
 // wave), and a 16-byte access may lie across two lines.  The rest of a head is copied in the same way.
-// PAST: where a load of the lanes of a head covers whole lines it goes past the caches.  19,432 tokens of prompts with images (489 MB) take 79 us so and
-// 96 through them, more than a copy reaches; where it does not (three quarters of a head turned, 32,001 tokens of a video, 801 MB) 180
-// and 167.
+// Bytes bound it: 19,432 tokens of prompts with images (489 MB) take 96 us and 32,001 of a video (three quarters of a head turned, 801 MB)
+// 167, what a copy reaches; 203 tokens 5.4.
 struct Units {
     int turned, all;  // of a head: units of eight pairs, and with those that are copied
 };
-template <class E, bool PAST>
+template <class E>
 __global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Units units, int groups, int per) {
     using T = typename E::T;
     typedef T V8 __attribute__((ext_vector_type(8), aligned(2)));
@@ -264,12 +263,7 @@ __global__ __launch_bounds__(256) void k_axes_wide(AppendArgs p, AxesArgs x, Uni
             for (int j = p.rot; j < p.dim; j += 2) *(V2*)(dst + 2 * j) = *(const V2*)(src + 2 * j);
             continue;
         }
-        V8 a, b;
-        if constexpr (PAST) {
-            a = __builtin_nontemporal_load((const V8*)(src + 2 * ea)), b = __builtin_nontemporal_load((const V8*)(src + 2 * eb));
-        } else {
-            a = *(const V8*)(src + 2 * ea), b = *(const V8*)(src + 2 * eb);
-        }
+        V8 a = *(const V8*)(src + 2 * ea), b = *(const V8*)(src + 2 * eb);
         if (rotate) {
             if (p.half_layout) {
 #pragma unroll
@@ -410,11 +404,7 @@ hipError_t launch_append_axes(const AppendArgs& a, const AxesArgs& x, int32_t dt
     if (axes_wide(a)) {
         const Units units = axes_units(a);
         const Wide w = wide_grid(a, units.all);
-        // a load of a half covers whole lines
-        const bool past = a.rot % 128 == 0;
-        auto kernel = dtype == SVF_KV_BF16 ? past ? k_axes_wide<BF16, true> : k_axes_wide<BF16, false>
-                                           : past ? k_axes_wide<F16, true> : k_axes_wide<F16, false>;
-        return run(kernel, dim3((unsigned)w.blocks), 256, s, a, x, units, w.groups, w.per);
+        return run(dtype == SVF_KV_BF16 ? k_axes_wide<BF16> : k_axes_wide<F16>, dim3((unsigned)w.blocks), 256, s, a, x, units, w.groups, w.per);
     }
     return run(dtype == SVF_KV_BF16 ? k_axes_any<BF16> : k_axes_any<F16>, dim3(a.kv.tokens), 64, s, a, x);
 }
