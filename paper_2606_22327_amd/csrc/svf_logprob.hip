@@ -125,7 +125,7 @@ __device__ inline V over_group(V x, Op op) {
     return x;
 }
 
-// Each line of a row is read once, by eight lanes: past the caches (4,001 rows of 128,000, 1,024 MB: 170 us, and 183 through them; 203
+// Each line of a row is read once, by eight lanes: past the caches (4,001 rows of 128,000, 1,024 MB: 174 us, and 183 through them; 203
 // rows 23.4 and 24.0; 517 rows of 50,001 in 32 bits, whose lines do not begin with a row, 28 both ways, and 30 before the grid began at a line).
 __device__ inline uint4 load_once(const uint4* at) {
     typedef uint32_t V4 __attribute__((ext_vector_type(4)));
@@ -391,7 +391,8 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     }
     for (int i = 0; i < NT / 64; i++) x.m = fmaxf(x.m, group_m[i]);
     {
-        const float d = fmaf(x.m, c, b), f = x.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-d), dc = fminf(d, 1000.f);
+        // (a part without a logit above -infinity has no distances)
+        const float d = x.m == -INFINITY ? 0.f : fmaf(x.m, c, b), f = __builtin_amdgcn_exp2f(-d), dc = fminf(d, 1000.f);
         sumy = over_wave(f * fmaf(sum, -dc, sumy), add);
         sum = over_wave(sum * f, add);
     }

@@ -292,3 +292,36 @@ def test_logits_that_require_a_gradient_are_refused():
         L.score(x, t)
     with torch.no_grad():
         assert L.score(x, t).rank.tolist() == [0, 0]
+
+
+# Few rows of many logits are split over workgroups, each of which may have its own kind of logits.
+
+@pytest.mark.parametrize("dtype,vocab", [(BF, 128000), (HF, 131071), (F32, 90001)])
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_parts_of_a_row(dtype, vocab, rows):
+    x, token, g = logits(13, rows, vocab, dtype)
+    lowest = torch.finfo(dtype).min
+    at = torch.arange(vocab)
+    for hidden in (at < vocab // 2, at >= vocab // 2, (at > 1000) & (at < vocab - 1000), at != 77777, at > 10):
+        check(x.masked_fill(hidden, -INF), token, top=20)
+        check(x.masked_fill(hidden, lowest), token, top=20)
+    for where in (0, 5000, vocab // 2, vocab - 1):
+        token = torch.full((rows,), where)
+        check(x, token, top=3)
+        for what in (NAN, INF, -INF):
+            y = x.clone()
+            y[0, where] = what
+            check(y, token, top=3)
+            check(y, (token + 1) % vocab, top=64)
+    check(torch.zeros_like(x), token, top=64)
+    steps = (at // (vocab // 7)).to(dtype).expand(rows, vocab).contiguous()
+    check(steps, token, top=64)
+    check(-steps, token, top=64)
+
+
+def test_the_widest_vocabulary():
+    vocab = 1 << 21
+    x, token, _ = logits(14, 2, vocab, BF)
+    token[0] = vocab - 1
+    check(x, token, top=64)
+    check(x.float(), token, top=64)
