@@ -133,8 +133,11 @@ int launched(hipError_t e) {
 }
 
 AttendSizes sizes(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first = 0) {
+    // With first tokens: those, and the windows of max_q rows; else all.
+    const int64_t cap = (int64_t)b->table_width * c->page_size, seen = (int64_t)first + a->window + b->max_q + 512;
+    const int64_t places = first > 0 && a->window > 0 && seen < cap ? seen : cap;
     return {c->num_pages,  c->page_size, c->kv_heads,    a->heads, c->head_dim, c->dtype,
-            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0, first};
+            b->num_tokens, b->num_seqs,  b->table_width, b->max_q, a->add_weight != 0, first, places};
 }
 
 int check_attend(const svf_kv_cache* c, const svf_kv_batch* b, const svf_kv_attend_args* a, int32_t first = 0) {

@@ -59,6 +59,7 @@ struct AttendArgs {
 // The sizes that an attention call's workspace and launches go by.
 struct AttendSizes {
     int32_t num_pages, page_size, kv_heads, heads, dim, dtype, tokens, seqs, width, max_q, add_weight, first;
+    int64_t places;  // slots of a sequence that its rows see at most, with what rounding to pieces of up to 256 adds
 };
 
 struct EvictArgs {

@@ -852,7 +852,7 @@ ChunkGrids grids(const AttendSizes& z, int32_t few) {
     g.blocks = (rows / kRows + seqs) * z.kv_heads;
     if (g.blocks < split_groups(z, few)) g.blocks = split_groups(z, few);
     // slot tiles at most, and where every slot has a page: each page is in the batch once
-    const int64_t cap = (int64_t)z.width * z.page_size, all = seqs * ((cap + kWSlots - 1) / kWSlots);
+    const int64_t all = seqs * ((z.places + kWSlots - 1) / kWSlots);
     // (with first tokens a sequence has one more that is not full)
     const int64_t pool = (int64_t)z.num_pages * z.page_size / kWSlots + seqs * (z.first > 0 ? 2 : 1);
     g.tiles = z.add_weight ? (all < pool ? all : pool) : 0;

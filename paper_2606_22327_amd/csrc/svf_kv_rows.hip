@@ -665,7 +665,7 @@ struct Layout {
 
 Layout layout(const AttendSizes& z) {
     Layout y;
-    const int64_t cap = (int64_t)z.width * z.page_size;
+    const int64_t cap = z.places;
     const int64_t most = (int64_t)z.seqs * z.kv_heads * ((cap + kUnit - 1) / kUnit > 0 ? (cap + kUnit - 1) / kUnit : 1);
     y.rows = few_rows(z);
     // What the GPU holds at a time, but eight units each where that still is one for every CU: the fewer parts a row has,
