@@ -553,7 +553,8 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // instructions take 0.33, exponentials 0.2 more, and products and exponentials of a tile follow each other.
 //
 // With first tokens (FIRST) a window leaves few slot tiles, so the rows are split over as many parts as there is room
-// for, whose sums k_weight_join adds up in their order.
+// for, whose sums k_weight_join adds up in their order: 145 us for 138 GFLOP's worth of pairs, of which 1 us a tile of 64 rows, the
+// rest the parts' beginnings and ends.
 constexpr int kWSlots = 256, kWRows = 64;
 constexpr int kMostWeightParts = 16;
 
@@ -571,6 +572,14 @@ template <bool FIRST>
 __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
     if (s.n <= 0 || s.n > p.kv.max_q || !ours(p, s)) return 0;
     return (line_of<FIRST>(p, s, kWSlots).places + kWSlots - 1) / kWSlots;
+}
+
+// The sum over sixteen lanes in each of them, without a way through LDS.
+__device__ inline float add_16(float x) {
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, true));   // quad_perm 1 0 3 2
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, true));   // quad_perm 2 3 0 1
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));  // eight lanes the other way round
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xf, 0xf, true));  // sixteen
 }
 
 template <class E, int D, bool FIRST>
@@ -744,7 +753,12 @@ __device__ inline void weigh_slots(const AttendArgs& p, const Seq& s, int seq, i
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             float x = sum[st][i];
-            for (int d = 16; d; d >>= 1) x += __shfl_xor(x, d);
+            if constexpr (FIRST) {
+                x = add_16(x);
+                x += __shfl_xor(x, 16);
+            } else {
+                for (int d = 16; d; d >>= 1) x += __shfl_xor(x, d);
+            }
             // the lane that looked this slot up has its row
             const int off = (i >> 2) * 8 + h * 4 + (i & 3);
             if (FIRST && to) {
@@ -829,7 +843,8 @@ int32_t split_groups(const AttendSizes& z, int32_t few) {
 }
 
 // Workgroups that the weights' parts fill: four times what the GPU holds, so that the last ones to come are short.  (2,048 tokens behind
-// 12,001 in a window of 4,096, 200 slot tiles: not split 346 us, filled once 191, twice 174, four times 168.)
+// 12,001 in a window of 4,096, 200 slot tiles, the whole call: not split some 530 us, filled once 359, twice 342, three times 334, four
+// times 332.)
 int32_t weight_groups(const AttendSizes& z) { return z.first > 0 && z.add_weight ? (z.dim <= 128 ? 2048 : 1024) : 0; }
 
 int64_t split_bytes(const AttendSizes& z, int32_t few) {
