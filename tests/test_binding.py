@@ -95,3 +95,37 @@ def test_what_the_short_way_leaves_is_done_or_refused():
                     (lambda: L.score(q[:, 0], b.kv_len[:1]), "token")):
         with pytest.raises(S.SvfError, match=text):
             f()
+
+
+@pytest.mark.gpu
+def test_two_threads_on_streams_of_their_own():
+    import threading
+    s = make(3, [700, 90], [1, 40], 8, 2, 128, 16, BF, garbage=0.0, stats=True)
+    b, q, k, v = batch_of(s), s["q"].cuda(), s["k"].cuda(), s["v"].cuda()
+    x = torch.randn((41, 70000), generator=torch.Generator().manual_seed(4)).to(BF).cuda()
+    token = torch.arange(41).cuda()
+
+    def both():
+        c = C.Cache(k, v, s["weight"].cuda())
+        return [*C.attend(q, b, c, window=100, first=9, add_weight=True), c.weight, *L.score(x, token, top=7)]
+
+    want, got, wrong = both(), {}, []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got[i] = both()
+                with pytest.raises(S.SvfError, match=("window" if i else "top")):       # each thread its own error
+                    C.attend(q, b, C.Cache(k, v), window=-1) if i else L.score(x, token, top=99)
+                torch.cuda.current_stream().synchronize()
+        except BaseException as e:  # noqa: BLE001
+            wrong.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and all(same(want, got[i]) for i in range(2)), wrong

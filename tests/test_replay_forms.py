@@ -101,6 +101,27 @@ def test_a_window_over_everything_reads_what_no_window_does():
 
 
 @pytest.mark.gpu
+def test_images_shrunk_by_weight_keep_the_order_of_the_text():
+    b, got = schedule(1, 14)
+    r = R.Replay(b.prompt, b.output, got["start"], b.M, heads=4, kv_heads=2, dim=64, keep=24, grid=(4, 4))
+    steps = 0
+    while True:
+        s = r.step()
+        if s is None:
+            break
+        steps += 1
+        # what the cache keeps of a request that it has shrunk: the first 4 tokens, and the newest of the text
+        batch, pos = s["batch"], r.cache.position.cpu()
+        for i, (n, request) in enumerate(zip(batch.kv_len.tolist(), s["request"])):
+            if n > 24 and int(request) in r.pages.held:
+                pages = r.pages.held[int(request)]
+                kept = [int(pos[pages[j // 16], 0, j % 16]) for j in range(24)]
+                newest = int(r.prompt[request]) + int(s["time"] - got["start"][request])
+                assert len(set(kept)) == 24 and set(range(4)) <= set(kept) and set(range(newest - 5, newest + 1)) <= set(kept)
+    assert steps > 0
+
+
+@pytest.mark.gpu
 def test_replay_of_a_workload_with_a_window_and_scores():
     sums = R.run(W.config(2, instances=1, n=30), heads=8, kv_heads=2, dim=64, window=64, first=4, grid=(8, 8), vocab=5000, top=2)
     whole = R.run(W.config(2, instances=1, n=30), heads=8, kv_heads=2, dim=64)
