@@ -10,11 +10,12 @@ namespace svfp {
 namespace {
 
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr int kEntries = 4096;   // pieces of a row whose largest logits are kept in LDS
-constexpr int kListed = 512;    // of them that may hold one of the best
-constexpr int kCand = kEntries / 2;  // logits that may be one of the best, in the pieces' place
-constexpr int kMostParts = 64;
-constexpr int NT = 512;  // threads of a workgroup
+constexpr int kListed = 512;  // pieces of a row that may hold one of the best
+constexpr int kMostParts = 64, kJoined = 2048;  // parts of a row, and best of all of them
+constexpr int kMost = 512;  // threads of a workgroup
+
+// Pieces of a row whose largest logits a workgroup keeps in LDS. (Logits that may be one of the best, in the pieces' place, are half as many.)
+constexpr int entries_of(int threads) { return threads == kMost ? 4096 : 1024; }
 
 // What a part of a row found: its largest logit, the sum of 2^y and of y 2^y over its logits, y their distance from that in log2 terms, and how
 // many come before the token.
@@ -113,7 +114,7 @@ __device__ inline V over_wave(V x, Op op) {
     return op(x, __shfl_xor(x, 32));
 }
 
-template <class V, class Op>
+template <int NT, class V, class Op>
 __device__ inline V over_group(V x, Op op) {
     __shared__ V part[NT / 64];
     x = over_wave(x, op);
@@ -195,11 +196,12 @@ __device__ inline Span<T> span_of(const Args& p, const Plan& plan, int row, int 
 // least ``top`` logits reach, so only pieces whose largest reaches it are read again, some more than ``top``, and of their logits those that reach it
 // are put in order by counting.  Where too many reach it (long runs of large logits), ``top`` rounds over the row find them one
 // by one; where too few are larger than -infinity, the lowest indices follow.
-template <class T, bool TOP>
+template <class T, bool TOP, int NT>
 __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
     using L = Logits<T>;
-    constexpr int W = L::W, U = 4;
+    constexpr int W = L::W, U = 4, kEntries = entries_of(NT), kCand = kEntries / 2;
     constexpr float kSlack = 8.f;
+    static_assert(9 * W - 2 <= NT, "a thread an edge");
     __shared__ float largest[TOP ? kEntries : 1];
     __shared__ uint16_t listed[TOP ? kListed : 1];
     __shared__ int hits[NT / 64];
@@ -408,14 +410,14 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
             sum += e;
             sumy = fmaf(e, fmaxf(y, -200.f), sumy);
         }
-        x.s = over_group(sum, add);
-        x.sy = over_group(sumy, add);
+        x.s = over_group<NT>(sum, add);
+        x.sy = over_group<NT>(sumy, add);
     }
     const bool bad = !(x.s * 0.f == 0.f);  // a logit that is no number, or +infinity
     if (known && (mine != mine || bad)) {  // a token that is no number comes behind all that are
         before = 0;
         for (int i = tid; i < s.count(); i += NT) before += key_of((float)s.x[s.nth(i)], s.nth(i)) > mine_key;
-        x.before = over_group(before, add);
+        x.before = over_group<NT>(before, add);
     }
     if (tid == 0) {
         if (plan.parts == 1)
@@ -509,7 +511,7 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
                     const uint64_t key = key_of((float)s.x[s.nth(i)], s.nth(i));
                     if (key < last) best = max(best, key);
                 }
-                last = over_group(best, [](uint64_t a, uint64_t b) { return max(a, b); });
+                last = over_group<NT>(best, [](uint64_t a, uint64_t b) { return max(a, b); });
                 if (tid == 0) emit(k, last);
             }
         }
@@ -519,7 +521,7 @@ __global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
 // The parts of a row: its scalars, and of the parts' best the best.
 template <class T>
 __global__ __launch_bounds__(256) void k_join(Args p, Plan plan) {
-    __shared__ uint64_t cand[kCand];
+    __shared__ uint64_t cand[kJoined];
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int64_t token = p.token_wide ? ((const int64_t*)p.token)[row] : ((const int32_t*)p.token)[row];
     const bool known = token >= 0 && token < p.vocab;
@@ -549,19 +551,23 @@ __global__ __launch_bounds__(256) void k_join(Args p, Plan plan) {
 }
 
 struct Layout {
-    int32_t parts, per, group;
+    int32_t parts, per, group, threads;
     int64_t keys, bytes;
 };
 
 Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     Layout y;
     const int64_t vectors = (int64_t)vocab / (dtype == SVF_LOGITS_F32 ? 4 : 8) + 1;
+    // Two waves a row where many rows are short, so that what follows a row's last logit is done for more rows at a time (bf16, best 20: 4,000
+    // rows of 2,644 26.7 us, 65.8 with eight waves; 1,548 of 8,000 19.5 and 28.4; 600 of 1,229 11.4 and 13.5), and not where rows are few
+    // (256 of 8,000 12.7, 10.6 with eight) or long (600 of 16,000 18.4 and 15.9).  With one wave 4,000 of 2,644 24.6, but 600 14.3 and 11.9.
+    y.threads = rows > 512 && vectors <= 1024 ? 128 : kMost;
     // as many parts as the GPU has CUs for and as a join can order candidates of, none of fewer vectors than eight a thread
     int64_t parts = 256 / (rows < 1 ? 1 : rows);
-    if (parts > vectors / (8 * NT)) parts = vectors / (8 * NT);
-    if (top > 0 && parts > kCand / 4 / top) parts = kCand / 4 / top;
+    if (parts > vectors / (8 * kMost)) parts = vectors / (8 * kMost);
+    if (top > 0 && parts > kJoined / 4 / top) parts = kJoined / 4 / top;
     // a part's pieces have to fit
-    const int64_t least = (vectors + kEntries * 32 - 33) / (kEntries * 32 - 32);
+    const int64_t most = (int64_t)entries_of(kMost) * 32, least = (vectors + most - 33) / (most - 32);
     if (parts < least) parts = least;
     if (parts > kMostParts) parts = kMostParts;
     if (parts < 1) parts = 1;
@@ -574,11 +580,15 @@ Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     return y;
 }
 
+template <class T, int NT>
+hipError_t launch_score(const Args& a, const Plan& plan, hipStream_t s) {
+    return svfk::run(a.top ? k_score<T, true, NT> : k_score<T, false, NT>, dim3((unsigned)(a.rows * plan.parts)), NT, s, a, plan);
+}
+
 template <class T>
 hipError_t launch_type(const Args& a, const Layout& y, hipStream_t s) {
     const Plan plan{y.parts, y.per, y.group, (Part*)a.ws, (uint64_t*)(a.ws + y.keys)};
-    const dim3 grid((unsigned)(a.rows * y.parts));
-    const hipError_t e = svfk::run(a.top ? k_score<T, true> : k_score<T, false>, grid, NT, s, a, plan);
+    const hipError_t e = y.threads == 128 ? launch_score<T, 128>(a, plan, s) : launch_score<T, kMost>(a, plan, s);
     if (e != hipSuccess || y.parts == 1) return e;
     return svfk::run(k_join<T>, dim3(a.rows), 256, s, a, plan);
 }
@@ -589,7 +599,7 @@ int64_t workspace(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) { ret
 
 int64_t threads(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     const Layout y = layout(rows, vocab, top, dtype);
-    return (int64_t)rows * y.parts * NT;
+    return (int64_t)rows * y.parts * y.threads;
 }
 
 hipError_t launch(const Args& a, int32_t dtype, hipStream_t s) {

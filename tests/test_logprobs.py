@@ -325,3 +325,49 @@ def test_the_widest_vocabulary():
     token[0] = vocab - 1
     check(x, token, top=64)
     check(x.float(), token, top=64)
+
+
+# Many short rows have two waves each.
+
+def short(rows, vocab, dtype):
+    """A kind of row after the other: (logits, tokens)."""
+    x, token, g = logits(15, rows, vocab, dtype)
+    lowest, at = torch.finfo(dtype).min, torch.arange(vocab)
+    kinds = [lambda y: y, lambda y: y.masked_fill(torch.rand(y.shape, generator=g) < 0.9, -INF),
+             lambda y: y.masked_fill(torch.rand(y.shape, generator=g) < 0.9, lowest), lambda y: torch.full_like(y, -INF),
+             lambda y: torch.full_like(y, lowest), lambda y: y * 0, lambda y: y.masked_fill(at == 11, NAN),
+             lambda y: y.masked_fill(at == vocab - 1, INF), lambda y: y.masked_fill(at == 0, 60.0),
+             lambda y: (at // 70).to(dtype).expand(y.shape), lambda y: (-at // 70).to(dtype).expand(y.shape),
+             lambda y: torch.where(at % 200 == 100, -INF, NAN).to(dtype).expand(y.shape),
+             lambda y: y.masked_fill(at >= 65, -INF), lambda y: y.masked_fill(at < vocab - 3, -INF)]
+    for k, kind in enumerate(kinds):
+        x[k::len(kinds)] = kind(x[k::len(kinds)])
+    token[::9] = 0
+    token[1::9] = vocab - 1
+    token[2::9] = -1
+    return x, token
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
+@pytest.mark.parametrize("vocab", [1, 8, 65, 71, 1025, 2644, 4091, 4092, 8183, 8184])
+def test_many_short_rows(dtype, vocab):
+    x, token = short(513, vocab, dtype)
+    check(x, token, top=min(vocab, 64))
+    check(x, token, top=min(vocab, 3), scale=0.7)
+    check(x, token)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
+@pytest.mark.parametrize("shift", [1, 4, 7])
+def test_many_short_rows_at_any_address(dtype, shift):
+    rows, vocab, stride = 600, 1231, 1234
+    x, token = short(rows, vocab, dtype)
+    wide = torch.full((rows * stride + 8,), INF, dtype=dtype)          # between the rows: never read
+    wide[shift:shift + rows * stride].view(rows, stride)[:, :vocab].copy_(x)
+    check(x, token, top=33, dev=wide.cuda()[shift:shift + rows * stride].view(rows, stride)[:, :vocab])
+
+
+def test_many_short_rows_of_huge_logits():
+    x, token, _ = logits(16, 520, 900, F32)
+    for y in (x * 1e30, x * 1e38, x + 3e7, x * 1e-30):
+        check(y, token, top=7)
