@@ -12,10 +12,10 @@ namespace {
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kListed = 512;  // pieces of a row that may hold one of the best
 constexpr int kMostParts = 64, kJoined = 2048;  // parts of a row, and best of all of them
-constexpr int kMost = 512;  // threads of a workgroup
+constexpr int kUsual = 512;  // threads of a workgroup
 
 // Pieces of a row whose largest logits a workgroup keeps in LDS. (Logits that may be one of the best, in the pieces' place, are half as many.)
-constexpr int entries_of(int threads) { return threads == kMost ? 4096 : 1024; }
+constexpr int entries_of(int threads) { return threads < kUsual ? 1024 : 4096; }
 
 // What a part of a row found: its largest logit, the sum of 2^y and of y 2^y over its logits, y their distance from that in log2 terms, and how
 // many come before the token.
@@ -197,7 +197,7 @@ __device__ inline Span<T> span_of(const Args& p, const Plan& plan, int row, int 
 // are put in order by counting.  Where too many reach it (long runs of large logits), ``top`` rounds over the row find them one
 // by one; where too few are larger than -infinity, the lowest indices follow.
 template <class T, bool TOP, int NT>
-__global__ __launch_bounds__(NT, 6) void k_score(Args p, Plan plan) {
+__global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan plan) {
     using L = Logits<T>;
     constexpr int W = L::W, U = 4, kEntries = entries_of(NT), kCand = kEntries / 2;
     constexpr float kSlack = 8.f;
@@ -561,16 +561,20 @@ Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     // Two waves a row where many rows are short, so that what follows a row's last logit is done for more rows at a time (bf16, best 20: 4,000
     // rows of 2,644 26.7 us, 65.8 with eight waves; 1,548 of 8,000 19.5 and 28.4; 600 of 1,229 11.4 and 13.5), and not where rows are few
     // (256 of 8,000 12.7, 10.6 with eight) or long (600 of 16,000 18.4 and 15.9).  With one wave 4,000 of 2,644 24.6, but 600 14.3 and 11.9.
-    y.threads = rows > 512 && vectors <= 1024 ? 128 : kMost;
+    y.threads = rows > 512 && vectors <= 1024 ? 128 : kUsual;
     // as many parts as the GPU has CUs for and as a join can order candidates of, none of fewer vectors than eight a thread
     int64_t parts = 256 / (rows < 1 ? 1 : rows);
-    if (parts > vectors / (8 * kMost)) parts = vectors / (8 * kMost);
+    if (parts > vectors / (8 * kUsual)) parts = vectors / (8 * kUsual);
     if (top > 0 && parts > kJoined / 4 / top) parts = kJoined / 4 / top;
     // a part's pieces have to fit
-    const int64_t most = (int64_t)entries_of(kMost) * 32, least = (vectors + most - 33) / (most - 32);
+    const int64_t most = (int64_t)entries_of(kUsual) * 32, least = (vectors + most - 33) / (most - 32);
     if (parts < least) parts = least;
     if (parts > kMostParts) parts = kMostParts;
     if (parts < 1) parts = 1;
+    // Sixteen waves where a CU has but one row and that is long, for twice the loads on their way (bf16: 203 rows of 128,000, 20 best, 22.3 us
+    // and 23.8 with eight, 64 best 26.9 and 30.1, 150 of 151,000 25.3 and 27.7; but 203 of 64,000 18.4 and 18.1, 400 of 128,000 37.5 and 31.8,
+    // and one in parts 17.8 and 17.4).
+    if (parts == 1 && rows <= 256 && vectors > 12288) y.threads = 1024;
     y.parts = (int32_t)parts;
     y.per = (int32_t)(((vectors + parts - 1) / parts + 31) & ~int64_t(31));
     // some hundred pieces: few for the bound, many for 64 of them to be a small part
@@ -588,7 +592,9 @@ hipError_t launch_score(const Args& a, const Plan& plan, hipStream_t s) {
 template <class T>
 hipError_t launch_type(const Args& a, const Layout& y, hipStream_t s) {
     const Plan plan{y.parts, y.per, y.group, (Part*)a.ws, (uint64_t*)(a.ws + y.keys)};
-    const hipError_t e = y.threads == 128 ? launch_score<T, 128>(a, plan, s) : launch_score<T, kMost>(a, plan, s);
+    const hipError_t e = y.threads == 128    ? launch_score<T, 128>(a, plan, s)
+                         : y.threads == 1024 ? launch_score<T, 1024>(a, plan, s)
+                                             : launch_score<T, kUsual>(a, plan, s);
     if (e != hipSuccess || y.parts == 1) return e;
     return svfk::run(k_join<T>, dim3(a.rows), 256, s, a, plan);
 }

@@ -327,7 +327,7 @@ def test_the_widest_vocabulary():
     check(x.float(), token, top=64)
 
 
-# Many short rows have two waves each.
+# Many short rows have two waves each, a long row to a CU has sixteen.
 
 def short(rows, vocab, dtype):
     """A kind of row after the other: (logits, tokens)."""
@@ -371,3 +371,20 @@ def test_many_short_rows_of_huge_logits():
     x, token, _ = logits(16, 520, 900, F32)
     for y in (x * 1e30, x * 1e38, x + 3e7, x * 1e-30):
         check(y, token, top=7)
+
+
+@pytest.mark.parametrize("dtype,vocab", [(BF, 98312), (HF, 131001), (F32, 50001)])
+@pytest.mark.parametrize("rows", [129, 256])
+def test_a_long_row_to_a_workgroup(dtype, vocab, rows):
+    x, token = short(rows, vocab, dtype)
+    check(x, token, top=64)
+    check(x, token, top=3)
+    check(x, token)
+
+
+def test_long_rows_at_any_address():
+    rows, vocab, stride, shift = 131, 99001, 99003, 3
+    x, token = short(rows, vocab, BF)
+    wide = torch.full((rows * stride + 8,), INF, dtype=BF)             # between the rows: never read
+    wide[shift:shift + rows * stride].view(rows, stride)[:, :vocab].copy_(x)
+    check(x, token, top=33, dev=wide.cuda()[shift:shift + rows * stride].view(rows, stride)[:, :vocab])
