@@ -45,6 +45,15 @@ bool number(PyObject* x, int64_t* to) {
     return over == 0;
 }
 
+// Runs a call while other threads may have Python's lock: a launch waits where the GPU's queue is full.
+template <class F>
+int unlocked(F f) {
+    PyThreadState* thread = PyEval_SaveThread();
+    const int rc = f();
+    PyEval_RestoreThread(thread);
+    return rc;
+}
+
 template <class P>
 P* at_of(const at::Tensor& t) {
     return static_cast<P*>(t.data_ptr());
@@ -162,8 +171,10 @@ PyObject* append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.v_token_stride = v->stride(0), a.v_head_stride = v->stride(1);
     a.out_token_stride = out.stride(0), a.out_head_stride = out.stride(1);
     a.heads = (int32_t)heads, a.layout = (int32_t)layout;
-    const int rc = axes ? svf_kv_append_axes(&call.cache, &call.batch, &a, &with, now.stream)
-                        : svf_kv_append(&call.cache, &call.batch, &a, now.stream);
+    const int rc = unlocked([&] {
+        return axes ? svf_kv_append_axes(&call.cache, &call.batch, &a, &with, now.stream)
+                    : svf_kv_append(&call.cache, &call.batch, &a, now.stream);
+    });
     if (rc != SVF_OK) return PyLong_FromLong(rc);
     if (x[8] != Py_None) {
         Py_INCREF(x[8]);
@@ -206,8 +217,10 @@ PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
         ws = at::empty({need}, q->options().dtype(at::kByte));
         a.workspace = ws.data_ptr(), a.workspace_bytes = need;
     }
-    const int rc = first ? svf_kv_attend_first(&call.cache, &call.batch, &a, (int32_t)first, now.stream)
-                         : svf_kv_attend(&call.cache, &call.batch, &a, now.stream);
+    const int rc = unlocked([&] {
+        return first ? svf_kv_attend_first(&call.cache, &call.batch, &a, (int32_t)first, now.stream)
+                     : svf_kv_attend(&call.cache, &call.batch, &a, now.stream);
+    });
     if (rc != SVF_OK) return PyLong_FromLong(rc);
     PyObject *o = THPVariable_Wrap(std::move(out)), *l = o ? THPVariable_Wrap(std::move(lse)) : nullptr;
     PyObject* both = l ? PyTuple_Pack(2, o, l) : nullptr;
@@ -251,7 +264,7 @@ PyObject* score(PyObject*, PyObject* const* x, Py_ssize_t n) {
         ws = at::empty({need}, logits->options().dtype(at::kByte));
         a.workspace = ws.data_ptr(), a.workspace_bytes = need;
     }
-    const int rc = svf_logprob(&a, now.stream);
+    const int rc = unlocked([&] { return svf_logprob(&a, now.stream); });
     if (rc != SVF_OK) return PyLong_FromLong(rc);
     PyObject* all = PyTuple_New(5);
     for (int i = 0; all && i < 5; i++) {
