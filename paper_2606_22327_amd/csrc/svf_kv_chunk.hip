@@ -109,11 +109,14 @@ __device__ inline int swizzle(int row) {
 // calls and 549 under the profiler: 950 to 1,110 TFLOP/s of products carried out, where a large one of the library reaches 1,350.
 // Counters of the prompts: the matrix units are busy for 0.48 of the cycles, other vector instructions take 0.36 at four cycles
 // each, and exponentials, at sixteen, 0.12 more; two waves a SIMD do not fill the waits between.
+// With first tokens a window leaves few tiles a row, and beginnings and ends weigh more: 64 dimensions then run in three waves a SIMD (six
+// prompts of 700 to 4,096 tokens, 16 heads, window 512 + 128: 105 us, and 113 in two; 128 + 4: 62 and 72). Without a window two are
+// as fast or faster (the prompts 187 us, 190 in three; 4,096 tokens in float16 93 and 98).
 // WIDE: pages of 16 slots or more, so that the sixteen slots that a wave fetches lie in one page: their address is the same for
 // the whole wave but for an offset that stays the same all along (a tile costs a wave 8 loads and some scalar
 // instructions, and 100 vector instructions otherwise).
 template <class E, int D, bool WIDE, bool FIRST>
-__global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_attend_chunk(AttendArgs p, ChunkPlan plan) {
+__global__ __launch_bounds__(256, (FIRST && D <= 64 ? 3 : D <= 128 ? 2 : 1)) void k_attend_chunk(AttendArgs p, ChunkPlan plan) {
     using T = typename E::T;
     using V8 = typename E::V8;
     typedef short s16x4 __attribute__((ext_vector_type(4)));
