@@ -555,11 +555,12 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // GFLOP, 8.5e8 exponentials) take 326 us; nothing bounds it alone: the matrix units are busy for 0.27 of the cycles, other vector
 // instructions take 0.33, exponentials 0.2 more, and products and exponentials of a tile follow each other.
 //
-// With first tokens (FIRST) a window leaves few slot tiles, so the rows are split over as many parts as there is room
-// for, whose sums k_weight_join adds up in their order: 145 us for 138 GFLOP's worth of pairs, of which 1 us a tile of 64 rows, the
-// rest the parts' beginnings and ends.
+// With first tokens (FIRST) a window leaves few slot tiles, and those of the first tokens are seen by every row: rows are split over
+// parts of about equal length, whose sums k_weight_join adds up in their order: 133 us for 138 GFLOP's worth of pairs, of which
+// 1 us a tile of 64 rows, the rest the parts' beginnings and ends. (Parts of at least four row tiles, six or eight: 256 tokens behind 12,001
+// 95, 92 and 92 us, 700 tokens of 256 dimensions 109, 102 and 104.)
 constexpr int kWSlots = 256, kWRows = 64;
-constexpr int kMostWeightParts = 16;
+constexpr int kMostWeightParts = 64, kLeastWeightPart = 6;  // parts of a slot tile, row tiles of one
 
 struct WeightPlan {
     int32_t groups;  // workgroups to fill (FIRST)
@@ -567,14 +568,98 @@ struct WeightPlan {
     float* part;     // [groups][kWSlots]
 };
 
-// The slot tiles that k_weight_chunk takes, and the parts of each, of ``total`` tiles of a key head.
-__device__ inline int weight_items(const WeightPlan& plan, int64_t total, int hk) { return (int)min((int64_t)plan.items, total * hk); }
-__device__ inline int weight_parts(const WeightPlan& plan, int items) { return max(1, min(kMostWeightParts, plan.groups / max(items, 1))); }
-
 template <bool FIRST>
 __device__ inline int slot_tiles(const AttendArgs& p, const Seq& s) {
     if (s.n <= 0 || s.n > p.kv.max_q || !ours(p, s)) return 0;
     return (line_of<FIRST>(p, s, kWSlots).places + kWSlots - 1) / kWSlots;
+}
+
+// The parts of so many row tiles, of about ``part`` each.
+__host__ __device__ inline int parts_of(int rows, int64_t part) {
+    const int64_t n = (rows + part / 2) / part;
+    return n < 1 ? 1 : n > kMostWeightParts ? kMostWeightParts : (int)n;
+}
+
+// The slot tiles of a sequence's key head, the first tokens' before the others, and the tiles of rows that see one of them, at most:
+// of the first tokens' no fewer.
+struct WeightTiles {
+    int head, all, head_rows, rows;
+    __device__ inline int64_t work() const { return (int64_t)head * head_rows + (int64_t)(all - head) * rows; }
+    // By parts of so many rows: the parts of all tiles, and (lower half) of those with more than one, which lie in WeightPlan::part.
+    __device__ inline int64_t parts(int64_t part) const {
+        const int64_t first = parts_of(head_rows, part), more = parts_of(rows, part), a = head * first, b = (all - head) * more;
+        return (a + b) << 32 | ((first > 1 ? a : 0) + (more > 1 ? b : 0));
+    }
+    // The tiles with more than one part, and (lower half) their parts.
+    __device__ inline int64_t split(int64_t part) const {
+        const int64_t first = parts_of(head_rows, part), more = parts_of(rows, part), a = first > 1 ? head : 0, b = more > 1 ? all - head : 0;
+        return (a + b) << 32 | (a * first + b * more);
+    }
+};
+__device__ inline WeightTiles weight_tiles(const AttendArgs& p, const Seq& s) {
+    const int all = slot_tiles<true>(p, s);
+    if (all <= 0) return {0, 0, 0, 0};
+    const int64_t G = p.heads / p.kv.kv_heads, some = min((int64_t)s.n, (int64_t)kWSlots + p.window);
+    return {min(all, (p.first + kWSlots - 1) / kWSlots), all, (int)((s.n * G + kWRows - 1) / kWRows), (int)((some * G + kWRows - 1) / kWRows)};
+}
+
+// Unit ``at`` of all that ``count`` has of tiles and parts in its upper half: its sequence and its number there; the units that lower
+// halves count before that sequence; and the row tiles of a part. Those go by all that there are to weigh, so that parts and tiles
+// that are not split are as many as the workgroups to fill, or half as many more than there are tiles. (A third of the room is for rounding: a
+// tile of one and a half parts has two.)  each = 0: there are more tiles than k_weight_chunk takes, and none is split.
+// For a whole workgroup of 256; seq < 0 where there is no such unit.
+struct WeightAt {
+    int64_t each, before;
+    int seq, unit;
+};
+template <class Count>
+__device__ inline WeightAt weight_at(const AttendArgs& p, const WeightPlan& plan, int at, Count count) {
+    __shared__ int64_t scan[8];
+    __shared__ WeightAt found;
+    const int hk = p.kv.kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = (p.kv.seqs + 255) / 256;
+    const int i0 = min(tid * per, p.kv.seqs), i1 = min(i0 + per, p.kv.seqs);
+    WeightTiles own{0, 0, 0, 0};
+    if (i0 < i1) own = weight_tiles(p, seq_of(p.kv, i0));
+    const auto tiles_of = [&](int i) { return i == i0 ? own : weight_tiles(p, seq_of(p.kv, i)); };
+    int64_t tiles = 0, work = 0;
+    for (int i = i0; i < i1; i++) {
+        const WeightTiles x = tiles_of(i);
+        tiles += x.all;
+        work += x.work();
+    }
+    for (int d = 32; d; d >>= 1) {
+        tiles += __shfl_xor(tiles, d);
+        work += __shfl_xor(work, d);
+    }
+    if (lane == 0) scan[wave] = tiles, scan[4 + wave] = work;
+    if (tid == 0) found.seq = -1;
+    __syncthreads();
+    tiles = scan[0] + scan[1] + scan[2] + scan[3];
+    work = scan[4] + scan[5] + scan[6] + scan[7];
+    if (tiles * hk > plan.items) return {0, 0, -1, 0};
+    const int64_t room = max(plan.groups - tiles * hk, (int64_t)plan.groups / 2) * 3 / 4;
+    const int64_t each = max((int64_t)kLeastWeightPart, (work * hk + room - 1) / room);
+
+    int64_t mine = 0;
+    for (int i = i0; i < i1; i++) mine += count(tiles_of(i), each);
+    int64_t before = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t x = __shfl_up(before, d);
+        if (lane >= d) before += x;
+    }
+    __syncthreads();
+    if (lane == 63) scan[wave] = before;
+    before -= mine;
+    __syncthreads();
+    for (int w = 0; w < wave; w++) before += scan[w];
+    for (int i = i0; i < i1 && before >> 32 <= at; i++) {
+        const int64_t c = count(tiles_of(i), each);
+        if (at < (before + c) >> 32) found = WeightAt{each, before & 0xffffffff, i, (int)(at - (before >> 32))};
+        before += c;
+    }
+    __syncthreads();
+    return {each, found.before, found.seq, found.unit};
 }
 
 // The sum over sixteen lanes in each of them, without a way through LDS.
@@ -777,18 +862,24 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
     const int hk = p.kv.kv_heads;
     int seq, tile;
     if constexpr (FIRST) {
-        int item = 0, part = 0, parts = 1, items = 0;
-        const auto place = [&](int64_t total) {
-            items = weight_items(plan, total, hk);
-            parts = weight_parts(plan, items);
-            if (blockIdx.x >= (int64_t)items * parts) return total;
-            part = blockIdx.x / items;
-            item = blockIdx.x - part * items;
-            return (int64_t)(item / hk);
-        };
-        if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan, seq, tile)) return;
-        float* to = parts > 1 ? plan.part + (int64_t)blockIdx.x * kWSlots : nullptr;
-        weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, item % hk, part, parts, to);
+        const WeightAt x = weight_at(p, plan, blockIdx.x / hk, [](const WeightTiles& t, int64_t each) { return t.parts(each); });
+        const int head = blockIdx.x % hk;
+        int part = 0, parts = 1;
+        float* to = nullptr;
+        if (x.each > 0) {
+            if (x.seq < 0) return;
+            seq = x.seq;
+            const WeightTiles t = weight_tiles(p, seq_of(p.kv, seq));
+            const int first = parts_of(t.head_rows, x.each), more = parts_of(t.rows, x.each), in = x.unit - t.head * first;
+            parts = in < 0 ? first : more;
+            tile = in < 0 ? x.unit / first : t.head + in / more;
+            part = in < 0 ? x.unit % first : in % more;
+            if (parts > 1) to = plan.part + ((x.before + x.unit) * hk + head) * kWSlots;
+        } else {
+            const auto place = [&](int64_t total) { return blockIdx.x < plan.items ? (int64_t)(blockIdx.x / hk) : total; };
+            if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan, seq, tile)) return;
+        }
+        weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, head, part, parts, to);
         return;
     }
     if (!find_item(p.kv, [&](int64_t) { return (int64_t)(blockIdx.x / hk); }, [&](const Seq& s) { return slot_tiles<FIRST>(p, s); }, scan,
@@ -797,25 +888,22 @@ __global__ __launch_bounds__(256, (D <= 128 ? 2 : 1)) void k_weight_chunk(Attend
     weigh_slots<E, D, FIRST>(p, seq_of(p.kv, seq), seq, tile, blockIdx.x % hk);
 }
 
-// The parts' sums of a tile's slots, a slot a thread.
+// The parts' sums of a split tile's slots, a slot a thread.
 __global__ __launch_bounds__(256) void k_weight_join(AttendArgs p, WeightPlan plan) {
-    __shared__ int64_t scan[4];
-    const int hk = p.kv.kv_heads, tid = threadIdx.x;
-    int seq, tile, items = 0, parts = 1;
-    const auto place = [&](int64_t total) {
-        items = weight_items(plan, total, hk);
-        parts = weight_parts(plan, items);
-        return parts > 1 && blockIdx.x < items ? (int64_t)(blockIdx.x / hk) : total;
-    };
-    if (!find_item(p.kv, place, [&](const Seq& s) { return slot_tiles<true>(p, s); }, scan, seq, tile)) return;
-    const Seq s = seq_of(p.kv, seq);
+    const int hk = p.kv.kv_heads, tid = threadIdx.x, head = blockIdx.x % hk;
+    const WeightAt x = weight_at(p, plan, blockIdx.x / hk, [](const WeightTiles& t, int64_t each) { return t.split(each); });
+    if (x.seq < 0) return;
+    const Seq s = seq_of(p.kv, x.seq);
+    const WeightTiles t = weight_tiles(p, s);
+    const int first = parts_of(t.head_rows, x.each), more = parts_of(t.rows, x.each), tile = x.unit, in = tile - t.head, parts = in < 0 ? first : more;
+    const int64_t part = x.before + (in < 0 ? tile * first : t.head * first + in * more);
     const int j = slot_of<true>(line_of<true>(p, s, kWSlots), tile * kWSlots) + tid;
-    const int row = j < s.len ? pool_row(p.kv, seq, j) : -1;
+    const int row = j < s.len ? pool_row(p.kv, x.seq, j) : -1;
     if (row < 0) return;
     float sum = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < parts; i++) sum += plan.part[((int64_t)i * items + blockIdx.x) * kWSlots + tid];
-    p.kv.weight[stat_index(p.kv, row, blockIdx.x % hk)] += sum;
+#pragma unroll 8
+    for (int i = 0; i < parts; i++) sum += plan.part[((part + i) * hk + head) * kWSlots + tid];
+    p.kv.weight[stat_index(p.kv, row, head)] += sum;
 }
 
 // Sequences with slots that have no page can have more tiles than that: those from ``first`` on, in a loop (a kernel of its own,
@@ -845,10 +933,11 @@ int32_t split_groups(const AttendSizes& z, int32_t few) {
     return least * z.kv_heads > groups / 2 ? 0 : groups;
 }
 
-// Workgroups that the weights' parts fill: four times what the GPU holds, so that the last ones to come are short.  (2,048 tokens behind
-// 12,001 in a window of 4,096, 200 slot tiles, the whole call: not split some 530 us, filled once 359, twice 342, three times 334, four
-// times 332.)
-int32_t weight_groups(const AttendSizes& z) { return z.first > 0 && z.add_weight ? (z.dim <= 128 ? 2048 : 1024) : 0; }
+// Workgroups that the weights' parts fill: five times what the GPU holds, so that the last ones to come are short.  (Whole calls, filled three
+// times, four times and five times: a prompt of 16,384 tokens in a window of 1,024 + 4 819, 765 and 756 us, 1,206 with as many parts for every
+// slot tile; six prompts of 16 heads, window 2,048 + 4, 330, 330 and 312; 2,048 tokens behind 12,001, window 4,096 + 16, 339, 334 and
+// 341, some 530 not split.)
+int32_t weight_groups(const AttendSizes& z) { return z.first > 0 && z.add_weight ? (z.dim <= 128 ? 2560 : 1280) : 0; }
 
 int64_t split_bytes(const AttendSizes& z, int32_t few) {
     const int32_t groups = split_groups(z, few);
@@ -856,6 +945,18 @@ int64_t split_bytes(const AttendSizes& z, int32_t few) {
 }
 
 int64_t chunk_workspace(const AttendSizes& z, int32_t few) { return split_bytes(z, few) + (int64_t)weight_groups(z) * kWSlots * 4; }
+
+// Parts of a tile at most, if all rows of the longest sequence see it.
+int most_parts(const AttendSizes& z) {
+    const int64_t rows = (int64_t)(z.max_q < z.tokens ? z.max_q : z.tokens) * (z.heads / z.kv_heads);
+    return weight_groups(z) ? parts_of((int)((rows + kWRows - 1) / kWRows), kLeastWeightPart) : 1;
+}
+
+// Workgroups of k_weight_chunk for so many tiles: those and the parts that weight_at makes.
+int64_t weight_blocks(const AttendSizes& z, int64_t tiles) {
+    const int64_t groups = weight_groups(z), all = tiles * most_parts(z), fill = tiles < groups / 2 ? groups : tiles + groups / 2;
+    return all < fill ? all : fill;
+}
 
 // Workgroups of the launches for these sizes.
 struct ChunkGrids {
@@ -902,9 +1003,9 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
     }
     if (g.tiles > 0) {
         const WeightPlan w{weight_groups(z), (int32_t)g.tiles, (float*)(ws + split_bytes(z, a.few))};
-        e = run(k_weight_chunk<E, D, FIRST>, dim3((unsigned)(g.tiles > w.groups ? g.tiles : w.groups)), 256, s, a, w);
+        e = run(k_weight_chunk<E, D, FIRST>, dim3((unsigned)weight_blocks(z, g.tiles)), 256, s, a, w);
         if (e != hipSuccess) return e;
-        if (w.groups) {  // tiles in two parts or more are at most half as many as that
+        if (most_parts(z) > 1) {  // split tiles have two parts or more, of which there are no more than w.groups
             e = run(k_weight_join, dim3((unsigned)(g.tiles < w.groups / 2 ? g.tiles : w.groups / 2)), 256, s, a, w);
             if (e != hipSuccess) return e;
         }
@@ -937,7 +1038,7 @@ int64_t attend_threads(const AttendSizes& z) {
     if (has_chunks(z)) {
         const ChunkGrids g = grids(z, few_rows(z));
         if (g.blocks > most) most = g.blocks;
-        if (g.tiles > most) most = g.tiles;
+        if (weight_blocks(z, g.tiles) > most) most = weight_blocks(z, g.tiles);
         if (g.more > most) most = g.more;
     }
     return most * 256;

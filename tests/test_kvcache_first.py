@@ -326,3 +326,28 @@ def test_first_is_refused_where_it_is_no_number_of_tokens():
     for bad in (-1, 2 ** 31):
         with pytest.raises(S.SvfError, match="first"):
             C.attend(s["q"].cuda(), batch_of(s), C.Cache(s["k"].cuda(), s["v"].cuda()), window=4, first=bad)
+
+
+# Every row of a prompt sees the first tokens: their weights are added up in more parts than those of the window's slots.
+
+@gpu
+@pytest.mark.parametrize("heads,kv_heads,dim,lens,new,causal,window,first", [
+    (8, 2, 128, [1500, 2300, 90], [1500, 700, 90], True, 100, 300), (8, 2, 128, [3000], [3000], True, 50, 4),
+    (8, 2, 128, [1100, 700], [600, 700], False, 400, 513), (4, 1, 64, [4500], [4500], True, 700, 600),
+    (16, 16, 256, [1900, 1400, 1900, 2100], [1900, 1400, 1900, 2100], True, 64, 4), (6, 2, 64, [70, 2000, 513], [70, 1999, 513], True, 1, 1)])
+def test_weights_of_prompts(heads, kv_heads, dim, lens, new, causal, window, first):
+    s = make(18, lens, new, heads, kv_heads, dim, 16, BF, stats=True)
+    _, _, a = check(s, window, first, causal=causal, add_weight=True)
+    _, _, b = check(s, window, first, causal=causal, add_weight=True)
+    assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("new", [60, 300])
+def test_weights_where_few_slots_have_a_page(new):
+    s = make(19, [max(new, 64), 300], [new, 30], 8, 2, 128, 16, BF, stats=True)
+    pages = -(-max(new, 64) // 16)
+    table = torch.full((2, 375), -1, dtype=torch.int32)
+    table[0, 375 - pages:], table[1, :19] = s["table"][0, :pages], s["table"][1, :19]
+    s["table"], s["kv_len"] = table, torch.tensor([375 * 16 - pages * 16 + max(new, 64), 300], dtype=torch.int32)
+    check(s, 4000, 100, add_weight=True)
