@@ -605,7 +605,7 @@ int64_t workspace(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) { ret
 
 int64_t threads(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     const Layout y = layout(rows, vocab, top, dtype);
-    return (int64_t)rows * y.parts * y.threads;
+    return (int64_t)rows * y.parts * (y.threads < kUsual ? kUsual : y.threads);  // as many rows of any vocabulary that is not split
 }
 
 hipError_t launch(const Args& a, int32_t dtype, hipStream_t s) {
