@@ -560,7 +560,11 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // 1 us a tile of 64 rows, the rest the parts' beginnings and ends. (Parts of at least four row tiles, six or eight: 256 tokens behind 12,001
 // 95, 92 and 92 us, 700 tokens of 256 dimensions 109, 102 and 104.)
 constexpr int kWSlots = 256, kWRows = 64;
-constexpr int kMostWeightParts = 64, kLeastWeightPart = 6;  // parts of a slot tile, row tiles of one
+constexpr int kMostWeightParts = 64;  // of a slot tile
+// Row tiles of a part at least, and where such parts would not fill what the GPU holds at a time (three chunks of 112 to 336 tokens with 256
+// dimensions, eight query heads on each of two key heads: 101 us, and 110 with parts of six).
+constexpr int kLeastWeightPart = 6, kLeastOfFew = 2;
+constexpr int kWeightFills = 5;  // times that parts fill what the GPU holds
 
 struct WeightPlan {
     int32_t groups;  // workgroups to fill (FIRST)
@@ -639,7 +643,8 @@ __device__ inline WeightAt weight_at(const AttendArgs& p, const WeightPlan& plan
     work = scan[4] + scan[5] + scan[6] + scan[7];
     if (tiles * hk > plan.items) return {0, 0, -1, 0};
     const int64_t room = max(plan.groups - tiles * hk, (int64_t)plan.groups / 2) * 3 / 4;
-    const int64_t each = max((int64_t)kLeastWeightPart, (work * hk + room - 1) / room);
+    const int64_t least = max((int64_t)kLeastOfFew, min((int64_t)kLeastWeightPart, (work * hk * kWeightFills + plan.groups - 1) / plan.groups));
+    const int64_t each = max(least, (work * hk + room - 1) / room);
 
     int64_t mine = 0;
     for (int i = i0; i < i1; i++) mine += count(tiles_of(i), each);
@@ -933,11 +938,11 @@ int32_t split_groups(const AttendSizes& z, int32_t few) {
     return least * z.kv_heads > groups / 2 ? 0 : groups;
 }
 
-// Workgroups that the weights' parts fill: five times what the GPU holds, so that the last ones to come are short.  (Whole calls, filled three
+// Workgroups that the weights' parts fill: what the GPU holds kWeightFills times, so that the last ones to come are short.  (Whole calls, filled three
 // times, four times and five times: a prompt of 16,384 tokens in a window of 1,024 + 4 819, 765 and 756 us, 1,206 with as many parts for every
 // slot tile; six prompts of 16 heads, window 2,048 + 4, 330, 330 and 312; 2,048 tokens behind 12,001, window 4,096 + 16, 339, 334 and
 // 341, some 530 not split.)
-int32_t weight_groups(const AttendSizes& z) { return z.first > 0 && z.add_weight ? (z.dim <= 128 ? 2560 : 1280) : 0; }
+int32_t weight_groups(const AttendSizes& z) { return z.first > 0 && z.add_weight ? (z.dim <= 128 ? 512 : 256) * kWeightFills : 0; }
 
 int64_t split_bytes(const AttendSizes& z, int32_t few) {
     const int32_t groups = split_groups(z, few);
@@ -946,15 +951,18 @@ int64_t split_bytes(const AttendSizes& z, int32_t few) {
 
 int64_t chunk_workspace(const AttendSizes& z, int32_t few) { return split_bytes(z, few) + (int64_t)weight_groups(z) * kWSlots * 4; }
 
-// Parts of a tile at most, if all rows of the longest sequence see it.
-int most_parts(const AttendSizes& z) {
+// Parts of a tile at most, if all rows of the longest sequence see it and a part has no fewer than ``least`` row tiles.
+int most_parts(const AttendSizes& z, int least) {
     const int64_t rows = (int64_t)(z.max_q < z.tokens ? z.max_q : z.tokens) * (z.heads / z.kv_heads);
-    return weight_groups(z) ? parts_of((int)((rows + kWRows - 1) / kWRows), kLeastWeightPart) : 1;
+    return weight_groups(z) ? parts_of((int)((rows + kWRows - 1) / kWRows), least) : 1;
 }
 
 // Workgroups of k_weight_chunk for so many tiles: those and the parts that weight_at makes.
 int64_t weight_blocks(const AttendSizes& z, int64_t tiles) {
-    const int64_t groups = weight_groups(z), all = tiles * most_parts(z), fill = tiles < groups / 2 ? groups : tiles + groups / 2;
+    const int64_t groups = weight_groups(z), fill = tiles < groups / 2 ? groups : tiles + groups / 2;
+    // parts of fewer row tiles than usual fill what the GPU holds once, and a third more by rounding
+    const int64_t few = tiles * most_parts(z, kLeastOfFew), once = tiles + groups / kWeightFills * 4 / 3 + 1, usual = tiles * most_parts(z, kLeastWeightPart);
+    const int64_t all = few < once ? few : once < usual ? usual : once;
     return all < fill ? all : fill;
 }
 
@@ -1005,7 +1013,7 @@ hipError_t launch(const AttendArgs& a, const AttendSizes& z, char* ws, hipStream
         const WeightPlan w{weight_groups(z), (int32_t)g.tiles, (float*)(ws + split_bytes(z, a.few))};
         e = run(k_weight_chunk<E, D, FIRST>, dim3((unsigned)weight_blocks(z, g.tiles)), 256, s, a, w);
         if (e != hipSuccess) return e;
-        if (most_parts(z) > 1) {  // split tiles have two parts or more, of which there are no more than w.groups
+        if (most_parts(z, kLeastOfFew) > 1) {  // split tiles have two parts or more, of which there are no more than w.groups
             e = run(k_weight_join, dim3((unsigned)(g.tiles < w.groups / 2 ? g.tiles : w.groups / 2)), 256, s, a, w);
             if (e != hipSuccess) return e;
         }
