@@ -136,20 +136,33 @@ __device__ inline uint4 load_once(const uint4* at) {
 // The distance of a logit from the largest of all in log2 terms (by halves, so that it does not pass what 32 bits hold on the way).
 __device__ inline float distance(float x, float m, float scale2) { return (0.5f * x - 0.5f * m) * (2.f * scale2); }
 
-// What a row's scalars come to.
+// What a row's sums come to: whether it has no distribution, or nothing that is allowed, and the logarithm of its sum. The largest logit's own power is 1, so
+// no sum is below that; rounded from a lane's reference and back it can be 1 - 2^-24, and a certain token would have a
+// probability above 1.
+struct Total {
+    bool bad, none;
+    float sum, log;
+};
+__device__ inline Total total_of(const Part& x) {
+    Total t;
+    t.bad = !(x.s * 0.f == 0.f) || x.m == INFINITY;
+    t.none = x.m == -INFINITY && x.s == 0.f;
+    t.sum = fmaxf(x.s, 1.f);
+    t.log = __builtin_amdgcn_logf(t.sum) * kLn2;
+    return t;
+}
 __device__ inline void write_row(const Args& p, int row, const Part& x, bool known, float mine) {
-    const bool none = x.m == -INFINITY && x.s == 0.f, bad = !(x.s * 0.f == 0.f) || x.m == INFINITY;
-    const float total = __builtin_amdgcn_logf(x.s) * kLn2, nan = __builtin_nanf("");
-    p.logprob[row] = !known || bad ? nan : none ? -INFINITY : distance(mine, x.m, p.scale) - total;
-    p.entropy[row] = bad ? nan : none ? 0.f : total - x.sy / x.s * kLn2;
+    const Total t = total_of(x);
+    const float nan = __builtin_nanf("");
+    p.logprob[row] = !known || t.bad ? nan : t.none ? -INFINITY : distance(mine, x.m, p.scale) - t.log;
+    p.entropy[row] = t.bad ? nan : t.none ? 0.f : fmaxf(t.log - x.sy / t.sum * kLn2, 0.f);
     p.rank[row] = known ? x.before : -1;
 }
 __device__ inline void write_top(const Args& p, int row, int at, const Part& x, uint64_t key) {
-    const bool none = x.m == -INFINITY && x.s == 0.f, bad = !(x.s * 0.f == 0.f) || x.m == INFINITY;
-    const float total = __builtin_amdgcn_logf(x.s) * kLn2;
+    const Total t = total_of(x);
     p.top_index[(int64_t)row * p.top + at] = (int)~(uint32_t)key;
     p.top_logprob[(int64_t)row * p.top + at] =
-        bad ? __builtin_nanf("") : none ? -INFINITY : distance(logit_of((uint32_t)(key >> 32)), x.m, p.scale) - total;
+        t.bad ? __builtin_nanf("") : t.none ? -INFINITY : distance(logit_of((uint32_t)(key >> 32)), x.m, p.scale) - t.log;
 }
 
 // The logits of one part: vectors [v0, v1) of the row's grid, and with the first part the up to 9 W - 2 logits before its first line

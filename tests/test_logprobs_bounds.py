@@ -1,0 +1,34 @@
+"""What no rounding may take from scores of answers: a probability is at most 1, an entropy at least 0."""
+
+import pytest
+import torch
+
+from test_logprobs import BF, F32, HF, INF, check, logits
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
+@pytest.mark.parametrize("rows,vocab", [(400, 1000), (300, 32000), (2, 150000)])
+@pytest.mark.parametrize("scale", [1.0, 1 / 0.7])
+def test_one_allowed_token_is_certain(dtype, rows, vocab, scale):
+    """All others at -infinity: ln 1 = 0, whatever the one logit is.  The sum is a power of two times its inverse, a step of
+    2^-23 each and half a one for the product, and its logarithm has a step: below 2^-21."""
+    from paper_2606_22327_amd import logprobs as L
+    _, token, g = logits(rows, rows, vocab, F32)
+    x = torch.full((rows, vocab), -INF, dtype=dtype)
+    x[torch.arange(rows), token] = (10 * torch.randn(rows, generator=g)).to(dtype)
+    r = L.score(x.cuda(), token.cuda(), top=2, scale=scale)
+    for y in (r.logprob, -r.entropy, r.top_logprob[:, 0]):
+        assert (y <= 0).all() and (y >= -2.0 ** -21).all(), (y.max(), y.min())
+    assert (r.top_logprob[:, 1] == -INF).all() and torch.equal(r.top_index[:, 0].cpu().long(), token)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("ahead", [8.0, 20.0, 40.0, 120.0])
+@pytest.mark.parametrize("rows,vocab", [(300, 5001), (3, 150000)])
+def test_near_certain_tokens(dtype, ahead, rows, vocab):
+    x, token, _ = logits(int(ahead), rows, vocab, dtype, 1.0)
+    x[torch.arange(rows), token] += ahead
+    r = check(x, token, top=5)
+    assert (r.logprob <= 0).all() and (r.top_logprob <= 0).all() and (r.entropy >= 0).all()
