@@ -287,33 +287,31 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan p
                 for (int i = 0; i < W; i++) before += __popcll(__ballot(L::at(w[u], i) >= least));
             }
         }
-        // 0 times -infinity is 0: from the first such logit of a wave on, distances are kept above what gives 0
-        const float had = sumy;
-        if (!masked) {
+        // A vector's powers by themselves, the vectors', then all that there were before: one after another, those of unlikely tokens would be
+        // lost beside a likely one's 1.  0 times -infinity is 0: from the first such logit of a wave on, distances are kept above
+        // what gives 0.
+        auto powers = [&](auto low) {
+            float more = 0.f, morey = 0.f;
 #pragma unroll
             for (int u = 0; u < U; u++) {
-                const uint4 x = __is_same(T, _Float16) ? again(w[u]) : w[u];
+                const uint4 x = low || __is_same(T, _Float16) ? again(w[u]) : w[u];
+                float part = 0.f, party = 0.f;
 #pragma unroll
                 for (int i = 0; i < W; i++) {
-                    const float y = fmaf(L::at(x, i), c, b), e = __builtin_amdgcn_exp2f(y);
-                    sum += e;
-                    sumy = fmaf(e, y, sumy);
+                    const float y = fmaf(L::at(x, i), c, b), e = __builtin_amdgcn_exp2f(y), near = low ? fmaxf(y, -200.f) : y;
+                    part = i ? part + e : e;
+                    party = i ? fmaf(e, near, party) : e * near;
                 }
+                more = u ? more + part : part;
+                morey = u ? morey + party : party;
             }
-            if (!__any(sumy != sumy)) return;
-            sumy = had;
-        }
-        const float once = masked ? 1.f : 0.f;
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const uint4 x = again(w[u]);
-#pragma unroll
-            for (int i = 0; i < W; i++) {
-                const float y = fmaf(L::at(x, i), c, b), e = __builtin_amdgcn_exp2f(y);
-                sum = fmaf(e, once, sum);
-                sumy = fmaf(e, fmaxf(y, -200.f), sumy);
-            }
-        }
+            if (!low && __any(morey != morey)) return false;
+            sum += more;
+            sumy += morey;
+            return true;
+        };
+        if (!masked && powers(std::false_type())) return;
+        powers(std::true_type());
         masked = true;
     };
     for (int it = 0; it < whole; it++, v += U * NT) {
