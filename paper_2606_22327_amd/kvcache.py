@@ -11,8 +11,8 @@ steps does to a layer's cache on the GPU:
 
 Argument marshalling only, in ``csrc/svf_binding.cpp`` for ordinary arguments and here for all others: every step runs in
 the HIP kernels of ``libsvfsim.so``, on torch's current stream of the tensors' device.  All tensors are
-on one GPU.  There are no backward passes: where gradients are recorded, tensors that
-require one are refused.  Arguments that can be checked on the host are, and raise
+on one GPU.  There are no derivatives: tensors that require a gradient, where gradients are recorded, and
+tensors with a tangent of forward mode are refused, and so is a call that is being traced.  Arguments that can be checked on the host are, and raise
 ``svfsim.SvfError`` (``SVF_EINVAL``); what lengths, offsets and page numbers in
 device memory do is said in ``svfkv.h``.
 """
@@ -21,9 +21,11 @@ from __future__ import annotations
 
 import math
 import struct
+import sys
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import svfsim
 
@@ -82,7 +84,7 @@ def _check(rc: int, error=last_error):
 
 
 # What follows is the long way, for whatever the binding has not taken: another device than the current one, tensors of
-# gradients, arguments to be refused.  The checks are one expression each where all is well; which of them failed is found out afterwards.
+# derivatives, traces, arguments to be refused.  The checks are one expression each where all is well; which of them failed is found out afterwards.
 
 def _pack(cache: Cache, batch: Batch, tokens: int) -> Tuple[bytes, bytes]:
     k, v, weight, position = cache
@@ -178,10 +180,19 @@ def _call(fn, dev: int, *packed, error=last_error):
         _check(rc, error)
 
 
-def _gradient():
-    """Called where a tensor requires a gradient, which would be lost without a word."""
-    _need(not torch.is_grad_enabled(),
-          "these calls have no backward pass: tensors must not require a gradient (or use torch.no_grad())")
+def _no_derivatives(*tensors: Optional[torch.Tensor]):
+    """Refuses what would be lost without a word: gradients that are recorded, tangents, a place in a trace (which would hold
+    this call's numbers, or its buffers without what the kernels write)."""
+    level = getattr(forward_ad, "_current_level", 0) >= 0       # else no tensor has a tangent
+    for t in tensors:
+        if t is not None and (t.requires_grad or level):
+            _need(not (t.requires_grad and torch.is_grad_enabled()),
+                  "these calls have no backward pass: tensors must not require a gradient (or use torch.no_grad())")
+            _need(not level or forward_ad.unpack_dual(t).tangent is None,
+                  "these calls have no derivative of forward mode: tensors must not have a tangent")
+    fx = sys.modules.get("torch.fx.experimental.proxy_tensor")
+    if torch.jit.is_tracing() or (fx is not None and fx.get_proxy_mode() is not None):
+        _need(False, "these calls cannot be traced")
 
 
 def _raw_stream(dev: int) -> int:
@@ -234,9 +245,7 @@ def append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.T
                                           _raw_stream(dev))
         if r is not None:
             return _check(r) if r.__class__ is int else r
-    if (q.requires_grad or k.requires_grad or v.requires_grad or cache.k.requires_grad or cache.v.requires_grad
-            or (rope is not None and rope.requires_grad) or (q_out is not None and q_out.requires_grad)):
-        _gradient()
+    _no_derivatives(q, k, v, cache.k, cache.v, rope, q_out)
     kind, kv_heads = _kind(cache)
     dev = kind[1]
     qt, qh = _rows(q, "q", *kind)
@@ -299,10 +308,7 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
         r = (_bound or _binding()).attend(q, batch, cache, causal, window, scale, add_weight, first, dev, _raw_stream(dev))
         if r is not None:
             return _check(r) if r.__class__ is int else r
-    if (q.requires_grad or cache.k.requires_grad or cache.v.requires_grad
-            or (add_weight and cache.weight is not None and cache.weight.requires_grad)
-            or (out is not None and out.requires_grad)):
-        _gradient()
+    _no_derivatives(q, cache.k, cache.v, cache.weight if add_weight else None, out)
     kind, _ = _kind(cache)
     qt, qh = _rows(q, "q", *kind)
     if batch.q_offsets is None:
@@ -347,8 +353,7 @@ def evict(batch: Batch, cache: Cache, budget: int, recent: int, next_position: t
     before ``next_position`` (int32 [seqs]) and the rest by largest ``cache.weight``
     (ties to the lower slot).  Rows move inside the cache; returns the new lengths."""
     k, kv_len = cache.k, batch.kv_len
-    if k.requires_grad or cache.v.requires_grad or (cache.weight is not None and cache.weight.requires_grad):
-        _gradient()
+    _no_derivatives(k, cache.v, cache.weight)
     kv, seqs = _pack(cache, batch, 0)
     if cache.weight is None or cache.position is None:
         _need(False, "evict needs the cache's weight and position")

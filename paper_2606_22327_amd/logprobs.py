@@ -4,8 +4,8 @@ tokens, their ranks, entropies and the best alternatives, from logits.
 ``score``   one row of logits and one token for each request of a step, or for each token of a prompt
 
 Argument marshalling only, in ``csrc/svf_binding.cpp`` for ordinary arguments and here for all others: every step runs in the HIP kernels of ``libsvfsim.so``, on
-torch's current stream of the tensors' device.  There is no backward pass: where gradients are recorded, logits that
-require one are refused.  What can be checked on the host raises ``svfsim.SvfError`` (``SVF_EINVAL``).
+torch's current stream of the tensors' device.  There are no derivatives: logits that require a gradient, where
+gradients are recorded, or have a tangent of forward mode are refused, and so is a call that is being traced.  What can be checked on the host raises ``svfsim.SvfError`` (``SVF_EINVAL``).
 """
 
 from __future__ import annotations
@@ -16,7 +16,7 @@ from typing import NamedTuple
 import torch
 
 from . import kvcache, svfsim
-from .kvcache import _call, _gradient, _need
+from .kvcache import _call, _need, _no_derivatives
 
 DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 TOKEN = {torch.int32: 4, torch.int64: 8}
@@ -54,8 +54,7 @@ def score(logits: torch.Tensor, token: torch.Tensor, top: int = 0, scale: float 
         r = (kvcache._bound or kvcache._binding()).score(logits, token, top, float(scale), dev, kvcache._raw_stream(dev))
         if r is not None:
             return Scores._make(r) if r.__class__ is tuple else kvcache._check(r, last_error)
-    if logits.requires_grad:
-        _gradient()
+    _no_derivatives(logits)
     shape, dev = logits.shape, logits.get_device()
     if not (len(shape) == 2 and logits.dtype in DTYPE and (shape[1] < 2 or logits.stride(1) == 1) and dev >= 0):
         _need(len(shape) == 2 and logits.dtype in DTYPE, "logits must be [rows, vocab], bfloat16, float16 or float32")
