@@ -5,12 +5,15 @@ the C ABI of ``include/svfsim.h``, the paged cache's operators
 (``include/svfkv.h``), the scores of answers (``include/svflogprob.h``) and the host-side exact optimum of tiny burst instances
 (``include/svfopt.h``).  It is built in-tree so that the same file
 is loaded by the tests, the smoke check and the benchmark.  ``_svfbinding.so`` beside it
-is the cache's binding to torch.
+is the binding to torch of the cache's calls and the scores; without a compiler or headers for it the library is built all the same.
 """
 
 import os
+import shutil
 import subprocess
 import sys
+import warnings
+from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -72,16 +75,27 @@ def build(verbose: bool = False) -> str:
 BINDING = os.path.join(PKG, "_svfbinding.so")
 
 
-def build_binding() -> str:
+def build_binding() -> Optional[str]:
+    """None, with a warning and without the file of an earlier build, where the compiler or one of the headers is not there: the
+    library serves without it, only slower calls from Python go through it."""
     import sysconfig
 
-    import torch
-
-    at = os.path.dirname(torch.__file__)
-    include = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"),
-               sysconfig.get_path("include")]
+    try:
+        import torch
+    except ImportError:
+        torch = None
+    python, at = sysconfig.get_path("include"), os.path.dirname(torch.__file__) if torch else ""
+    include = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"), python]
+    missing = [what for what, there in (("g++", shutil.which("g++")), ("Python.h", os.path.exists(os.path.join(python, "Python.h"))),
+                                        ("torch", torch), ("torch's headers", torch and os.path.isdir(include[1]))) if not there]
+    if missing:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)
+        warnings.warn(f"the binding to torch is not built: no {', no '.join(missing)}", RuntimeWarning, stacklevel=2)
+        return None
     tmp = BINDING + ".tmp"
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          f'-DSVF_TORCH_VERSION="{torch.__version__}"',
           "-I", INCLUDE, *[x for i in include for x in ("-isystem", i)], os.path.join(CSRC, "svf_binding.cpp"), "-o", tmp,
           "-L", PKG, "-l:libsvfsim.so", "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
           "-Wl,-rpath,$ORIGIN"])

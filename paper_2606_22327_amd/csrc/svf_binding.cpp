@@ -295,4 +295,9 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_svfbinding", nullptr, -1, kMetho
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__svfbinding() { return PyModule_Create(&kModule); }
+// ``torch_version``: the torch whose headers this was built with.  kvcache.py uses it with no other.
+PyMODINIT_FUNC PyInit__svfbinding() {
+    PyObject* m = PyModule_Create(&kModule);
+    if (m && PyModule_AddStringConstant(m, "torch_version", SVF_TORCH_VERSION) != 0) Py_CLEAR(m);
+    return m;
+}

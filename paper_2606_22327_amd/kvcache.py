@@ -9,7 +9,8 @@ steps does to a layer's cache on the GPU:
 ``rope_table``   cosines and sines by position, for the rotation
 ``pair_axes``   which axis of a position each pair of a head turns by
 
-Argument marshalling only, in ``csrc/svf_binding.cpp`` for ordinary arguments and here for all others: every step runs in
+Argument marshalling only, in ``csrc/svf_binding.cpp`` for ordinary arguments and here for all others (for all, with a
+warning, where that is not built): every step runs in
 the HIP kernels of ``libsvfsim.so``, on torch's current stream of the tensors' device.  All tensors are
 on one GPU.  There are no derivatives: tensors that require a gradient, where gradients are recorded, and
 tensors with a tangent of forward mode are refused, and so is a call that is being traced.  Arguments that can be checked on the host are, and raise
@@ -22,6 +23,7 @@ from __future__ import annotations
 import math
 import struct
 import sys
+import warnings
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
@@ -207,16 +209,26 @@ _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)     # 
 _bound = None
 
 
+class _NoBinding:
+    """In the place of a binding that there is not: takes nothing, so that every call goes the long way."""
+
+    append = attend = score = staticmethod(lambda *a: None)
+
+
 def _binding():
-    """The compiled binding (raises if it is not built)."""
+    """The compiled binding, if it is built and of this torch."""
     global _bound
     if _bound is None:
         svfsim.load()       # torch's runtime, then the library, then what links both
         try:
             from . import _svfbinding
+            why = "" if getattr(_svfbinding, "torch_version", None) == str(torch.__version__) else "it is of another torch"
         except ImportError as e:
-            raise RuntimeError(f"_svfbinding.so is not built ({e}); run __graft_entry__.build()") from None
-        _bound = _svfbinding
+            why = str(e)
+        if why:
+            warnings.warn(f"_svfbinding.so is not used ({why}): calls take some microseconds more; run __graft_entry__.build()",
+                          RuntimeWarning, stacklevel=3)
+        _bound = _NoBinding if why else _svfbinding
     return _bound
 
 
