@@ -215,7 +215,11 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan p
     constexpr int W = L::W, U = 4, kEntries = entries_of(NT), kCand = kEntries / 2;
     constexpr float kSlack = 8.f;
     static_assert(9 * W - 2 <= NT, "a thread an edge");
-    __shared__ float largest[TOP ? kEntries : 1];
+    // the pieces' largest logits, and in their place, once those are done with, keys of logits
+    __shared__ __align__(16) char board[TOP ? kEntries * sizeof(float) : 16];
+    float* const largest = (float*)board;
+    uint64_t* const cand = (uint64_t*)board;
+    static_assert(__alignof__(board) >= alignof(uint64_t) && kCand * sizeof(uint64_t) <= kEntries * sizeof(float), "the keys fit and lie at their boundary");
     __shared__ uint16_t listed[TOP ? kListed : 1];
     __shared__ int hits[NT / 64];
     __shared__ uint64_t sh_bound;
@@ -453,7 +457,6 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan p
         }
         __syncthreads();
         // the logits that reach it, in the pieces' place
-        uint64_t* cand = (uint64_t*)largest;
         const int pieces = min(sh_listed, kListed);
         for (int i0 = tid; i0 < pieces << shift; i0 += 2 * NT) {
             uint4 w[2];
