@@ -118,7 +118,8 @@ __global__ __launch_bounds__(256, waves_per_simd(D, RT)) void k_attend_rows(Atte
     using T = typename E::T;
     using V8 = typename E::V8;
     constexpr int KS = D / 32, VD = D / 16;
-    __shared__ float red[4][16][D + 4];
+    __shared__ __align__(16) float red[4][16][D + 4];
+    static_assert(__alignof__(red) >= alignof(f32x4) && D / 16 % 4 == 0, "four at a time are written at their boundary");
     __shared__ float red_m[4][16], red_l[4][16];
     __shared__ int64_t scan[4];
     __shared__ uint32_t odd_marks[16 * RT][16];  // a word for D / 16 dimensions of a row
