@@ -585,7 +585,8 @@ __host__ __device__ inline int parts_of(int rows, int64_t part) {
 }
 
 // The slot tiles of a sequence's key head, the first tokens' before the others, and the tiles of rows that see one of them, at most:
-// of the first tokens' no fewer.
+// of the first tokens' no fewer.  (Not causal, rows before a window's slots see them too.  Counted as if they did not, 4,096 tokens, window 100 + 4, eight
+// query heads on two key heads took 190 us with weights, and 177 as here; 32 on eight 449 and 419; 2,048, eight on one 90 and 76.)
 struct WeightTiles {
     int head, all, head_rows, rows;
     __device__ inline int64_t work() const { return (int64_t)head * head_rows + (int64_t)(all - head) * rows; }
@@ -603,7 +604,7 @@ struct WeightTiles {
 __device__ inline WeightTiles weight_tiles(const AttendArgs& p, const Seq& s) {
     const int all = slot_tiles<true>(p, s);
     if (all <= 0) return {0, 0, 0, 0};
-    const int64_t G = p.heads / p.kv.kv_heads, some = min((int64_t)s.n, (int64_t)kWSlots + p.window);
+    const int64_t G = p.heads / p.kv.kv_heads, some = p.causal ? min((int64_t)s.n, (int64_t)kWSlots + p.window) : s.n;
     return {min(all, (p.first + kWSlots - 1) / kWSlots), all, (int)((s.n * G + kWRows - 1) / kWRows), (int)((some * G + kWRows - 1) / kWRows)};
 }
 
