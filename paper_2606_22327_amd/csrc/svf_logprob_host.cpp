@@ -59,8 +59,8 @@ int svf_logprob(const svf_logprob_args* a, void* hip_stream) {
     if (int rc = check(a)) return rc;
     if (a->row_stride < 0 || a->row_stride >= kStrideLimit) return fail(SVF_EINVAL, "row_stride must be in 0 .. 2^40");
     if (a->token_bytes != 4 && a->token_bytes != 8) return fail(SVF_EINVAL, "token_bytes must be 4 or 8 (%d)", a->token_bytes);
-    const float scale = a->scale * 1.4426950408889634f;  // for powers of two
-    if (!(scale > 0.f) || !(2.f * scale < INFINITY)) return fail(SVF_EINVAL, "scale must be above 0 and below 2^126");
+    const float scale = a->scale * 1.4426950408889634f;  // for powers of two; twice that is a number too
+    if (!(scale > 0.f) || !(a->scale < 0x1p126f)) return fail(SVF_EINVAL, "scale must be above 0 and below 2^126");
     if (a->rows == 0) return SVF_OK;
     if (!a->logits || !a->token || !a->logprob || !a->entropy || !a->rank || (a->top > 0 && (!a->top_logprob || !a->top_index)))
         return fail(SVF_EINVAL, "logits, token and outputs must not be NULL");
