@@ -3,10 +3,36 @@
 import pytest
 import torch
 
-from test_kvcache import BF, make
+from test_kvcache import BF, HF, make
 from test_kvcache_first import check
 
 pytestmark = pytest.mark.gpu
+
+
+def thinned(seed, lens, new, heads, kv_heads, dim, page, dtype, keep):
+    """Sequences of ``lens`` slots of which only the pages ``keep`` (from the end where negative) are there."""
+    held = [sorted({x % -(-n // page) for x in keep}) for n in lens]
+    s = make(seed, [len(h) * page for h in held], new, heads, kv_heads, dim, page, dtype, garbage=0.0, stats=True)
+    g = torch.Generator().manual_seed(seed)
+    s["k"], s["v"] = (torch.randn(s[x].shape, generator=g).to(dtype) for x in ("k", "v"))
+    table = torch.full((len(lens), max(-(-n // page) for n in lens)), -1, dtype=torch.int32)
+    for i, h in enumerate(held):
+        table[i, h] = s["table"][i, :len(h)]
+    s["table"], s["kv_len"] = table, torch.tensor(lens, dtype=torch.int32)
+    return s
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("heads,kv_heads,dim,new", [(8, 2, 128, 1), (8, 2, 128, 5), (4, 4, 64, 1), (8, 2, 256, 3)])
+@pytest.mark.parametrize("page", [1, 16, 64])
+def test_few_rows_of_sequences_with_more_slots_than_the_pool(dtype, heads, kv_heads, dim, new, page):
+    """There is room for the scores of as many slots as the pool has: those of most units here are formed again."""
+    s = thinned(1, [6000, 4100, 5000, 700], [new, 1, new, 1], heads, kv_heads, dim, page, dtype, (0, 1, 2, 33, 41, -20, -9, -2, -1))
+    for window, first in ((4000, 100), (3000, 7), (6000, 40)):
+        a = check(s, window, first, add_weight=True)
+        b = check(s, window, first, add_weight=True)
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+        check(s, window, first, causal=False, add_weight=True)
 
 
 @pytest.mark.parametrize("heads,kv_heads,dim,lens,new,window,first", [
