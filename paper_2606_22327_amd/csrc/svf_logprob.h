@@ -9,6 +9,11 @@
 
 namespace svfp {
 
+// No lane's reference lies below this in log2 terms: it would be rounded by more than 2^-4, and from some -2^31 on powers relative to it would
+// be infinite.  A lane with lower logits alone (a mask's finite number) adds 0, as it should, where the row has larger ones;
+// where it has none, and where references are as far above 0, all is summed again.
+constexpr float kFarthest = -1048576.f;
+
 struct Args {
     const char* logits;
     const char* token;
@@ -19,7 +24,7 @@ struct Args {
     int32_t* top_index;
     char* ws;
     int64_t row_stride;  // bytes
-    float scale, scale2;  // scale2: times log2(e)
+    float scale, scale2, low;  // scale2: times log2(e); low: the logit that comes to kFarthest
     int32_t rows, vocab, top, token_wide;
 };
 

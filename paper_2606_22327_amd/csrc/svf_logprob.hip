@@ -279,9 +279,9 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan p
             }
         }
         m = fmaxf(m, most);
-        const float far = fmaf(most, c, b);
+        const float ref = fmaxf(most, p.low), far = fmaf(ref, c, b);
         if (__any(far > kSlack)) {
-            const float now = far > kSlack ? -most * c : b, step = now - b, keep = __builtin_amdgcn_exp2f(step);
+            const float now = far > kSlack ? -ref * c : b, step = now - b, keep = __builtin_amdgcn_exp2f(step);
             sumy = keep * fmaf(sum, step, sumy);
             sum *= keep;
             b = now;
@@ -342,12 +342,12 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan p
         const int i = s.edge(tid);
         const float x = (float)s.x[i];
         m = fmaxf(m, x);
-        const float far = fmaf(x, c, b);
+        const float ref = fmaxf(x, p.low), far = fmaf(ref, c, b);
         if (far > kSlack) {
-            const float step = -x * c - b, keep = __builtin_amdgcn_exp2f(step);
+            const float step = -ref * c - b, keep = __builtin_amdgcn_exp2f(step);
             sumy = keep * fmaf(sum, step, sumy);
             sum *= keep;
-            b = -x * c;
+            b = -ref * c;
         }
         const float y = fmaf(x, c, b), e = __builtin_amdgcn_exp2f(y);
         sum += e;
@@ -421,7 +421,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : 6) void k_score(Args p, Plan p
     x.s = x.sy = 0.f, x.before = 0;
     for (int i = 0; i < NT / 64; i++) x.s += group[i].s, x.sy += group[i].sy, x.before += group[i].before;
     // Logits so large that a reference in log2 terms is rounded by more than 2^-4, or none in 32 bits: once more, each distance by itself.
-    if (x.m != -INFINITY && !(fabsf(x.m * c) < 1048576.f) && x.m != INFINITY) {
+    if (x.m != -INFINITY && !(fabsf(x.m * c) < -kFarthest) && x.m != INFINITY) {
         sum = sumy = 0.f;
         for (int i = tid; i < s.count(); i += NT) {
             const float y = distance((float)s.x[s.nth(i)], x.m, c), e = __builtin_amdgcn_exp2f(y);

@@ -80,6 +80,7 @@ int svf_logprob(const svf_logprob_args* a, void* hip_stream) {
     k.ws = static_cast<char*>(a->workspace);
     k.row_stride = a->row_stride * item(a);
     k.scale = a->scale, k.scale2 = scale;
+    k.low = svfp::kFarthest / scale;
     k.rows = a->rows;
     k.vocab = a->vocab;
     k.top = a->top;
