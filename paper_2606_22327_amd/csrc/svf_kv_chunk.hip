@@ -552,7 +552,7 @@ __global__ __launch_bounds__(256) void k_join_chunk(AttendArgs p, ChunkPlan plan
 // A workgroup has 256 slots, 64 for each wave, whose keys stay in registers while the rows'
 // queries pass through LDS, 64 at a time; a lane sums its own rows for 32 slots and the lanes
 // are added at the end, so nothing is added atomically.  2,048 tokens over 14,049 slots of 8 key heads (32 query heads, 218
-// GFLOP, 8.5e8 exponentials) take 326 us; nothing bounds it alone: the matrix units are busy for 0.27 of the cycles, other vector
+// GFLOP, 8.5e8 exponentials) take 300 us; nothing bounds it alone: the matrix units are busy for 0.27 of the cycles, other vector
 // instructions take 0.33, exponentials 0.2 more, and products and exponentials of a tile follow each other.
 //
 // With first tokens (FIRST) a window leaves few slot tiles, and those of the first tokens are seen by every row: rows are split over

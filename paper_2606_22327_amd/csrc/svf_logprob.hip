@@ -127,7 +127,7 @@ __device__ inline V over_group(V x, Op op) {
 }
 
 // Each line of a row is read once, by eight lanes: past the caches (4,001 rows of 128,000, 1,024 MB: 174 us, and 183 through them; 203
-// rows 23.4 and 24.0; 517 rows of 50,001 in 32 bits, whose lines do not begin with a row, 28 both ways, and 30 before the grid began at a line).
+// rows, eight waves each then, 23.4 and 24.0; 517 rows of 50,001 in 32 bits, whose lines do not begin with a row, 28 both ways, and 30 before the grid began at a line).
 __device__ inline uint4 load_once(const uint4* at) {
     typedef uint32_t V4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const V4*)at));
@@ -626,7 +626,7 @@ Layout layout(int32_t rows, int32_t vocab, int32_t top, int32_t dtype) {
     if (parts < least) parts = least;
     if (parts > kMostParts) parts = kMostParts;
     if (parts < 1) parts = 1;
-    // Sixteen waves where a CU has but one row and that is long, for twice the loads on their way (bf16: 203 rows of 128,000, 20 best, 22.3 us
+    // Sixteen waves where a CU has but one row and that is long, for twice the loads on their way (bf16: 203 rows of 128,000, 20 best, 21.5 us
     // and 23.8 with eight, 64 best 26.9 and 30.1, 150 of 151,000 25.3 and 27.7; but 203 of 64,000 18.4 and 18.1, 400 of 128,000 37.5 and 31.8,
     // and one in parts 17.8 and 17.4).
     if (parts == 1 && rows <= 256 && vectors > 12288) y.threads = 1024;

@@ -312,7 +312,7 @@ def attend(q: torch.Tensor, batch: Batch, cache: Cache, causal: bool = True, win
     their sequences' slots: (``out`` like q, ``lse`` float32 [tokens, heads]).
     ``scale`` is 1/sqrt(head_dim) by default; ``window`` > 0 lets a token see that many
     slots up to its own, and the sequence's ``first`` slots besides; pages of slots that no token sees any more may be
-    given back (-1 in the page table).    ``add_weight`` adds every slot's softmax, summed
+    given back (-1 in the page table).  ``add_weight`` adds every slot's softmax, summed
     over the tokens and the query heads that share its key head, to
     ``cache.weight``.  A token that sees no slot has out = 0, lse = -inf."""
     if out is None and q.is_cuda:
